@@ -451,6 +451,73 @@ int det_qdecoder_layer(const det_layer_weights *w, const det_layer_cfg *cfg, voi
                        void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * An 8-bit paged KV cache and attention over it (the paper is silent on the cache; the form keeps section 6.1's contract: a
+ * token's codes are a function of its own row, never of later tokens, so a prompt in one pass and token by token, and a
+ * sequence in whatever pages it lies, give the same bytes).
+ *
+ * A pool is [n_pages, Hkv] records of DET_KV8_RECORD bytes; a record holds DET_KV8_PAGE = 64 tokens of one KV head of D = 128:
+ *     K codes [64][128] int8,  V codes [4][128][16] int8 (token 16 g + i, column d at [g][d][i]),  K scales [64] fp32,  V scales [64] fp32.
+ * The scale's block is one token of one KV head:  amax = max|x|;  d = amax / 127 (fp32);  code = clamp(rint(x / d), -127, 127), 0 if
+ * d == 0;  value = code * d.  A row with an infinity or NaN has codes 0 and the scale NaN.  page_table [n_slots, max_pages] int32 names the
+ * page of tokens 64 i .. 64 i + 63 of a slot; an entry outside 0..n_pages-1 names none.  Pages may be shared between slots and may be
+ * anywhere; what lies in them past a row's length is never used.
+ *   Shapes: D == 128, max_pages <= DET_KV8_MAX_PAGES; pool 16-byte aligned. */
+#define DET_KV8_PAGE 64
+#define DET_KV8_RECORD 16896
+#define DET_KV8_MAX_PAGES 131072
+/* Bytes of a pool (of one layer); 0 if the shape is unsupported. */
+size_t det_kv8_pool_bytes(int n_pages, int Hkv, int D);
+
+/* The rows of a fused projection into the cache.  qkv [R, (Hq + 2 Hkv) D] bf16 with row stride ldqkv (ldqkv % 8 == 0): query heads, key
+ * heads, value heads.  qbuf[r] = det_rope(query heads, positions[r]); the key heads, rotated and rounded to bf16 the same way, and the value
+ * heads are quantized into position positions[r] of slot slots[r] (slots NULL: slot r).  rope_cos/sin [Lrope, D/2] fp32, 16-byte aligned;
+ * the rotation clamps positions to 0..Lrope-1.  A row whose slot, position or page does not exist is written to qbuf only.  No two rows
+ * of one call may name the same (slot, position), nor a page that slots share. */
+int det_kv8_rope_append(const void *qkv, int ldqkv, void *qbuf, void *pool, const int32_t *page_table, int n_pages,
+                        int n_slots, int max_pages, const int32_t *positions, const int32_t *slots, const float *rope_cos,
+                        const float *rope_sin, int R, int Hq, int Hkv, int D, int Lrope, void *stream);
+
+/* k, v [R, Hkv, D] bf16: the values (code * d, rounded once) of position positions[r] of slot slots[r] (NULL: slot r); zeros where there
+ * is no such page. */
+int det_kv8_read(const void *pool, const int32_t *page_table, int n_pages, int n_slots, int max_pages,
+                 const int32_t *positions, const int32_t *slots, void *k, void *v, int R, int Hkv, int D, void *stream);
+
+/* Page dst[i] = page src[i] in every layer of pools [n_layers, n_pages, Hkv] that lie one behind the other, i < n.  A page may be
+ * the source of several copies; no page may be the destination of two, nor of one and a source.  Pairs that name a page outside
+ * 0..n_pages-1 are left out. */
+int det_kv8_copy_pages(void *pool, int n_layers, int n_pages, int Hkv, int D, const int32_t *src, const int32_t *dst, int n,
+                       void *stream);
+
+/* Attention of R rows over the cache: row r, query head h (KV head h / (Hq/Hkv)), the first len = seqlens[r] tokens (clamped to
+ * 0..64 max_pages) of slot slots[r] (NULL: slot r; a slot outside 0..n_slots-1 has no tokens).  Tokens without a page are left out; a row
+ * without any token gives zeros.  Several rows may share a slot (a prompt's rows at lengths 1..T, the rows of drafted tokens).
+ *   s_j = scale * (q . c_j) d^K_j,   out = bf16( sum_j p_j d^V_j c^V_j ),   p = softmax(s).
+ * The order: q's (row, head) as integers n_d = rint(q_d 2^(22-E)), 2^E the power of two above its largest magnitude; n . c_j exact, brought to
+ * fp32 from its digits to base 256.  Chunk c = tokens [256 c, 256 c + 256): in units of log2, m_c = ceil(max s_j), e_j = 2^(s_j - m_c) by the
+ * hardware's exponential, l_c their sum in a fixed order; weights e_j d^V_j as integers rint(w 2^(22-E_c)), 2^E_c above the chunk's largest;
+ * their products with the codes exact.  Chunks are folded in ascending order, relative to the largest m so far.  A row's bytes do not depend
+ * on R, on the other rows, on the pages it lies in or on the call's max_pages.
+ *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  ws: det_attn_decode_kv8_workspace_bytes bytes. */
+size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
+int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
+                        int max_pages, const int32_t *seqlens, const int32_t *slots, void *out, void *ws, size_t ws_bytes,
+                        int R, int Hq, int Hkv, int D, float scale, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Verification of drafted tokens against the target's probabilities, from given random numbers (section 6.6: the tokens are a function of
+ * what is given; nothing is drawn here).  For sequence b with n = n_drafts[b] drafts (n_drafts NULL: N; clamped to 0..N):
+ *   draft i < n is accepted while all before it were and u[b][i] * q[b][i][x_i] < p[b][i][x_i], x_i = drafts[b][i] (decided exactly; an id
+ *   outside 0..V-1 is rejected);  a = the number accepted = accepted[b];
+ *   r_j = max(p[b][a][j] - q[b][a][j], 0) if a < n, else p[b][a][j];  where all r_j are 0, r_j = p[b][a][j] (NaN and negative values count 0);
+ *   the token = smallest j with r_0 + .. + r_j > u[b][N] * sum r (the last j with r_j > 0 if none, 0 if there is none), fp64 sums.
+ *   tokens[b] = x_0 .. x_{a-1}, the token, then -1.
+ * q NULL: the drafts were certain (q = 1 at x_i, 0 elsewhere).
+ *   p [B, N+1, V], q [B, N, V], u [B, N+1] fp32, u in [0, 1);  drafts [B, N], accepted [B], tokens [B, N+1] int32.  p, q 16-byte aligned.
+ *   1 <= N <= 63. */
+int det_verify_drafts(const float *p, const float *q, const int32_t *drafts, const int32_t *n_drafts, const float *u,
+                      int32_t *accepted, int32_t *tokens, int B, int N, int V, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Output commitment (the paper's section 6.7 records SHA256(prompt || logits || tokens) for every
  * execution, and a receipt commits to the output by its hash, section 4.1).  HOST code on HOST
  * pointers: SHA-256 (FIPS 180-4) is a serial chain, so the caller copies what it wants committed

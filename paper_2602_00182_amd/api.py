@@ -25,6 +25,8 @@ __all__ = [
     "det_qgemm_w4a8_swiglu", "det_quant_pack_w4_gate_up", "quant_pack_gate_up", "det_rmsnorm_quant_q8",
     "det_qdecoder_layer_workspace_bytes", "det_qdecoder_layer", "det_attn_decode_quant_q8",
     "det_qgemm_w4a8_swiglu_quant_supported", "det_qgemm_w4a8_swiglu_quant",
+    "KV8_PAGE", "KV8_RECORD", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
+    "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8", "det_verify_drafts",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -703,3 +705,101 @@ def det_next_token(prompts, prompt_lens, last_sampled, tokens_out, positions_out
         _contig(prompts, torch.int32), Tp, _contig(prompt_lens, torch.int32), _contig(last_sampled, torch.int32),
         _contig(tokens_out, torch.int32), _contig(positions_out, torch.int32), _contig(history, torch.int32),
         Th, t, B, _stream(stream)))
+
+
+KV8_PAGE, KV8_RECORD = 64, 16896  # tokens of a page of the 8-bit cache; bytes of a page and KV head
+
+
+def det_kv8_pool_bytes(n_pages: int, Hkv: int, D: int = 128) -> int:
+    return lib().det_kv8_pool_bytes(n_pages, Hkv, D)
+
+
+def kv8_pool(n_layers: int, n_pages: int, Hkv: int, D: int = 128, device="cuda") -> torch.Tensor:
+    """Allocates the pools of n_layers layers, [n_layers, n_pages, Hkv, KV8_RECORD] bytes; the other calls take one layer's."""
+    if n_layers < 1 or det_kv8_pool_bytes(n_pages, Hkv, D) == 0:
+        raise DetError("det_kv8_pool_bytes", 2)
+    return torch.zeros((n_layers, n_pages, Hkv, KV8_RECORD), dtype=torch.uint8, device=device)
+
+
+def _kv8(pool, page_table):
+    """(pool, page_table, n_pages, n_slots, max_pages) of a call, and Hkv."""
+    if pool.dim() != 3 or pool.shape[2] != KV8_RECORD or page_table.dim() != 2:
+        raise ValueError("bad page pool or table")
+    return (_contig(pool, torch.uint8), _contig(page_table, torch.int32), pool.shape[0], page_table.shape[0], page_table.shape[1]), pool.shape[1]
+
+
+def _slots(slots, R: int, n_slots: int):
+    if slots is None:
+        if n_slots < R:
+            raise ValueError("fewer slots than rows")
+        return None
+    if slots.shape != (R,):
+        raise ValueError("bad slots")
+    return _contig(slots, torch.int32)
+
+
+def det_kv8_rope_append(qkv, qbuf, pool, page_table, positions, slots, rope_cos, rope_sin, stream=None) -> None:
+    """qkv [R, (Hq + 2 Hkv) 128]: query heads rotated into qbuf [R, Hq, 128], key heads (rotated) and value heads quantized into the pages
+    of (slot, position).  qkv may be a row-strided view; slots None: row r uses slot r."""
+    R, Hq, D = qbuf.shape
+    cache, Hkv = _kv8(pool, page_table)
+    n = (Hq + 2 * Hkv) * D
+    if qkv.shape != (R, n) or qkv.stride(1) != 1 or positions.shape != (R,):
+        raise ValueError("bad projection rows")
+    if rope_cos.dim() != 2 or rope_cos.shape[1] != D // 2 or rope_sin.shape != rope_cos.shape:
+        raise ValueError("bad rope tables")
+    _check("det_kv8_rope_append", lib().det_kv8_rope_append(
+        _ptr(qkv, torch.bfloat16), _ld(qkv, n), _contig(qbuf, torch.bfloat16), *cache, _contig(positions, torch.int32),
+        _slots(slots, R, page_table.shape[0]), _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), R, Hq, Hkv, D,
+        rope_cos.shape[0], _stream(stream)))
+
+
+def det_kv8_read(pool, page_table, positions, slots, k, v, stream=None) -> None:
+    """k, v [R, Hkv, 128] bf16: the cache's values at (slot, position); slots None: row r reads slot r."""
+    R, Hkv, D = k.shape
+    cache, heads = _kv8(pool, page_table)
+    if heads != Hkv or v.shape != k.shape or positions.shape != (R,):
+        raise ValueError("bad cache rows")
+    _check("det_kv8_read", lib().det_kv8_read(
+        *cache, _contig(positions, torch.int32), _slots(slots, R, page_table.shape[0]), _contig(k, torch.bfloat16),
+        _contig(v, torch.bfloat16), R, Hkv, D, _stream(stream)))
+
+
+def det_kv8_copy_pages(pool, src, dst, stream=None) -> None:
+    """Page dst[i] = page src[i] in every layer of pool [n_layers, n_pages, Hkv, KV8_RECORD]; see the header for what src and dst may name."""
+    if pool.dim() != 4 or pool.shape[3] != KV8_RECORD or src.dim() != 1 or dst.shape != src.shape:
+        raise ValueError("bad page pool or pairs")
+    n_layers, n_pages, Hkv, _ = pool.shape
+    _check("det_kv8_copy_pages", lib().det_kv8_copy_pages(
+        _contig(pool, torch.uint8), n_layers, n_pages, Hkv, 128, _contig(src, torch.int32), _contig(dst, torch.int32), src.shape[0],
+        _stream(stream)))
+
+
+def det_attn_decode_kv8_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_pages: int) -> int:
+    return lib().det_attn_decode_kv8_workspace_bytes(R, Hq, Hkv, D, max_pages)
+
+
+def det_attn_decode_kv8(q, pool, page_table, seqlens, slots, out, ws, scale: float, stream=None) -> None:
+    """out [R, Hq, 128] = attention of q over the first seqlens[r] tokens of slot slots[r] (None: slot r) of the 8-bit cache."""
+    R, Hq, D = q.shape
+    cache, Hkv = _kv8(pool, page_table)
+    if out.shape != q.shape or seqlens.shape != (R,):
+        raise ValueError("bad attention shapes")
+    _check("det_attn_decode_kv8", lib().det_attn_decode_kv8(
+        _contig(q, torch.bfloat16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, page_table.shape[0]),
+        _contig(out, torch.bfloat16), _contig(ws), ws.numel() * ws.element_size(), R, Hq, Hkv, D, scale, _stream(stream)))
+
+
+def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, stream=None) -> None:
+    """Drafted tokens [B, N] against the target's probabilities p [B, N+1, V] and the draft's q [B, N, V] (None: the drafts were certain)
+    with the random numbers u [B, N+1]; n_drafts [B] or None (all N).  accepted [B]; tokens [B, N+1]: the accepted drafts, one more, -1."""
+    B, N = drafts.shape
+    V = p.shape[-1]
+    if p.shape != (B, N + 1, V) or u.shape != (B, N + 1) or accepted.shape != (B,) or tokens.shape != (B, N + 1):
+        raise ValueError("bad verification shapes")
+    if (q is not None and q.shape != (B, N, V)) or (n_drafts is not None and n_drafts.shape != (B,)):
+        raise ValueError("bad verification shapes")
+    _check("det_verify_drafts", lib().det_verify_drafts(
+        _contig(p, torch.float32), None if q is None else _contig(q, torch.float32), _contig(drafts, torch.int32),
+        None if n_drafts is None else _contig(n_drafts, torch.int32), _contig(u, torch.float32), _contig(accepted, torch.int32),
+        _contig(tokens, torch.int32), B, N, V, _stream(stream)))
