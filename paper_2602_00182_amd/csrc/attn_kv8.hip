@@ -90,20 +90,45 @@ __device__ __forceinline__ void fold_step(float& m, float& l, float mc, float lc
     l = __builtin_fmaf(lc, b, l * a);
     m = to;
 }
+__device__ __forceinline__ float fold_value(float o, float oc, float a, float b) { return __builtin_fmaf(oc, b, o * a); }
 // A row that no token reaches has l = 0 and gives zeros.
 __device__ __forceinline__ float attn_quotient(float o, float l) { return l == 0.0f ? 0.0f : o / l; }
 
 // ---------------------------------------------------------------- a tile's query
 
-struct tile_q {
-    v4i digit[3][2];  // lane: pair lane % 16, columns 32 (lane / 16) + 16 h + 0..15 of the digit (0 the highest)
-    float factor[4];  // of the pairs 4 (lane / 16) + 0..3: what an integer score stands for, in units of log2
+// Sixteen consecutive columns of a query as digits: the bytes of one operand of the matrix instruction.
+struct q_digits {
+    v4i d[3];  // the highest digit first
 };
 
-// q: the 128 values of this lane's pair (lane % 16), or null.
-__device__ __forceinline__ void load_q(const uint16_t* q, float scale_log2, tile_q& t)
+// w: eight words of two bf16 each; up = 2^(22 - E).
+__device__ __forceinline__ q_digits cut_query(const uint32_t* w, float up)
 {
-    const int lane = threadIdx.x & 63, group = lane >> 4;
+    q_digits o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // four columns
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = w[2 * k + (i >> 1)];
+            const float x = (i & 1) ? bf16hi_to_f32(pair) : bf16lo_to_f32(pair);
+            // adding 1.5 * 2^23 leaves the nearest integer n in the low bits; + 0x8080 makes bytes 0 and 1 the digits plus 128
+            y[i] = __float_as_uint(__builtin_fmaf(x, up, 12582912.0f)) - 0x4B400000u + 0x8080u;
+        }
+        uint32_t b0, b1, b2;
+        gather_bytes(y, b0, b1, b2);
+        o.d[0][k] = (int)b2;
+        o.d[1][k] = (int)(b1 ^ 0x80808080u);
+        o.d[2][k] = (int)(b0 ^ 0x80808080u);
+    }
+    return o;
+}
+
+// The query of this lane's operand row: q its 128 values (or null), of which the lane takes columns 32 (lane / 16) + 16 h + 0..15.  factor: what an
+// integer score stands for, in units of log2 (NaN for a query that is not finite).
+__device__ __forceinline__ void load_query(const uint16_t* q, float scale_log2, q_digits (&digits)[2], float& factor)
+{
+    const int group = (threadIdx.x & 63) >> 4;
     uint32_t w[16] = {};
     if (q) {
 #pragma unroll
@@ -125,33 +150,10 @@ __device__ __forceinline__ void load_q(const uint16_t* q, float scale_log2, tile
     big = fmaxf(big, __shfl_xor(big, 32, kWave));
     const int e = exponent_above(big);
     const float up = pow2i(22 - e);
-    const float factor = big < __builtin_inff() ? scale_log2 * pow2i(e - 22) : __builtin_nanf("");
-#pragma unroll
-    for (int r = 0; r < 4; ++r) t.factor[r] = __shfl(factor, 4 * group + r, kWave);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {  // four columns
-        uint32_t y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t pair = w[2 * k + (i >> 1)];
-            const float x = (i & 1) ? bf16hi_to_f32(pair) : bf16lo_to_f32(pair);
-            // adding 1.5 * 2^23 leaves the nearest integer n in the low bits; + 0x8080 makes bytes 0 and 1 the digits plus 128
-            y[i] = __float_as_uint(__builtin_fmaf(x, up, 12582912.0f)) - 0x4B400000u + 0x8080u;
-        }
-        uint32_t b0, b1, b2;
-        gather_bytes(y, b0, b1, b2);
-        t.digit[0][k >> 2][k & 3] = (int)b2;
-        t.digit[1][k >> 2][k & 3] = (int)(b1 ^ 0x80808080u);
-        t.digit[2][k >> 2][k & 3] = (int)(b0 ^ 0x80808080u);
-    }
+    factor = big < __builtin_inff() ? scale_log2 * pow2i(e - 22) : __builtin_nanf("");
+    digits[0] = cut_query(w, up);
+    digits[1] = cut_query(w + 8, up);
 }
-
-// ---------------------------------------------------------------- one chunk of one slot, one wave
-
-struct chunk_result {
-    float m[4], l[4];    // of the pairs 4 (lane / 16) + 0..3
-    float o[8][4];       // of the same pairs, column 16 n + lane % 16
-};
 
 __device__ __forceinline__ void wave_lds_order()
 {
@@ -159,156 +161,89 @@ __device__ __forceinline__ void wave_lds_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-// len: tokens that each of this lane's four pairs sees of the slot; longest: the largest of the tile's.  digits: 3 * 16 * kDigitStride bytes of LDS
-// of this wave.
-__device__ __forceinline__ void attend_chunk(const kv8_cache& c, const tile_q& q, int slot, int kvh, int chunk, const int (&len)[4], int longest,
-                                             uint8_t* digits, chunk_result& res)
+// Length of a row of the call: 0 where its slot is none.
+__device__ __forceinline__ int row_length(const kv8_attn_args& a, int row, int& slot)
 {
-    const int lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
-    const v4i zero = {0, 0, 0, 0};
-    const uint8_t* rec[kChunkPages];
-#pragma unroll
-    for (int p = 0; p < kChunkPages; ++p) {
-        const int page = chunk * kChunkPages + p;
-        rec[p] = page * kPage < longest ? kv8_record(c, slot, page, kvh) : nullptr;
-    }
-
-    float s[kChunkPages][4][4];  // page, token 4 col + t, pair
-    float dv[kChunkPages][4];
-#pragma unroll
-    for (int p = 0; p < kChunkPages; ++p) {
-        if (!rec[p]) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                dv[p][t] = 0.0f;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[p][t][r] = -__builtin_inff();
-            }
-            continue;
-        }
-        const float4 ks = *reinterpret_cast<const float4*>(rec[p] + kRecordKs + 16 * col);
-        const float4 vs = *reinterpret_cast<const float4*>(rec[p] + kRecordVs + 16 * col);
-        float dk[4] = {ks.x, ks.y, ks.z, ks.w};
-        const float dvr[4] = {vs.x, vs.y, vs.z, vs.w};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            // a V row that is not finite poisons its token's score: the rows that see the token become NaN, the others do not
-            dk[t] = dk[t] + 0.0f * dvr[t];
-            dv[p][t] = fabsf(dvr[t]) < __builtin_inff() ? dvr[t] : 0.0f;
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const uint8_t* row = rec[p] + (4 * col + t) * kHeadDim + 32 * group;
-            const v4i k0 = *reinterpret_cast<const v4i*>(row), k1 = *reinterpret_cast<const v4i*>(row + 16);
-            v4i d[3];
-#pragma unroll
-            for (int g = 0; g < 3; ++g) {
-                d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.digit[g][0], k0, zero, 0, 0, 0);
-                d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.digit[g][1], k1, d[g], 0, 0, 0);
-            }
-            const int token = chunk * kChunk + p * kPage + 4 * col + t;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float low = (float)(d[1][r] * 256 + d[2][r]) * q.factor[r];
-                const float x = __builtin_fmaf((float)d[0][r], 65536.0f * q.factor[r], low) * dk[t];
-                s[p][t][r] = token < len[r] ? x : -__builtin_inff();
-            }
-        }
-    }
-
-    // softmax of the chunk relative to an integer power of two; weights against the largest of them
-    float safe[4], up[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float m = -__builtin_inff();
-#pragma unroll
-        for (int p = 0; p < kChunkPages; ++p)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) m = fmaxf(m, s[p][t][r]);
-        m = __builtin_ceilf(row_max(m));
-        res.m[r] = m;
-        safe[r] = m == -__builtin_inff() ? 0.0f : m;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float sum[kChunkPages], w = 0.0f;
-#pragma unroll
-        for (int p = 0; p < kChunkPages; ++p) {
-            float e[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                e[t] = __builtin_amdgcn_exp2f(s[p][t][r] - safe[r]);
-                s[p][t][r] = e[t] * dv[p][t];
-                w = fmaxf(w, s[p][t][r]);
-            }
-            sum[p] = (e[0] + e[1]) + (e[2] + e[3]);
-        }
-        res.l[r] = row_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
-        const int e = exponent_above(row_max(w));
-        up[r] = pow2i(22 - e);
-        safe[r] = pow2i(e - 22);
-    }
-
-    v4i acc[3][8];
-#pragma unroll
-    for (int g = 0; g < 3; ++g)
-#pragma unroll
-        for (int n = 0; n < 8; ++n) acc[g][n] = zero;
-#pragma unroll
-    for (int p = 0; p < kChunkPages; ++p) {
-        if (!rec[p]) continue;
-        wave_lds_order();
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            uint32_t y[4], b0, b1, b2;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(s[p][t][r], up[r], 8421504.0f));  // 2^23 + 0x8080
-            gather_bytes(y, b0, b1, b2);
-            uint8_t* at = digits + (4 * group + r) * kDigitStride + 4 * col;
-            *reinterpret_cast<uint32_t*>(at) = b2;
-            *reinterpret_cast<uint32_t*>(at + kPairs * kDigitStride) = b1 ^ 0x80808080u;
-            *reinterpret_cast<uint32_t*>(at + 2 * kPairs * kDigitStride) = b0 ^ 0x80808080u;
-        }
-        wave_lds_order();
-        v4i w[3];
-#pragma unroll
-        for (int g = 0; g < 3; ++g) w[g] = *reinterpret_cast<const v4i*>(digits + (g * kPairs + col) * kDigitStride + 16 * group);
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const v4i v = *reinterpret_cast<const v4i*>(rec[p] + kRecordV + group * (16 * kHeadDim) + (16 * n + col) * 16);
-#pragma unroll
-            for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, acc[g][n], 0, 0, 0);
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            res.o[n][r] = __builtin_fmaf((float)acc[0][n][r], 65536.0f, (float)(acc[1][n][r] * 256 + acc[2][n][r])) * safe[r];
+    slot = a.slots ? a.slots[row] : row;
+    const long long n = (long long)a.seqlens[row] + a.len_offset, most = (long long)a.c.max_pages * kPage;
+    return (unsigned)slot < (unsigned)a.c.n_slots ? (int)(n < 0 ? 0 : (n > most ? most : n)) : 0;
 }
 
-// ---------------------------------------------------------------- kernels
-
-// One wave: a tile of up to sixteen (row, head) pairs that read one KV head, one chunk.  Rows of a tile may name different slots: those
-// that name the same one go through it together, one slot after the other.  Grid (KV heads, tiles, chunks).
-__global__ __launch_bounds__(64, 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
+// What a score's token contributes with: d^K, poisoned where the token's V row is not finite (the rows that see the token become NaN, the others
+// do not), and d^V, 0 there.
+__device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float (&dk)[4], float (&dv)[4])
 {
-    __shared__ __attribute__((aligned(16))) uint8_t digits[3 * kPairs * kDigitStride];
-    const int lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
+    const float4 ks = *reinterpret_cast<const float4*>(rec + kRecordKs + 16 * col);
+    const float4 vs = *reinterpret_cast<const float4*>(rec + kRecordVs + 16 * col);
+    const float k[4] = {ks.x, ks.y, ks.z, ks.w}, v[4] = {vs.x, vs.y, vs.z, vs.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        dk[t] = k[t] + 0.0f * v[t];
+        dv[t] = fabsf(v[t]) < __builtin_inff() ? v[t] : 0.0f;
+    }
+}
+
+// A score in units of log2 from its digit sums.
+__device__ __forceinline__ float score_of(int d0, int d1, int d2, float factor, float dk)
+{
+    return __builtin_fmaf((float)d0, 65536.0f * factor, (float)(d1 * 256 + d2) * factor) * dk;
+}
+
+// ---------------------------------------------------------------- a chunk by four waves, a page each
+
+// One chunk for a tile of up to sixteen (row, head) pairs that read one KV head.  Rows of a tile may name different slots: those that name the
+// same one go through it together, one slot after the other.  Grid (KV heads, tiles, chunks).
+//
+// PACK: up to four pairs (one row of up to four heads a KV head).  Their digits fill the sixteen rows of one operand, row 4 pair + digit, so a
+// product is one instruction instead of three and a lane has all digits of one pair: a quarter of the scores' arithmetic.
+// All of a page's loads are asked for before the first is used; the workgroups of a compute unit hide one another's way to memory.
+template <bool PACK>
+__global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
+{
+    constexpr int NP = PACK ? 1 : 4;                 // pairs of a lane
+    constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
+    constexpr int SUMS = PACK ? 144 : 132;           // words of a pair's sums: lanes of different pairs meet in no bank
+    __shared__ __attribute__((aligned(16))) uint8_t digits[4][DIGITS * kPairs * kDigitStride];
+    __shared__ float top[2][4][PAIRS];               // largest score, largest weight of each wave
+    __shared__ float lsum[4][PAIRS][16];
+    __shared__ int sums[PACK ? 4 : 1][2][PAIRS * SUMS];  // digit sums of the values: the high one, the two low ones together
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, group = lane >> 4, col = lane & 15;
     const int kvh = blockIdx.x, chunk = blockIdx.z;
-    // this lane's pair: col
-    const int row = blockIdx.y * a.rows_per_tile + col / a.G, head = kvh * a.G + col % a.G;
-    const bool live = col < a.rows_per_tile * a.G && row < a.R;
-    int len = 0, slot = -1;
-    if (live) {
-        slot = a.slots ? a.slots[row] : row;
-        const long long n = (long long)a.seqlens[row] + a.len_offset, most = (long long)a.c.max_pages * kPage;
-        len = (unsigned)slot < (unsigned)a.c.n_slots ? (int)(n < 0 ? 0 : (n > most ? most : n)) : 0;
+    const int row0 = blockIdx.y * a.rows_per_tile;
+    // pair number `col` of the tile
+    const bool live = col < a.rows_per_tile * a.G && row0 + col / a.G < a.R;
+    int slot = -1, len = 0;
+    if (live) len = row_length(a, row0 + col / a.G, slot);
+    // chunk 0 also answers for rows that see nothing
+    if (chunk == 0) {
+        for (int p = wave; p < a.rows_per_tile * a.G; p += 4) {
+            if (row0 + p / a.G < a.R && __builtin_amdgcn_readlane(len, p) == 0)
+                reinterpret_cast<uint32_t*>(a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim)[lane] = 0u;
+        }
     }
     unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
     if (todo == 0) return;
-    tile_q q;
-    load_q(live ? a.q + ((size_t)row * a.Hq + head) * kHeadDim : nullptr, a.scale_log2, q);
+
+    const int qp = PACK ? col >> 2 : col;  // the pair of this lane's operand row
+    q_digits qd[2];
+    float factor;
+    load_query(qp < a.rows_per_tile * a.G && row0 + qp / a.G < a.R ? a.q + ((size_t)(row0 + qp / a.G) * a.Hq + kvh * a.G + qp % a.G) * kHeadDim : nullptr,
+               a.scale_log2, qd, factor);
+    float factors[NP];
+#pragma unroll
+    for (int r = 0; r < NP; ++r) factors[r] = __shfl(factor, PACK ? 4 * group : 4 * group + r, kWave);
+    if constexpr (PACK) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int dg = col & 3;
+                qd[h].d[0][i] = dg == 0 ? qd[h].d[0][i] : dg == 1 ? qd[h].d[1][i] : dg == 2 ? qd[h].d[2][i] : 0;
+            }
+    }
+
+    const v4i zero = {0, 0, 0, 0};
+    bool first = true;
     while (todo != 0) {
         const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
         const int mine = slot == now ? len : 0;
@@ -317,40 +252,190 @@ __global__ __launch_bounds__(64, 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
         int longest = mine;
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
-        int lens[4];
+        int lens[NP];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) lens[r] = __shfl(mine, 4 * group + r, kWave);
-        chunk_result res;
-        attend_chunk(a.c, q, now, kvh, chunk, lens, __builtin_amdgcn_readfirstlane(longest), digits, res);
+        for (int r = 0; r < NP; ++r) lens[r] = __shfl(mine, PACK ? group : 4 * group + r, kWave);
+        const int page = chunk * kChunkPages + wave;
+        const uint8_t* rec = page * kPage < __builtin_amdgcn_readfirstlane(longest) ? kv8_record(a.c, now, page, kvh) : nullptr;
+        if (!first) __syncthreads();  // the last slot's sums have been read
+        first = false;
+
+        float s[4][NP], dv[4] = {};
+        v4i vc[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int pair = 4 * group + r;
-            if (!((members >> pair) & 1u)) continue;
-            const size_t at = ((size_t)(blockIdx.y * a.rows_per_tile + pair / a.G) * a.Hq + kvh * a.G + pair % a.G) * a.chunks + chunk;
-            if (col == 0) {
-                a.part_m[at] = res.m[r];
-                a.part_l[at] = res.l[r];
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
+        if (rec) {
+            v4i kc[4][2];
+            float dk[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kc[t][h] = *reinterpret_cast<const v4i*>(rec + (4 * col + t) * kHeadDim + 32 * group + 16 * h);
+            token_scales(rec, col, dk, dv);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) vc[n] = *reinterpret_cast<const v4i*>(rec + kRecordV + group * (16 * kHeadDim) + (16 * n + col) * 16);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v4i d[DIGITS];
+#pragma unroll
+                for (int g = 0; g < DIGITS; ++g) {
+                    d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
+                    d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
+                }
+                const int token = page * kPage + 4 * col + t;
+#pragma unroll
+                for (int r = 0; r < NP; ++r) {
+                    float x;
+                    if constexpr (PACK) x = score_of(d[0][0], d[0][1], d[0][2], factors[0], dk[t]);
+                    else x = score_of(d[0][r], d[1][r], d[2][r], factors[r], dk[t]);
+                    s[t][r] = token < lens[r] ? x : -__builtin_inff();
+                }
             }
+        }
 #pragma unroll
-            for (int n = 0; n < 8; ++n) a.part_o[at * kHeadDim + 16 * n + col] = res.o[n][r];
+        for (int r = 0; r < NP; ++r) {
+            const float m = row_max(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r])));
+            if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
+        }
+        if constexpr (!PACK) {
+            for (int i = tid; i < PAIRS * SUMS; i += 256) sums[0][0][i] = sums[0][1][i] = 0;
+        }
+        __syncthreads();
+        float mc[NP];
+#pragma unroll
+        for (int r = 0; r < NP; ++r) {
+            const int p = PACK ? group : 4 * group + r;
+            mc[r] = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
+            const float safe = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+            float e[4], w = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                e[t] = __builtin_amdgcn_exp2f(s[t][r] - safe);
+                s[t][r] = e[t] * dv[t];
+                w = fmaxf(w, s[t][r]);
+            }
+            lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
+            w = row_max(w);
+            if (col == 0) top[1][wave][p] = w;
+        }
+        __syncthreads();
+        float up[NP];
+#pragma unroll
+        for (int r = 0; r < NP; ++r) {
+            const int p = PACK ? group : 4 * group + r;
+            up[r] = pow2i(22 - exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))));
+        }
+        v4i acc[DIGITS][8];
+        if (rec) {
+#pragma unroll
+            for (int r = 0; r < NP; ++r) {
+                uint32_t y[4], b[3];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(s[t][r], up[r], 8421504.0f));  // 2^23 + 0x8080
+                gather_bytes(y, b[2], b[1], b[0]);
+                b[1] ^= 0x80808080u;
+                b[2] ^= 0x80808080u;
+                // operand rows: PACK 4 pair + digit; else one operand a digit, row = pair
+#pragma unroll
+                for (int g = 0; g < 3; ++g)
+                    *reinterpret_cast<uint32_t*>(digits[wave] + (PACK ? 4 * group + g : g * kPairs + 4 * group + r) * kDigitStride + 4 * col) = b[g];
+                if constexpr (PACK) *reinterpret_cast<uint32_t*>(digits[wave] + (4 * group + 3) * kDigitStride + 4 * col) = 0u;
+            }
+            wave_lds_order();
+            v4i w[DIGITS];
+#pragma unroll
+            for (int g = 0; g < DIGITS; ++g) w[g] = *reinterpret_cast<const v4i*>(digits[wave] + (g * kPairs + col) * kDigitStride + 16 * group);
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int g = 0; g < DIGITS; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], vc[n], zero, 0, 0, 0);
+            if constexpr (!PACK) {
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {  // integers: the order of these additions changes nothing
+                        const int at = (4 * group + r) * SUMS + 16 * n + col;
+                        atomicAdd(&sums[0][0][at], acc[0][n][r]);
+                        atomicAdd(&sums[0][1][at], acc[1][n][r] * 256 + acc[2][n][r]);
+                    }
+            }
+        }
+        if constexpr (PACK) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                sums[wave][0][group * SUMS + 16 * n + col] = rec ? acc[0][n][0] : 0;
+                sums[wave][1][group * SUMS + 16 * n + col] = rec ? acc[0][n][1] * 256 + acc[0][n][2] : 0;
+            }
+        }
+        __syncthreads();
+
+        // the chunk's result: a wave takes a pair at a time, a lane two columns
+        for (int p = wave; p < PAIRS; p += 4) {
+            if (!((members >> p) & 1u)) continue;
+            const float lc = row_sum((lsum[0][p][col] + lsum[1][p][col]) + (lsum[2][p][col] + lsum[3][p][col]));
+            const float m = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
+            const float down = pow2i(exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))) - 22);
+            float o[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                int hi = 0, lo = 0;
+#pragma unroll
+                for (int w = 0; w < (PACK ? 4 : 1); ++w) {
+                    hi += sums[w][0][p * SUMS + 2 * lane + k];
+                    lo += sums[w][1][p * SUMS + 2 * lane + k];
+                }
+                o[k] = __builtin_fmaf((float)hi, 65536.0f, (float)lo) * down;
+            }
+            const size_t head = (size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G;
+            if (__builtin_amdgcn_readlane(len, p) <= kChunk) {  // the row's only chunk
+                float fm = -__builtin_inff(), l = 0.0f, fa, fb;
+                fold_step(fm, l, m, lc, fa, fb);
+                reinterpret_cast<uint32_t*>(a.out + head * kHeadDim)[lane] =
+                    pack_bf16x2(attn_quotient(fold_value(0.0f, o[0], fa, fb), l), attn_quotient(fold_value(0.0f, o[1], fa, fb), l));
+            } else {
+                const size_t at = head * a.chunks + chunk;
+                if (lane == 0) {
+                    a.part_m[at] = m;
+                    a.part_l[at] = lc;
+                }
+                reinterpret_cast<float2*>(a.part_o + at * kHeadDim)[lane] = make_float2(o[0], o[1]);
+            }
         }
     }
 }
 
-// The chunks of one (row, head), folded in ascending order.  Grid (R * Hq), one column a thread.
+// The chunks of one (row, head) of more than one chunk, folded in ascending order.  Grid (R * Hq), one column a thread; a block of chunks is asked
+// for at once.
 __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
 {
+    constexpr int AHEAD = 16;
     const size_t at = blockIdx.x;
-    const int row = (int)(at / a.Hq);
-    const int slot = a.slots ? a.slots[row] : row;
-    const long long n = (long long)a.seqlens[row] + a.len_offset, most = (long long)a.c.max_pages * kPage;
-    const int len = (unsigned)slot < (unsigned)a.c.n_slots ? (int)(n < 0 ? 0 : (n > most ? most : n)) : 0;
+    int slot;
+    const int len = row_length(a, (int)(at / a.Hq), slot);
+    if (len <= kChunk) return;
     const int chunks = (len + kChunk - 1) / kChunk;
+    const float* pm = a.part_m + at * a.chunks;
+    const float* pl = a.part_l + at * a.chunks;
+    const float* po = a.part_o + at * a.chunks * kHeadDim + threadIdx.x;
     float m = -__builtin_inff(), l = 0.0f, o = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
-        float fa, fb;
-        fold_step(m, l, a.part_m[at * a.chunks + c], a.part_l[at * a.chunks + c], fa, fb);
-        o = __builtin_fmaf(a.part_o[(at * a.chunks + c) * kHeadDim + threadIdx.x], fb, o * fa);
+    for (int c0 = 0; c0 < chunks; c0 += AHEAD) {
+        float x[AHEAD], xm[AHEAD], xl[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int c = min(c0 + k, chunks - 1);
+            xm[k] = pm[c];
+            xl[k] = pl[c];
+            x[k] = po[(size_t)c * kHeadDim];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {  // past the last chunk: one without tokens, which changes nothing
+            const bool there = c0 + k < chunks;
+            float fa, fb;
+            fold_step(m, l, there ? xm[k] : -__builtin_inff(), there ? xl[k] : 0.0f, fa, fb);
+            o = fold_value(o, there ? x[k] : 0.0f, fa, fb);
+        }
     }
     a.out[at * kHeadDim + threadIdx.x] = f32_to_bf16_rne(attn_quotient(o, l));
 }
@@ -380,7 +465,8 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.R = R;
     a.Hq = Hq;
     a.G = Hq / cache.Hkv;
-    a.rows_per_tile = kPairs / a.G;
+    const bool packed = !slots && a.G <= 4;  // rows that share nothing, one to a tile
+    a.rows_per_tile = slots ? kPairs / a.G : 1;
     a.len_offset = len_offset;
     a.chunks = (cache.max_pages + kChunkPages - 1) / kChunkPages;
     a.scale_log2 = scale * 1.44269504f;
@@ -390,8 +476,10 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.part_l = a.part_m + pairs;
     const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
     if (tiles > 65535 || a.chunks > 65535 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
-    hipLaunchKernelGGL(kv8_attn_chunk_kernel, dim3(cache.Hkv, (unsigned)tiles, a.chunks), dim3(64), 0, s, a);
-    hipLaunchKernelGGL(kv8_attn_combine_kernel, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);
+    const dim3 grid(cache.Hkv, (unsigned)tiles, a.chunks);
+    if (packed) hipLaunchKernelGGL(kv8_attn_chunk_kernel<true>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(kv8_attn_chunk_kernel<false>, grid, dim3(256), 0, s, a);
+    if (a.chunks > 1) hipLaunchKernelGGL(kv8_attn_combine_kernel, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);
     return check_launch();
 }
 
