@@ -440,6 +440,193 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
     a.out[at * kHeadDim + threadIdx.x] = f32_to_bf16_rne(attn_quotient(o, l));
 }
 
+// ---------------------------------------------------------------- many rows: a wave walks the chunks of its tile
+
+// One wave: a tile of up to sixteen (row, head) pairs that read one KV head goes through all their chunks, the running softmax in registers: nothing
+// is stored between, and a tile's rows (of one prompt, mostly) share every read.  Rows that name different slots are walked one slot after the
+// other.  Four neighbouring tiles to a workgroup, so that they find one another's pages in the cache of their compute unit; the last rows, which
+// have most to read, begin.  Grid (KV heads, tiles / 4).
+constexpr int kWalkStride = kChunk + 16;  // bytes of a pair's digits of a chunk
+__global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a, int tiles)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t digits_of[4][3 * kPairs * kWalkStride];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
+    uint8_t* digits = digits_of[wave];
+    const int kvh = blockIdx.x, tile = 4 * (gridDim.y - 1 - blockIdx.y) + wave;
+    if (tile >= tiles) return;
+    const int row0 = tile * a.rows_per_tile;
+    const bool live = col < a.rows_per_tile * a.G && row0 + col / a.G < a.R;
+    int slot = -1, len = 0;
+    if (live) len = row_length(a, row0 + col / a.G, slot);
+    q_digits qd[2];
+    float factor, factors[4];
+    load_query(live ? a.q + ((size_t)(row0 + col / a.G) * a.Hq + kvh * a.G + col % a.G) * kHeadDim : nullptr, a.scale_log2, qd, factor);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
+    const v4i zero = {0, 0, 0, 0};
+
+    unsigned todo = (unsigned)(__ballot(live) & 0xFFFFull);
+    while (todo != 0) {
+        const int lead = __builtin_ctz(todo);
+        const int now = __builtin_amdgcn_readlane(slot, lead);
+        const unsigned members = (unsigned)(__ballot(live && slot == now) & 0xFFFFull);
+        todo &= ~members;
+        const bool mine = (members >> col) & 1u;
+        int longest = mine ? len : 0, shortest = mine ? len : 0x7FFFFFFF;
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) {
+            longest = max(longest, __shfl_xor(longest, off, kWave));
+            shortest = min(shortest, __shfl_xor(shortest, off, kWave));
+        }
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        shortest = __builtin_amdgcn_readfirstlane(shortest);
+        float m[4], l[4], o[8][4];
+        int lens[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            lens[r] = __shfl(mine ? len : 0, 4 * group + r, kWave);
+            m[r] = -__builtin_inff();
+            l[r] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) o[n][r] = 0.0f;
+        }
+        for (int chunk = 0; chunk * kChunk < longest; ++chunk) {
+            const uint8_t* rec[kChunkPages];
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                const int page = chunk * kChunkPages + p;
+                rec[p] = page * kPage < longest ? kv8_record(a.c, now, page, kvh) : nullptr;
+            }
+            float s[kChunkPages][4][4];  // page, token 4 col + t, pair
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                if (rec[p]) {
+                    v4i kc[4][2];
+                    float dk[4], dv[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) kc[t][h] = *reinterpret_cast<const v4i*>(rec[p] + (4 * col + t) * kHeadDim + 32 * group + 16 * h);
+                    token_scales(rec[p], col, dk, dv);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        v4i d[3];
+#pragma unroll
+                        for (int g = 0; g < 3; ++g) {
+                            d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
+                            d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[p][t][r] = score_of(d[0][r], d[1][r], d[2][r], factors[r], dk[t]);
+                    }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[p][t][r] = -__builtin_inff();
+                }
+            }
+            if ((chunk + 1) * kChunk > shortest) {
+#pragma unroll
+                for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const int token = chunk * kChunk + p * kPage + 4 * col + t;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? s[p][t][r] : -__builtin_inff();
+                    }
+            }
+            float mc[4], safe[4], sum[4], top[4], lc[4], down[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x = -__builtin_inff();
+#pragma unroll
+                for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) x = fmaxf(x, s[p][t][r]);
+                mc[r] = __builtin_ceilf(row_max(x));
+                safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+                top[r] = 0.0f;
+            }
+            float sums[kChunkPages][4];
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                float dk[4], dv[4] = {};
+                if (rec[p]) token_scales(rec[p], col, dk, dv);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float e[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        e[t] = __builtin_amdgcn_exp2f(s[p][t][r] - safe[r]);
+                        s[p][t][r] = e[t] * dv[t];
+                        top[r] = fmaxf(top[r], s[p][t][r]);
+                    }
+                    sums[p][r] = (e[0] + e[1]) + (e[2] + e[3]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                lc[r] = row_sum((sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]));
+                const int e = exponent_above(row_max(top[r]));
+                sum[r] = pow2i(22 - e);
+                down[r] = pow2i(e - 22);
+            }
+            wave_lds_order();
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t y[4], b0, b1, b2;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(s[p][t][r], sum[r], 8421504.0f));  // 2^23 + 0x8080
+                    gather_bytes(y, b0, b1, b2);
+                    uint8_t* at = digits + (4 * group + r) * kWalkStride + p * kPage + 4 * col;
+                    *reinterpret_cast<uint32_t*>(at) = b2;
+                    *reinterpret_cast<uint32_t*>(at + kPairs * kWalkStride) = b1 ^ 0x80808080u;
+                    *reinterpret_cast<uint32_t*>(at + 2 * kPairs * kWalkStride) = b0 ^ 0x80808080u;
+                }
+            wave_lds_order();
+            v4i acc[3][8];
+#pragma unroll
+            for (int g = 0; g < 3; ++g)
+#pragma unroll
+                for (int n = 0; n < 8; ++n) acc[g][n] = zero;
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                if (!rec[p]) continue;
+                v4i w[3];
+#pragma unroll
+                for (int g = 0; g < 3; ++g) w[g] = *reinterpret_cast<const v4i*>(digits + (g * kPairs + col) * kWalkStride + p * kPage + 16 * group);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const v4i v = *reinterpret_cast<const v4i*>(rec[p] + kRecordV + group * (16 * kHeadDim) + (16 * n + col) * 16);
+#pragma unroll
+                    for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, acc[g][n], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float fa, fb;
+                fold_step(m[r], l[r], mc[r], lc[r], fa, fb);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float oc = __builtin_fmaf((float)acc[0][n][r], 65536.0f, (float)(acc[1][n][r] * 256 + acc[2][n][r])) * down[r];
+                    o[n][r] = fold_value(o[n][r], oc, fa, fb);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int p = 4 * group + r;
+            if (!((members >> p) & 1u)) continue;
+            uint16_t* out = a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) out[16 * n + col] = f32_to_bf16_rne(attn_quotient(o[n][r], l[r]));
+        }
+    }
+}
+
 static size_t workspace_bytes(int R, int Hq, int max_pages)
 {
     const size_t chunks = ((size_t)max_pages + kChunkPages - 1) / kChunkPages;
@@ -475,6 +662,10 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.part_m = a.part_o + pairs * kHeadDim;
     a.part_l = a.part_m + pairs;
     const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
+    if (slots && tiles * cache.Hkv >= 2048) {
+        hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3(cache.Hkv, (unsigned)((tiles + 3) / 4)), dim3(256), 0, s, a, (int)tiles);
+        return check_launch();
+    }
     if (tiles > 65535 || a.chunks > 65535 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
     const dim3 grid(cache.Hkv, (unsigned)tiles, a.chunks);
     if (packed) hipLaunchKernelGGL(kv8_attn_chunk_kernel<true>, grid, dim3(256), 0, s, a);

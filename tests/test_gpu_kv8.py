@@ -209,9 +209,10 @@ def test_rows_that_share_slots_in_any_order(d, Hq, Hkv):
         assert np.array_equal(down_bf16(one)[0], got[r]), rows[r]
 
 
-def test_prompt_rows_are_the_tokens_decoded_one_by_one(d):
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (32, 8), (16, 16), (8, 1), (15, 5)])
+def test_prompt_rows_are_the_tokens_decoded_one_by_one(d, Hq, Hkv):
     """Many rows of a prompt in one call against calls of one row: the same bytes whatever form the sizes select."""
-    lengths, Hq, Hkv = [1203, 700, 389], 8, 2
+    lengths = [1203, 700, 389]
     cache = Cache(7340, lengths, Hkv)
     slots = np.repeat(np.arange(3), lengths).astype(np.int32)
     lens = np.concatenate([np.arange(1, n + 1) for n in lengths]).astype(np.int32)
