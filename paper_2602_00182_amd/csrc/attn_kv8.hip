@@ -8,7 +8,10 @@
 //            the cache holds to half a code only.
 // Softmax: a chunk's reference m_c is an integer (the ceiling of its largest score in units of log2), so the factors by which chunks are
 // brought together are powers of two.  Chunks are folded in ascending order.
+#include <type_traits>
+
 #include "kv8.h"
+#include "stream.h"
 
 namespace det {
 
@@ -25,9 +28,8 @@ struct kv8_attn_args {
     const int32_t* seqlens;
     const int32_t* slots;
     uint16_t* out;  // [R, Hq, 128]
-    float* part_m;  // [R, Hq, chunks]
-    float* part_l;
-    float* part_o;  // [R, Hq, chunks, 128]
+    float* part_o;  // [R, Hq, chunks, 128]: a chunk's weighted sums, in units of its 2^(E-22)
+    float4* part;   // [R, Hq, chunks]: its m, l, 2^(E-22)
     int R, Hq, G, rows_per_tile, len_offset, chunks;
     float scale_log2;  // scale * log2(e)
 };
@@ -80,17 +82,19 @@ __device__ __forceinline__ float row_sum(float v)
     return v + row_ror<1>(v);
 }
 
-// The running softmax of a row: weights relative to 2^m, their sum l.  fold_step joins a chunk's (mc, lc) and gives the factors of the
-// sums so far (a) and of the chunk's (b).
-__device__ __forceinline__ void fold_step(float& m, float& l, float mc, float lc, float& a, float& b)
+// The running softmax of a row: weights relative to 2^m, their sum l.  fold_step joins a chunk's (mc, lc), whose sums are in units of `unit`, and
+// gives the factors of the sums so far (a) and of the chunk's (b): powers of two, so where a rounding falls does not hang on when they are applied.
+__device__ __forceinline__ void fold_step(float& m, float& l, float mc, float lc, float unit, float& a, float& b)
 {
     const float to = fmaxf(m, mc);
     a = pow2_step(m, to);
     b = pow2_step(mc, to);
     l = __builtin_fmaf(lc, b, l * a);
+    b = b * unit;
     m = to;
 }
 __device__ __forceinline__ float fold_value(float o, float oc, float a, float b) { return __builtin_fmaf(oc, b, o * a); }
+__device__ __forceinline__ float digits_value(int d0, int d1, int d2) { return __builtin_fmaf((float)d0, 65536.0f, (float)(d1 * 256 + d2)); }
 // A row that no token reaches has l = 0 and gives zeros.
 __device__ __forceinline__ float attn_quotient(float o, float l) { return l == 0.0f ? 0.0f : o / l; }
 
@@ -124,7 +128,7 @@ __device__ __forceinline__ q_digits cut_query(const uint32_t* w, float up)
     return o;
 }
 
-// The query of this lane's operand row: q its 128 values (or null), of which the lane takes columns 32 (lane / 16) + 16 h + 0..15.  factor: what an
+// The query of this lane's operand row: q its 128 values (or null), of which the lane takes columns 64 h + 16 (lane / 16) + 0..15.  factor: what an
 // integer score stands for, in units of log2 (NaN for a query that is not finite).
 __device__ __forceinline__ void load_query(const uint16_t* q, float scale_log2, q_digits (&digits)[2], float& factor)
 {
@@ -133,7 +137,7 @@ __device__ __forceinline__ void load_query(const uint16_t* q, float scale_log2, 
     if (q) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint4 x = *reinterpret_cast<const uint4*>(q + 32 * group + 8 * k);
+            const uint4 x = *reinterpret_cast<const uint4*>(q + 64 * (k >> 1) + 16 * group + 8 * (k & 1));
             w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
         }
     }
@@ -150,9 +154,16 @@ __device__ __forceinline__ void load_query(const uint16_t* q, float scale_log2, 
     big = fmaxf(big, __shfl_xor(big, 32, kWave));
     const int e = exponent_above(big);
     const float up = pow2i(22 - e);
-    factor = big < __builtin_inff() ? scale_log2 * pow2i(e - 22) : __builtin_nanf("");
+    // never 0: a masked score, -inf, stays what it is
+    factor = big < __builtin_inff() ? fmaxf(scale_log2 * pow2i(e - 22), 0x1p-126f) : __builtin_nanf("");
     digits[0] = cut_query(w, up);
     digits[1] = cut_query(w + 8, up);
+}
+
+// Sixteen bytes of a record: one address for the wave, one offset a lane.
+__device__ __forceinline__ v4i load16(const uint8_t* rec, uint32_t offset, int constant)
+{
+    return *reinterpret_cast<const v4i*>(rec + (size_t)offset + constant);
 }
 
 __device__ __forceinline__ void wave_lds_order()
@@ -170,11 +181,12 @@ __device__ __forceinline__ int row_length(const kv8_attn_args& a, int row, int& 
 }
 
 // What a score's token contributes with: d^K, poisoned where the token's V row is not finite (the rows that see the token become NaN, the others
-// do not), and d^V, 0 there.
-__device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float (&dk)[4], float (&dv)[4])
+// do not), and d^V, 0 there // (scales: the page's K scales, its V scales behind them).
+__device__ __forceinline__ void clean_scales(const uint8_t* scales, int col, float (&dk)[4], float (&dv)[4])
 {
-    const float4 ks = *reinterpret_cast<const float4*>(rec + kRecordKs + 16 * col);
-    const float4 vs = *reinterpret_cast<const float4*>(rec + kRecordVs + 16 * col);
+    const uint32_t at = 16 * col;
+    const float4 ks = *reinterpret_cast<const float4*>(scales + (size_t)at);
+    const float4 vs = *reinterpret_cast<const float4*>(scales + (size_t)at + (kRecordVs - kRecordKs));
     const float k[4] = {ks.x, ks.y, ks.z, ks.w}, v[4] = {vs.x, vs.y, vs.z, vs.w};
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -182,11 +194,15 @@ __device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float 
         dv[t] = fabsf(v[t]) < __builtin_inff() ? v[t] : 0.0f;
     }
 }
-
-// A score in units of log2 from its digit sums.
-__device__ __forceinline__ float score_of(int d0, int d1, int d2, float factor, float dk)
+__device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float (&dk)[4], float (&dv)[4])
 {
-    return __builtin_fmaf((float)d0, 65536.0f * factor, (float)(d1 * 256 + d2) * factor) * dk;
+    clean_scales(rec + kRecordKs, col, dk, dv);
+}
+
+// A score from its digit sums; times the row's factor it is in units of log2.
+__device__ __forceinline__ float score_of(int d0, int d1, int d2, float dk)
+{
+    return digits_value(d0, d1, d2) * dk;
 }
 
 // ---------------------------------------------------------------- a chunk by four waves, a page each
@@ -243,6 +259,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
     }
 
     const v4i zero = {0, 0, 0, 0};
+    const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col;
     bool first = true;
     while (todo != 0) {
         const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
@@ -256,7 +273,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
 #pragma unroll
         for (int r = 0; r < NP; ++r) lens[r] = __shfl(mine, PACK ? group : 4 * group + r, kWave);
         const int page = chunk * kChunkPages + wave;
-        const uint8_t* rec = page * kPage < __builtin_amdgcn_readfirstlane(longest) ? kv8_record(a.c, now, page, kvh) : nullptr;
+        const uint8_t* rec = page * kPage < __builtin_amdgcn_readfirstlane(longest) ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
         if (!first) __syncthreads();  // the last slot's sums have been read
         first = false;
 
@@ -272,10 +289,10 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) kc[t][h] = *reinterpret_cast<const v4i*>(rec + (4 * col + t) * kHeadDim + 32 * group + 16 * h);
+                for (int h = 0; h < 2; ++h) kc[t][h] = load16(rec, key_at, t * kHeadDim + 64 * h);
             token_scales(rec, col, dk, dv);
 #pragma unroll
-            for (int n = 0; n < 8; ++n) vc[n] = *reinterpret_cast<const v4i*>(rec + kRecordV + group * (16 * kHeadDim) + (16 * n + col) * 16);
+            for (int n = 0; n < 8; ++n) vc[n] = load16(rec, value_at, 256 * n);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 v4i d[DIGITS];
@@ -288,15 +305,15 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
 #pragma unroll
                 for (int r = 0; r < NP; ++r) {
                     float x;
-                    if constexpr (PACK) x = score_of(d[0][0], d[0][1], d[0][2], factors[0], dk[t]);
-                    else x = score_of(d[0][r], d[1][r], d[2][r], factors[r], dk[t]);
+                    if constexpr (PACK) x = score_of(d[0][0], d[0][1], d[0][2], dk[t]);
+                    else x = score_of(d[0][r], d[1][r], d[2][r], dk[t]);
                     s[t][r] = token < lens[r] ? x : -__builtin_inff();
                 }
             }
         }
 #pragma unroll
         for (int r = 0; r < NP; ++r) {
-            const float m = row_max(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r])));
+            const float m = row_max(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r]))) * factors[r];
             if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
         }
         if constexpr (!PACK) {
@@ -312,7 +329,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
             float e[4], w = 0.0f;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                e[t] = __builtin_amdgcn_exp2f(s[t][r] - safe);
+                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factors[r], -safe));
                 s[t][r] = e[t] * dv[t];
                 w = fmaxf(w, s[t][r]);
             }
@@ -376,7 +393,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
             if (!((members >> p) & 1u)) continue;
             const float lc = row_sum((lsum[0][p][col] + lsum[1][p][col]) + (lsum[2][p][col] + lsum[3][p][col]));
             const float m = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
-            const float down = pow2i(exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))) - 22);
+            const float unit = pow2i(exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))) - 22);
             float o[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -386,20 +403,17 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
                     hi += sums[w][0][p * SUMS + 2 * lane + k];
                     lo += sums[w][1][p * SUMS + 2 * lane + k];
                 }
-                o[k] = __builtin_fmaf((float)hi, 65536.0f, (float)lo) * down;
+                o[k] = __builtin_fmaf((float)hi, 65536.0f, (float)lo);
             }
             const size_t head = (size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G;
             if (__builtin_amdgcn_readlane(len, p) <= kChunk) {  // the row's only chunk
                 float fm = -__builtin_inff(), l = 0.0f, fa, fb;
-                fold_step(fm, l, m, lc, fa, fb);
+                fold_step(fm, l, m, lc, unit, fa, fb);
                 reinterpret_cast<uint32_t*>(a.out + head * kHeadDim)[lane] =
                     pack_bf16x2(attn_quotient(fold_value(0.0f, o[0], fa, fb), l), attn_quotient(fold_value(0.0f, o[1], fa, fb), l));
             } else {
                 const size_t at = head * a.chunks + chunk;
-                if (lane == 0) {
-                    a.part_m[at] = m;
-                    a.part_l[at] = lc;
-                }
+                if (lane == 0) a.part[at] = make_float4(m, lc, unit, 0.0f);
                 reinterpret_cast<float2*>(a.part_o + at * kHeadDim)[lane] = make_float2(o[0], o[1]);
             }
         }
@@ -416,44 +430,132 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
     const int len = row_length(a, (int)(at / a.Hq), slot);
     if (len <= kChunk) return;
     const int chunks = (len + kChunk - 1) / kChunk;
-    const float* pm = a.part_m + at * a.chunks;
-    const float* pl = a.part_l + at * a.chunks;
+    const float4* ps = a.part + at * a.chunks;
     const float* po = a.part_o + at * a.chunks * kHeadDim + threadIdx.x;
     float m = -__builtin_inff(), l = 0.0f, o = 0.0f;
     for (int c0 = 0; c0 < chunks; c0 += AHEAD) {
-        float x[AHEAD], xm[AHEAD], xl[AHEAD];
+        float x[AHEAD];
+        float4 xs[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int c = min(c0 + k, chunks - 1);
-            xm[k] = pm[c];
-            xl[k] = pl[c];
+            xs[k] = ps[c];
             x[k] = po[(size_t)c * kHeadDim];
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {  // past the last chunk: one without tokens, which changes nothing
             const bool there = c0 + k < chunks;
             float fa, fb;
-            fold_step(m, l, there ? xm[k] : -__builtin_inff(), there ? xl[k] : 0.0f, fa, fb);
+            fold_step(m, l, there ? xs[k].x : -__builtin_inff(), there ? xs[k].y : 0.0f, xs[k].z, fa, fb);
             o = fold_value(o, there ? x[k] : 0.0f, fa, fb);
         }
     }
     a.out[at * kHeadDim + threadIdx.x] = f32_to_bf16_rne(attn_quotient(o, l));
 }
 
-// ---------------------------------------------------------------- many rows: a wave walks the chunks of its tile
+// ---------------------------------------------------------------- a chunk by one wave: what both walks share
 
-// One wave: a tile of up to sixteen (row, head) pairs that read one KV head goes through all their chunks, the running softmax in registers: nothing
-// is stored between, and a tile's rows (of one prompt, mostly) share every read.  Rows that name different slots are walked one slot after the
-// other.  Four neighbouring tiles to a workgroup, so that they find one another's pages in the cache of their compute unit; the last rows, which
-// have most to read, begin.  Grid (KV heads, tiles / 4).
-constexpr int kWalkStride = kChunk + 16;  // bytes of a pair's digits of a chunk
-__global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a, int tiles)
+// One digit of four neighbouring tokens' weights to a word: the weights as integers of 22 bits.
+__device__ __forceinline__ void cut_weights(const float (&w)[4][4], int r, float up, uint32_t (&b)[3])
 {
-    __shared__ __attribute__((aligned(16))) uint8_t digits_of[4][3 * kPairs * kWalkStride];
+    uint32_t y[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(w[t][r], up, 8421504.0f));  // 2^23 + 0x8080
+    gather_bytes(y, b[2], b[1], b[0]);
+    b[1] ^= 0x80808080u;
+    b[2] ^= 0x80808080u;
+}
+
+// Scores to weights e d^V, in place, and what the fold needs of the chunk.  scales(p, dk, dv): those of this lane's tokens of page p.
+template <class Scales>
+__device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], const float (&factors)[4], Scales scales, float (&mc)[4],
+                                                float (&lc)[4], float (&up)[4], float (&unit)[4])
+{
+    float safe[4], sum[kChunkPages][4], top[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float x = -__builtin_inff();
+#pragma unroll
+        for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x = fmaxf(x, s[p][t][r]);
+        mc[r] = __builtin_ceilf(row_max(x) * factors[r]);
+        safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+        top[r] = 0.0f;
+    }
+#pragma unroll
+    for (int p = 0; p < kChunkPages; ++p) {
+        float dk[4], dv[4];
+        scales(p, dk, dv);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float e[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][t][r], factors[r], -safe[r]));
+                s[p][t][r] = e[t] * dv[t];
+                top[r] = fmaxf(top[r], s[p][t][r]);
+            }
+            sum[p][r] = (e[0] + e[1]) + (e[2] + e[3]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        lc[r] = row_sum((sum[0][r] + sum[1][r]) + (sum[2][r] + sum[3][r]));
+        const int e = exponent_above(row_max(top[r]));
+        up[r] = pow2i(22 - e);
+        unit[r] = pow2i(e - 22);
+    }
+}
+
+// The digits of a chunk's weights into a wave's LDS, as the second product takes them: of each digit sixteen rows (pairs) of 256 bytes (tokens), the
+// sixteen-byte pieces of a row swizzled by the pair.  here: the lane, hidden from the compiler, so that it keeps no addresses over a loop.
+constexpr int kChunkDigits = 3 * kPairs * kChunk;
+__device__ __forceinline__ void store_digits(const float (&w)[kChunkPages][4][4], const float (&up)[4], uint8_t* digits, int here)
+{
+    const int g4 = here >> 4, c = here & 15;
+    wave_lds_order();
+#pragma unroll
+    for (int p = 0; p < kChunkPages; ++p) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            uint32_t b[3];
+            cut_weights(w[p], r, up[r], b);
+            // piece (4 p + c / 4) ^ (4 g4 + r) of row 4 g4 + r
+            uint8_t* at = digits + kChunk * (4 * g4 + r) + 64 * (p ^ g4) + 16 * ((c >> 2) ^ r) + 4 * (c & 3);
+#pragma unroll
+            for (int g = 0; g < 3; ++g) *reinterpret_cast<uint32_t*>(at + g * kPairs * kChunk) = b[g];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    wave_lds_order();
+}
+// This lane's operand of digit g, tokens of page p.
+__device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, int here)
+{
+    return *reinterpret_cast<const v4i*>(digits + g * kPairs * kChunk + ((272 * (here & 15)) ^ (16 * (here >> 4) + 64 * p)));
+}
+
+__device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int kvh, unsigned members, const float (&l)[4], const float (&o)[8][4])
+{
+    const int lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int p = 4 * group + r;
+        if (!((members >> p) & 1u)) continue;
+        uint16_t* out = a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) out[16 * n + col] = f32_to_bf16_rne(attn_quotient(o[n][r], l[r]));
+    }
+}
+
+// One wave walks its tile for itself, its pages straight from memory, one slot after the other: for tiles whose neighbours' rows name other slots.
+// digits_of: the workgroup's digits.
+__device__ __forceinline__ void walk_alone(const kv8_attn_args& a, int kvh, int tile, uint8_t* digits_of)
+{
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
-    uint8_t* digits = digits_of[wave];
-    const int kvh = blockIdx.x, tile = 4 * (gridDim.y - 1 - blockIdx.y) + wave;
-    if (tile >= tiles) return;
+    uint8_t* digits = digits_of + wave * kChunkDigits;
     const int row0 = tile * a.rows_per_tile;
     const bool live = col < a.rows_per_tile * a.G && row0 + col / a.G < a.R;
     int slot = -1, len = 0;
@@ -464,179 +566,340 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a, 
 #pragma unroll
     for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
     const v4i zero = {0, 0, 0, 0};
+    const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col;
 
     unsigned todo = (unsigned)(__ballot(live) & 0xFFFFull);
     while (todo != 0) {
-        const int lead = __builtin_ctz(todo);
-        const int now = __builtin_amdgcn_readlane(slot, lead);
+        const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
         const unsigned members = (unsigned)(__ballot(live && slot == now) & 0xFFFFull);
         todo &= ~members;
-        const bool mine = (members >> col) & 1u;
-        int longest = mine ? len : 0, shortest = mine ? len : 0x7FFFFFFF;
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) {
-            longest = max(longest, __shfl_xor(longest, off, kWave));
-            shortest = min(shortest, __shfl_xor(shortest, off, kWave));
-        }
-        longest = __builtin_amdgcn_readfirstlane(longest);
-        shortest = __builtin_amdgcn_readfirstlane(shortest);
+        int longest = (members >> col) & 1u ? len : 0;
         float m[4], l[4], o[8][4];
         int lens[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            lens[r] = __shfl(mine ? len : 0, 4 * group + r, kWave);
+            lens[r] = __shfl(longest, 4 * group + r, kWave);
             m[r] = -__builtin_inff();
             l[r] = 0.0f;
 #pragma unroll
             for (int n = 0; n < 8; ++n) o[n][r] = 0.0f;
         }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+        longest = __builtin_amdgcn_readfirstlane(longest);
         for (int chunk = 0; chunk * kChunk < longest; ++chunk) {
+            const int pages = min(kChunkPages, (longest - chunk * kChunk + kPage - 1) / kPage);
             const uint8_t* rec[kChunkPages];
+            unsigned gone = 0;
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                const uint8_t* at = p < pages ? kv8_record_uniform(a.c, now, chunk * kChunkPages + p, kvh) : nullptr;
+                gone |= at ? 0u : 1u << p;
+                rec[p] = at ? at : a.c.pool;
+            }
+            float s[kChunkPages][4][4];
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                float dk[4], dv[4];
+                token_scales(rec[p], col, dk, dv);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const v4i k0 = load16(rec[p], key_at, t * kHeadDim), k1 = load16(rec[p], key_at, t * kHeadDim + 64);
+                    v4i d[3];
+#pragma unroll
+                    for (int g = 0; g < 3; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], k0, zero, 0, 0, 0);
+#pragma unroll
+                    for (int g = 0; g < 3; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], k1, d[g], 0, 0, 0);
+                    const int token = (gone >> p) & 1u ? 0x7FFFFFFF : chunk * kChunk + p * kPage + 4 * col + t;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? score_of(d[0][r], d[1][r], d[2][r], dk[t]) : -__builtin_inff();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float mc[4], lc[4], up[4], unit[4];
+            softmax_weights(s, factors, [&](int p, float (&dk)[4], float (&dv)[4]) { token_scales(rec[p], col, dk, dv); }, mc, lc, up, unit);
+            int here = lane;
+            asm volatile("" : "+v"(here));
+            float fa[4], fb[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) fold_step(m[r], l[r], mc[r], lc[r], unit[r], fa[r], fb[r]);
+            store_digits(s, up, digits, here);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                v4i acc[3];
+#pragma unroll
+                for (int p = 0; p < kChunkPages; ++p) {
+                    const v4i v = load16(rec[p], value_at, 256 * n);
+#pragma unroll
+                    for (int g = 0; g < 3; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_digits(digits, g, p, here), v, p == 0 ? zero : acc[g], 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[n][r] = fold_value(o[n][r], digits_value(acc[0][r], acc[1][r], acc[2][r]), fa[r], fb[r]);
+                if (n % 2) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        store_rows(a, row0, kvh, members, l, o);
+    }
+}
+
+// ---------------------------------------------------------------- many rows: the chunks of a tile, one after the other
+
+// A workgroup takes four neighbouring tiles of sixteen (row, head) pairs of one KV head, a tile a wave, through all chunks of the slot they name, the
+// running softmax in registers: nothing is stored between.  A chunk comes in eight steps of 8 KB through a ring of three LDS slots, two in flight, one
+// barrier a step: the K codes of its four pages, then four times 32 columns of all its V codes, so that a step's digit sums are finished when it
+// ends and few are held.  The scales come beside the K codes.  Tiles whose rows name several slots go through them one after the other.
+//
+// K rows lie in LDS as the products take them: row 16 t + c holds token 4 c + t (so that a lane's scores are of four neighbouring tokens, and four
+// digits make a word), its sixteen-byte pieces swizzled by c / 2: a read of sixteen bytes a lane is served in quarters of lanes 0-3, 12-15 and, of the
+// next sixteen, 4-11, and those then lie in different banks.  The digits' rows of 256 tokens are swizzled by the pair.
+constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = kRecordV;  // slots, steps in flight, bytes of a slot
+constexpr int kSteps = 2 * kChunkPages;                             // of a chunk: its pages' K codes, then quarters of its V codes
+constexpr int kWalkSlots = 4;                                       // slots that a workgroup's rows may name to be walked together
+
+// DMA instructions of a wave that may stay in flight when step j's data is needed: those of the steps behind it (3 for K codes, 2 for V codes).
+constexpr int walk_wait(int j)
+{
+    int n = 0;
+    for (int k = 1; k < kRingAhead; ++k) n += (j + k) % kSteps < kChunkPages ? 3 : 2;
+    return n;
+}
+template <int N>
+__device__ __forceinline__ void wait_loads_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+__global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[kRing * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t scales[2 * kChunkPages * 512 + 512];  // two chunks' (K, V of each page); what no one reads
+    __shared__ __attribute__((aligned(1024))) uint8_t digits_of[4 * kChunkDigits];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, group = lane >> 4, col = lane & 15;
+    uint8_t* digits = digits_of + wave * kChunkDigits;
+    const int kvh = blockIdx.x, tile0 = 4 * (gridDim.y - 1 - blockIdx.y);  // the last rows, which have most to read, begin
+    // lane: pair `col` of tile `group`; every wave knows all four tiles
+    const int pair_row = (tile0 + group) * a.rows_per_tile + col / a.G;
+    const bool live = col < a.rows_per_tile * a.G && pair_row < a.R;
+    int slot = -1, len = 0;
+    if (live) len = row_length(a, pair_row, slot);
+
+    int kinds = 0;
+    for (unsigned long long left = __ballot(live); left != 0 && kinds <= kWalkSlots; ++kinds) {
+        const int now = __builtin_amdgcn_readlane(slot, __builtin_ctzll(left));
+        left &= ~__ballot(live && slot == now);
+    }
+    if (kinds > kWalkSlots) {
+        walk_alone(a, kvh, tile0 + wave, digits_of);
+        return;
+    }
+
+    const int my_row0 = (tile0 + wave) * a.rows_per_tile;
+    q_digits qd[2];
+    float factor, factors[4];
+    load_query(col < a.rows_per_tile * a.G && my_row0 + col / a.G < a.R
+                   ? a.q + ((size_t)(my_row0 + col / a.G) * a.Hq + kvh * a.G + col % a.G) * kHeadDim : nullptr,
+               a.scale_log2, qd, factor);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
+    const v4i zero = {0, 0, 0, 0};
+
+    // what this wave brings of a step: two blocks of 1 KB, of V codes those of one page; and with K codes one of the page's rows of scales
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_char_t*)ring, scales_at = (uint32_t)(uintptr_t)(lds_char_t*)scales;
+    uint32_t key_from[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int c = 8 * b + (lane >> 3);  // LDS row 16 wave + c: token 4 c + wave
+        key_from[b] = 512 * c + 128 * wave + 16 * ((lane & 7) ^ (c >> 1));
+    }
+    const uint32_t value_from = kRecordV + 2048 * (lane >> 5) + 16 * (lane & 31);  // of sixteen tokens 32 columns, of the next sixteen too
+    const uint32_t scale_from = kRecordKs + 256 * (wave & 1) + 4 * lane;
+    // where it reads: a K row's piece, a V operand, a pair's digits
+    const uint32_t key_at = 128 * col + 16 * (group ^ (col >> 1)), value_at = 512 * group + 16 * col;
+
+    unsigned long long todo = __ballot(live);
+    while (todo != 0) {
+        const int now = __builtin_amdgcn_readlane(slot, __builtin_ctzll(todo));
+        const unsigned long long all = __ballot(live && slot == now);
+        todo &= ~all;
+        // of the workgroup, and of this wave's tile
+        int longest = (all >> lane) & 1ull ? len : 0;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        const unsigned members = (unsigned)(all >> (16 * wave)) & 0xFFFFu;
+        const int pair_len = __shfl(len, 16 * wave + col, kWave);
+        int mine = (members >> col) & 1u ? pair_len : 0, least = (members >> col) & 1u ? pair_len : 0x7FFFFFFF;
+        int lens[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lens[r] = __shfl(mine, 4 * group + r, kWave);
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) {
+            mine = max(mine, __shfl_xor(mine, off, kWave));
+            least = min(least, __shfl_xor(least, off, kWave));
+        }
+        const int my_longest = __builtin_amdgcn_readfirstlane(mine), my_shortest = __builtin_amdgcn_readfirstlane(least);
+
+        float m[4], l[4], o[8][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            m[r] = -__builtin_inff();
+            l[r] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) o[n][r] = 0.0f;
+        }
+        // records of a chunk; where a page is missing, any (its tokens are masked)
+        auto look_up = [&](int chunk, const uint8_t* (&rec)[kChunkPages + 1]) {
+            unsigned gone = 0;
+            rec[kChunkPages] = a.c.pool;
 #pragma unroll
             for (int p = 0; p < kChunkPages; ++p) {
                 const int page = chunk * kChunkPages + p;
-                rec[p] = page * kPage < longest ? kv8_record(a.c, now, page, kvh) : nullptr;
+                const uint8_t* at = page * kPage < longest ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
+                gone |= at ? 0u : 1u << p;
+                rec[p] = at ? at : a.c.pool;
+                rec[kChunkPages] = p == wave ? rec[p] : rec[kChunkPages];  // the page whose V codes this wave brings
             }
-            float s[kChunkPages][4][4];  // page, token 4 col + t, pair
+            return gone;
+        };
+        // step j of a chunk with the records rec, into ring slot `to`
+        auto bring = [&](int j, const uint8_t* const (&rec)[kChunkPages + 1], int chunk, int to) {
+            const uint8_t* from = rec[j < kChunkPages ? j : kChunkPages];
+            const uint32_t at = ring_at + to * kStepBytes + 2048 * wave;
+            if (j < kChunkPages) {
+                dma_block(from, key_from[0], at);
+                dma_block(from, key_from[1], at + 1024);
+                dma_words(from, scale_from, wave < 2 ? scales_at + ((chunk & 1) * kChunkPages + j) * 512 + 256 * wave
+                                                     : scales_at + 2 * kChunkPages * 512 + 256 * (wave - 2));
+            } else {
+                dma_block(from + 512 * (j - kChunkPages), value_from, at);
+                dma_block(from + 512 * (j - kChunkPages) + 4096, value_from, at + 1024);
+            }
+        };
+        const uint8_t *rec[kChunkPages + 1], *next[kChunkPages + 1];
+        unsigned gone = look_up(0, rec);
+        int place = 0;  // ring slot of the step at hand
 #pragma unroll
-            for (int p = 0; p < kChunkPages; ++p) {
-                if (rec[p]) {
-                    v4i kc[4][2];
-                    float dk[4], dv[4];
+        for (int j = 0; j < kRingAhead; ++j) bring(j, rec, 0, j);
+        for (int chunk = 0; chunk * kChunk < longest; ++chunk) {
+            const unsigned next_gone = look_up(chunk + 1, next);
+            int here = lane;  // unknown to the compiler: what follows from it is not kept in registers over the loop
+            asm volatile("" : "+v"(here));
+            const bool busy = chunk * kChunk < my_longest;
+            const int pages = min(kChunkPages, (my_longest - chunk * kChunk + kPage - 1) / kPage);  // of this wave's rows
+            auto arrive = [&](auto step) {
+                constexpr int j = decltype(step)::value;
+                wait_loads_barrier<walk_wait(j)>();
+                const int to = place == 0 ? kRing - 1 : place - 1;
+                if (j + kRingAhead < kSteps) bring((j + kRingAhead) % kSteps, rec, chunk, to);
+                else bring((j + kRingAhead) % kSteps, next, chunk + 1, to);
+                const uint8_t* codes = ring + place * kStepBytes;
+                place = place + 1 == kRing ? 0 : place + 1;
+                return codes;
+            };
+            const uint8_t* chunk_scales = scales + (chunk & 1) * kChunkPages * 512;
+            float s[kChunkPages][4][4];  // page, token 4 col + t, pair
+            auto keys = [&](auto step) {
+                constexpr int p = decltype(step)::value;
+                const uint8_t* codes = arrive(step);
+                if (!busy || p >= pages) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) kc[t][h] = *reinterpret_cast<const v4i*>(rec[p] + (4 * col + t) * kHeadDim + 32 * group + 16 * h);
-                    token_scales(rec[p], col, dk, dv);
+                        for (int r = 0; r < 4; ++r) s[p][t][r] = 0.0f;
+                    return;
+                }
+                float dk[4], dv[4];
+                clean_scales(chunk_scales + 512 * p, col, dk, dv);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        v4i d[3];
+                for (int two = 0; two < 2; ++two) {
+                    v4i d[2][3];
 #pragma unroll
-                        for (int g = 0; g < 3; ++g) {
-                            d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
-                            d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const v4i k = *reinterpret_cast<const v4i*>(codes + (h ? key_at ^ 64u : key_at) + 2048 * (2 * two + t));
+#pragma unroll
+                            for (int g = 0; g < 3; ++g) d[t][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[h].d[g], k, h ? d[t][g] : zero, 0, 0, 0);
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[p][t][r] = score_of(d[0][r], d[1][r], d[2][r], factors[r], dk[t]);
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[p][2 * two + t][r] = score_of(d[t][0][r], d[t][1][r], d[t][2][r], dk[2 * two + t]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            keys(std::integral_constant<int, 0>{});
+            keys(std::integral_constant<int, 1>{});
+            keys(std::integral_constant<int, 2>{});
+            keys(std::integral_constant<int, 3>{});
+            float fa[4], fb[4];
+            if (busy) {
+                float mc[4], up[4], unit[4], lc[4];
+                if ((chunk + 1) * kChunk > my_shortest || gone != 0) {
+#pragma unroll
+                    for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const int token = (gone >> p) & 1u ? 0x7FFFFFFF : chunk * kChunk + p * kPage + 4 * (here & 15) + t;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? s[p][t][r] : -__builtin_inff();
+                        }
+                }
+                softmax_weights(s, factors, [&](int p, float (&dk)[4], float (&dv)[4]) { clean_scales(chunk_scales + 512 * p, col, dk, dv); }, mc, lc, up, unit);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) fold_step(m[r], l[r], mc[r], lc[r], unit[r], fa[r], fb[r]);
+                store_digits(s, up, digits, here);
+            }
+            auto values = [&](auto step) {
+                constexpr int j = decltype(step)::value - kChunkPages;
+                const uint8_t* codes = arrive(step);
+                if (!busy) return;
+                v4i acc[3][2];
+#pragma unroll
+                for (int p = 0; p < kChunkPages; ++p) {
+                    if (p < pages) {
+                        v4i w[3];
+#pragma unroll
+                        for (int g = 0; g < 3; ++g) w[g] = load_digits(digits, g, p, here);
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const v4i v = *reinterpret_cast<const v4i*>(codes + value_at + 2048 * p + 256 * n);
+#pragma unroll
+                            for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, p == 0 ? zero : acc[g][n], 0, 0, 0);
+                        }
                     }
-                } else {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[p][t][r] = -__builtin_inff();
                 }
-            }
-            if ((chunk + 1) * kChunk > shortest) {
 #pragma unroll
-                for (int p = 0; p < kChunkPages; ++p)
+                for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int token = chunk * kChunk + p * kPage + 4 * col + t;
+                    for (int r = 0; r < 4; ++r)
+                        o[2 * j + n][r] = fold_value(o[2 * j + n][r], digits_value(acc[0][n][r], acc[1][n][r], acc[2][n][r]), fa[r], fb[r]);
+            };
+            values(std::integral_constant<int, 4>{});
+            values(std::integral_constant<int, 5>{});
+            values(std::integral_constant<int, 6>{});
+            values(std::integral_constant<int, 7>{});
+            gone = next_gone;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? s[p][t][r] : -__builtin_inff();
-                    }
-            }
-            float mc[4], safe[4], sum[4], top[4], lc[4], down[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x = -__builtin_inff();
-#pragma unroll
-                for (int p = 0; p < kChunkPages; ++p)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) x = fmaxf(x, s[p][t][r]);
-                mc[r] = __builtin_ceilf(row_max(x));
-                safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
-                top[r] = 0.0f;
-            }
-            float sums[kChunkPages][4];
-#pragma unroll
-            for (int p = 0; p < kChunkPages; ++p) {
-                float dk[4], dv[4] = {};
-                if (rec[p]) token_scales(rec[p], col, dk, dv);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float e[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        e[t] = __builtin_amdgcn_exp2f(s[p][t][r] - safe[r]);
-                        s[p][t][r] = e[t] * dv[t];
-                        top[r] = fmaxf(top[r], s[p][t][r]);
-                    }
-                    sums[p][r] = (e[0] + e[1]) + (e[2] + e[3]);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                lc[r] = row_sum((sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]));
-                const int e = exponent_above(row_max(top[r]));
-                sum[r] = pow2i(22 - e);
-                down[r] = pow2i(e - 22);
-            }
-            wave_lds_order();
-#pragma unroll
-            for (int p = 0; p < kChunkPages; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    uint32_t y[4], b0, b1, b2;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(s[p][t][r], sum[r], 8421504.0f));  // 2^23 + 0x8080
-                    gather_bytes(y, b0, b1, b2);
-                    uint8_t* at = digits + (4 * group + r) * kWalkStride + p * kPage + 4 * col;
-                    *reinterpret_cast<uint32_t*>(at) = b2;
-                    *reinterpret_cast<uint32_t*>(at + kPairs * kWalkStride) = b1 ^ 0x80808080u;
-                    *reinterpret_cast<uint32_t*>(at + 2 * kPairs * kWalkStride) = b0 ^ 0x80808080u;
-                }
-            wave_lds_order();
-            v4i acc[3][8];
-#pragma unroll
-            for (int g = 0; g < 3; ++g)
-#pragma unroll
-                for (int n = 0; n < 8; ++n) acc[g][n] = zero;
-#pragma unroll
-            for (int p = 0; p < kChunkPages; ++p) {
-                if (!rec[p]) continue;
-                v4i w[3];
-#pragma unroll
-                for (int g = 0; g < 3; ++g) w[g] = *reinterpret_cast<const v4i*>(digits + (g * kPairs + col) * kWalkStride + p * kPage + 16 * group);
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    const v4i v = *reinterpret_cast<const v4i*>(rec[p] + kRecordV + group * (16 * kHeadDim) + (16 * n + col) * 16);
-#pragma unroll
-                    for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, acc[g][n], 0, 0, 0);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float fa, fb;
-                fold_step(m[r], l[r], mc[r], lc[r], fa, fb);
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    const float oc = __builtin_fmaf((float)acc[0][n][r], 65536.0f, (float)(acc[1][n][r] * 256 + acc[2][n][r])) * down[r];
-                    o[n][r] = fold_value(o[n][r], oc, fa, fb);
-                }
-            }
+            for (int p = 0; p <= kChunkPages; ++p) rec[p] = next[p];
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int p = 4 * group + r;
-            if (!((members >> p) & 1u)) continue;
-            uint16_t* out = a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim;
-#pragma unroll
-            for (int n = 0; n < 8; ++n) out[16 * n + col] = f32_to_bf16_rne(attn_quotient(o[n][r], l[r]));
-        }
+        // the steps asked for past the last chunk have to land before the ring begins anew
+        wait_loads_barrier<0>();
+        store_rows(a, my_row0, kvh, members, l, o);
     }
 }
 
 static size_t workspace_bytes(int R, int Hq, int max_pages)
 {
     const size_t chunks = ((size_t)max_pages + kChunkPages - 1) / kChunkPages;
-    return (size_t)R * Hq * chunks * (kHeadDim + 2) * sizeof(float);
+    return (size_t)R * Hq * chunks * (kHeadDim + 4) * sizeof(float);
 }
 
 int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset, void* out,
                          void* ws, size_t ws_bytes, int R, int Hq, int D, float scale, hipStream_t s)
 {
-    if (!q || !seqlens || !out || !ws || R < 1 || Hq < 1) return DET_EINVAL;
+    if (!q || !seqlens || !out || !ws || R < 1 || Hq < 1 || !(scale > 0.0f) || !(scale < __builtin_inff()))
+        return DET_EINVAL;
     const int rc = kv8_check(cache.pool, cache.table, cache.n_pages, cache.n_slots, cache.max_pages, cache.Hkv, D);
     if (rc != DET_OK) return rc;
     if (Hq % cache.Hkv != 0 || Hq / cache.Hkv > kPairs || cache.Hkv > 65535) return DET_ESHAPE;
@@ -659,11 +922,10 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.scale_log2 = scale * 1.44269504f;
     const size_t pairs = (size_t)R * Hq * a.chunks;
     a.part_o = static_cast<float*>(ws);
-    a.part_m = a.part_o + pairs * kHeadDim;
-    a.part_l = a.part_m + pairs;
+    a.part = reinterpret_cast<float4*>(a.part_o + pairs * kHeadDim);
     const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
     if (slots && tiles * cache.Hkv >= 2048) {
-        hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3(cache.Hkv, (unsigned)((tiles + 3) / 4)), dim3(256), 0, s, a, (int)tiles);
+        hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3(cache.Hkv, (unsigned)((tiles + 3) / 4)), dim3(256), 0, s, a);
         return check_launch();
     }
     if (tiles > 65535 || a.chunks > 65535 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;

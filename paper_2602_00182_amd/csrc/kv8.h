@@ -33,6 +33,19 @@ __device__ __forceinline__ uint8_t* kv8_record(const kv8_cache& c, int slot, int
     return c.pool + ((size_t)page * c.Hkv + kvh) * kRecord;
 }
 
+// The same for a slot and page that the whole wave asks for: the table's entry comes by the scalar path, the record's address stays in scalar
+// registers.
+__device__ __forceinline__ const uint8_t* kv8_record_uniform(const kv8_cache& c, int slot, int page_of_slot, int kvh)
+{
+    typedef const __attribute__((address_space(4))) int32_t* constant_ints;
+    slot = __builtin_amdgcn_readfirstlane(slot);
+    page_of_slot = __builtin_amdgcn_readfirstlane(page_of_slot);
+    if ((unsigned)slot >= (unsigned)c.n_slots || (unsigned)page_of_slot >= (unsigned)c.max_pages) return nullptr;
+    const int page = ((constant_ints)(uintptr_t)c.table)[(size_t)slot * c.max_pages + page_of_slot];
+    if ((unsigned)page >= (unsigned)c.n_pages) return nullptr;
+    return c.pool + ((size_t)page * c.Hkv + kvh) * kRecord;
+}
+
 // det_attn_decode_kv8 with the length taken as seqlens[r] + len_offset (a layer passes its positions and 1).
 int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset, void* out,
                          void* ws, size_t ws_bytes, int R, int Hq, int D, float scale, hipStream_t s);

@@ -28,7 +28,22 @@ __device__ __forceinline__ void dma_block(const void* base, uint32_t lane_off, u
         : "memory");
 }
 
-// The same from an address of each lane's own.
+// Four bytes a lane: lane l lands at lds_addr + 4 l.
+__device__ __forceinline__ void dma_words(const void* base, uint32_t lane_off, uint32_t lds_addr)
+{
+    uint32_t saved_m0;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dword %2, %3\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved_m0)
+        : "s"(lds_addr), "v"(lane_off), "s"(base)
+        : "memory");
+}
+
+// Sixteen bytes from an address of each lane's own.
 __device__ __forceinline__ void dma_lane(const void* src, uint32_t lds_addr)
 {
     uint32_t saved_m0;

@@ -232,6 +232,27 @@ def test_prompt_rows_are_the_tokens_decoded_one_by_one(d, Hq, Hkv):
         assert np.array_equal(down_bf16(some), got[a:b])
 
 
+def test_many_rows_of_many_slots_in_no_order(d):
+    """As many rows as a prompt has, but every one of some forty sequences, interleaved; a stretch of one slot and of two among them."""
+    rng = np.random.default_rng(7345)
+    lengths = [int(n) for n in rng.integers(1, 700, 40)]
+    Hq, Hkv = 32, 8
+    cache = Cache(7345, lengths, Hkv)
+    slots = rng.integers(0, 40, 1400).astype(np.int32)
+    slots[200:300], slots[600:700] = 7, rng.choice([3, 5], 100)
+    lens = np.array([rng.integers(0, lengths[s] + 1) for s in slots], dtype=np.int32)
+    q = ds.normal_bf16(7346, (1400, Hq, D), 1.5)
+    step("1400 rows of 40 slots")
+    pool, table, qd = up(cache.pool), up(cache.table), up_bf16(q)
+    got = down_bf16(attn(d, qd, pool, table, up(lens), up(slots)))
+    pick = list(range(0, 1400, 97)) + [200, 260, 640, 1399]
+    ref, tol = attend(cache, q[pick], lens[pick], slots[pick])
+    assert (np.abs(bits_to_f64(got[pick]) - ref) <= tol).all()
+    for r in pick:
+        one = attn(d, qd[r:r + 1], pool, table, up(lens[r:r + 1]), up(slots[r:r + 1]))
+        assert np.array_equal(down_bf16(one)[0], got[r]), r
+
+
 def test_extreme_scores_and_values(d):
     """One weight that is all (scores in the hundreds), equal scores, values of very different sizes, zero queries and zero keys."""
     def edit(k, v):

@@ -33,7 +33,8 @@ CASES += [("det_kv8_copy_pages", COPY, change, code) for change, code in [
     (dict(Hkv=0), EINVAL), (dict(D=64), ESHAPE), (dict(n_layers=65536), ESHAPE), (dict(pool=P + 8), EALIGN)]]
 CASES += [("det_attn_decode_kv8", ATTN, change, code) for change, code in [
     (dict(q=0), EINVAL), (dict(pool=0), EINVAL), (dict(table=0), EINVAL), (dict(seqlens=0), EINVAL), (dict(out=0), EINVAL), (dict(ws=0), EINVAL),
-    (dict(R=0), EINVAL), (dict(Hq=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(max_pages=-1), EINVAL), (dict(D=64), ESHAPE), (dict(Hq=5), ESHAPE),
+    (dict(R=0), EINVAL), (dict(Hq=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(max_pages=-1), EINVAL), (dict(scale=0.0), EINVAL),
+    (dict(scale=-0.1), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(D=64), ESHAPE), (dict(Hq=5), ESHAPE),
     (dict(Hq=34), ESHAPE), (dict(R=3), ESHAPE), (dict(max_pages=131073), ESHAPE), (dict(q=P + 2), EALIGN), (dict(out=P + 4), EALIGN),
     (dict(ws=P + 8), EALIGN), (dict(ws_bytes=0), EWORKSPACE)]]
 CASES += [("det_verify_drafts", VERIFY, change, code) for change, code in [
