@@ -61,6 +61,20 @@ __device__ __forceinline__ void gather_bytes(const uint32_t (&y)[4], uint32_t& b
     b2 = __builtin_amdgcn_perm(h2, l2, 0x05040100u);
 }
 
+// The larger of two, the largest of three, in one instruction: fmaxf would first have every operand quieted, which nothing here needs.
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float d;
+    asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
 // Maximum and sum over the sixteen lanes of a row of lanes (rotations: every lane has the result; a sum adds the same pairs in each).
 template <int N>
 __device__ __forceinline__ float row_ror(float v)
@@ -69,10 +83,10 @@ __device__ __forceinline__ float row_ror(float v)
 }
 __device__ __forceinline__ float row_max(float v)
 {
-    v = fmaxf(v, row_ror<8>(v));
-    v = fmaxf(v, row_ror<4>(v));
-    v = fmaxf(v, row_ror<2>(v));
-    return fmaxf(v, row_ror<1>(v));
+    v = max2(v, row_ror<8>(v));
+    v = max2(v, row_ror<4>(v));
+    v = max2(v, row_ror<2>(v));
+    return max2(v, row_ror<1>(v));
 }
 __device__ __forceinline__ float row_sum(float v)
 {
@@ -95,8 +109,9 @@ __device__ __forceinline__ void fold_step(float& m, float& l, float mc, float lc
 }
 __device__ __forceinline__ float fold_value(float o, float oc, float a, float b) { return __builtin_fmaf(oc, b, o * a); }
 __device__ __forceinline__ float digits_value(int d0, int d1, int d2) { return __builtin_fmaf((float)d0, 65536.0f, (float)(d1 * 256 + d2)); }
-// A row that no token reaches has l = 0 and gives zeros.
-__device__ __forceinline__ float attn_quotient(float o, float l) { return l == 0.0f ? 0.0f : o / l; }
+// What a row's sums are multiplied with.  A row that no token reaches has l = 0 and gives zeros.
+__device__ __forceinline__ float row_factor(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 // ---------------------------------------------------------------- a tile's query
 
@@ -188,6 +203,14 @@ __device__ __forceinline__ void clean_scales(const uint8_t* scales, int col, flo
     const float4 ks = *reinterpret_cast<const float4*>(scales + (size_t)at);
     const float4 vs = *reinterpret_cast<const float4*>(scales + (size_t)at + (kRecordVs - kRecordKs));
     const float k[4] = {ks.x, ks.y, ks.z, ks.w}, v[4] = {vs.x, vs.y, vs.z, vs.w};
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        dk[t] = k[t];
+        dv[t] = v[t];
+        bad |= !(fabsf(v[t]) < __builtin_inff());
+    }
+    if (__ballot(bad) == 0) return;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         dk[t] = k[t] + 0.0f * v[t];
@@ -409,8 +432,9 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
             if (__builtin_amdgcn_readlane(len, p) <= kChunk) {  // the row's only chunk
                 float fm = -__builtin_inff(), l = 0.0f, fa, fb;
                 fold_step(fm, l, m, lc, unit, fa, fb);
+                const float by = row_factor(l);
                 reinterpret_cast<uint32_t*>(a.out + head * kHeadDim)[lane] =
-                    pack_bf16x2(attn_quotient(fold_value(0.0f, o[0], fa, fb), l), attn_quotient(fold_value(0.0f, o[1], fa, fb), l));
+                    to_bf16(fold_value(0.0f, o[0], fa, fb) * by) | ((uint32_t)to_bf16(fold_value(0.0f, o[1], fa, fb) * by) << 16);
             } else {
                 const size_t at = head * a.chunks + chunk;
                 if (lane == 0) a.part[at] = make_float4(m, lc, unit, 0.0f);
@@ -450,7 +474,7 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
             o = fold_value(o, there ? x[k] : 0.0f, fa, fb);
         }
     }
-    a.out[at * kHeadDim + threadIdx.x] = f32_to_bf16_rne(attn_quotient(o, l));
+    a.out[at * kHeadDim + threadIdx.x] = to_bf16(o * row_factor(l));
 }
 
 // ---------------------------------------------------------------- a chunk by one wave: what both walks share
@@ -478,7 +502,7 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
 #pragma unroll
         for (int p = 0; p < kChunkPages; ++p)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) x = fmaxf(x, s[p][t][r]);
+            for (int t = 0; t < 4; t += 2) x = max3(x, s[p][t][r], s[p][t + 1][r]);
         mc[r] = __builtin_ceilf(row_max(x) * factors[r]);
         safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
         top[r] = 0.0f;
@@ -494,8 +518,8 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
             for (int t = 0; t < 4; ++t) {
                 e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][t][r], factors[r], -safe[r]));
                 s[p][t][r] = e[t] * dv[t];
-                top[r] = fmaxf(top[r], s[p][t][r]);
             }
+            top[r] = max3(max3(top[r], s[p][0][r], s[p][1][r]), s[p][2][r], s[p][3][r]);
             sum[p][r] = (e[0] + e[1]) + (e[2] + e[3]);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -545,8 +569,9 @@ __device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int
         const int p = 4 * group + r;
         if (!((members >> p) & 1u)) continue;
         uint16_t* out = a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim;
+        const float by = row_factor(l[r]);
 #pragma unroll
-        for (int n = 0; n < 8; ++n) out[16 * n + col] = f32_to_bf16_rne(attn_quotient(o[n][r], l[r]));
+        for (int n = 0; n < 8; ++n) out[16 * n + col] = to_bf16(o[n][r] * by);
     }
 }
 
