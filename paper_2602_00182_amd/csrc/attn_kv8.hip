@@ -30,7 +30,7 @@ struct kv8_attn_args {
     uint16_t* out;  // [R, Hq, 128]
     float* part_o;  // [R, Hq, chunks, 128]: a chunk's weighted sums, in units of its 2^(E-22)
     float4* part;   // [R, Hq, chunks]: its m, l, 2^(E-22)
-    int R, Hq, G, rows_per_tile, len_offset, chunks;
+    int R, Hq, G, rows_per_tile, len_offset, chunks, inverse_G;
     float scale_log2;  // scale * log2(e)
 };
 
@@ -121,7 +121,7 @@ struct q_digits {
 };
 
 // w: eight words of two bf16 each; up = 2^(22 - E).
-__device__ __forceinline__ q_digits cut_query(const uint32_t* w, float up)
+__device__ __forceinline__ q_digits cut_half(const uint32_t* w, float up)
 {
     q_digits o;
 #pragma unroll
@@ -143,36 +143,33 @@ __device__ __forceinline__ q_digits cut_query(const uint32_t* w, float up)
     return o;
 }
 
-// The query of this lane's operand row: q its 128 values (or null), of which the lane takes columns 64 h + 16 (lane / 16) + 0..15.  factor: what an
-// integer score stands for, in units of log2 (NaN for a query that is not finite).
-__device__ __forceinline__ void load_query(const uint16_t* q, float scale_log2, q_digits (&digits)[2], float& factor)
+// The query of this lane's operand row: q its 128 values (or null), of which the lane takes columns 64 h + 16 (lane / 16) + 0..15.
+__device__ __forceinline__ void ask_query(const uint16_t* q, uint32_t (&w)[16])
 {
     const int group = (threadIdx.x & 63) >> 4;
-    uint32_t w[16] = {};
-    if (q) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint4 x = *reinterpret_cast<const uint4*>(q + 64 * (k >> 1) + 16 * group + 8 * (k & 1));
-            w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
-        }
-    }
-    float big = 0.0f;
-    bool bad = false;
+    for (int k = 0; k < 16; ++k) w[k] = 0u;
+    if (!q) return;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const float a = fabsf(bf16lo_to_f32(w[k])), b = fabsf(bf16hi_to_f32(w[k]));
-        bad |= !(a < __builtin_inff()) | !(b < __builtin_inff());
-        big = fmaxf(big, fmaxf(a, b));
+    for (int k = 0; k < 4; ++k) {
+        const uint4 x = *reinterpret_cast<const uint4*>(q + 64 * (k >> 1) + 16 * group + 8 * (k & 1));
+        w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
     }
-    big = bad ? __builtin_inff() : big;
-    big = fmaxf(big, __shfl_xor(big, 16, kWave));
-    big = fmaxf(big, __shfl_xor(big, 32, kWave));
-    const int e = exponent_above(big);
+}
+// factor: what an integer score stands for, in units of log2 (NaN for a query that is not finite).
+__device__ __forceinline__ void cut_query(const uint32_t (&w)[16], float scale_log2, q_digits (&digits)[2], float& factor)
+{
+    uint32_t big = 0u;  // magnitudes of bf16 order like the integers of their bits; NaN and infinities are the largest
+#pragma unroll
+    for (int k = 0; k < 16; ++k) big = max(big, max(w[k] & 0x7FFF0000u, (w[k] << 16) & 0x7FFF0000u));
+    big = max(big, (uint32_t)__shfl_xor((int)big, 16, kWave));
+    big = max(big, (uint32_t)__shfl_xor((int)big, 32, kWave));
+    const int e = exponent_above(__uint_as_float(big));
     const float up = pow2i(22 - e);
     // never 0: a masked score, -inf, stays what it is
-    factor = big < __builtin_inff() ? fmaxf(scale_log2 * pow2i(e - 22), 0x1p-126f) : __builtin_nanf("");
-    digits[0] = cut_query(w, up);
-    digits[1] = cut_query(w + 8, up);
+    factor = big < 0x7F800000u ? fmaxf(scale_log2 * pow2i(e - 22), 0x1p-126f) : __builtin_nanf("");
+    digits[0] = cut_half(w, up);
+    digits[1] = cut_half(w + 8, up);
 }
 
 // Sixteen bytes of a record: one address for the wave, one offset a lane.
@@ -197,30 +194,38 @@ __device__ __forceinline__ int row_length(const kv8_attn_args& a, int row, int& 
 
 // What a score's token contributes with: d^K, poisoned where the token's V row is not finite (the rows that see the token become NaN, the others
 // do not), and d^V, 0 there // (scales: the page's K scales, its V scales behind them).
-__device__ __forceinline__ void clean_scales(const uint8_t* scales, int col, float (&dk)[4], float (&dv)[4])
+__device__ __forceinline__ void clean_scales(float (&dk)[4], float (&dv)[4])
+{
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bad |= !(fabsf(dv[t]) < __builtin_inff());
+    if (__ballot(bad) == 0) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        dk[t] = dk[t] + 0.0f * dv[t];
+        dv[t] = fabsf(dv[t]) < __builtin_inff() ? dv[t] : 0.0f;
+    }
+}
+__device__ __forceinline__ void ask_scales(const uint8_t* scales, int col, float (&dk)[4], float (&dv)[4])
 {
     const uint32_t at = 16 * col;
     const float4 ks = *reinterpret_cast<const float4*>(scales + (size_t)at);
     const float4 vs = *reinterpret_cast<const float4*>(scales + (size_t)at + (kRecordVs - kRecordKs));
-    const float k[4] = {ks.x, ks.y, ks.z, ks.w}, v[4] = {vs.x, vs.y, vs.z, vs.w};
-    bool bad = false;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        dk[t] = k[t];
-        dv[t] = v[t];
-        bad |= !(fabsf(v[t]) < __builtin_inff());
-    }
-    if (__ballot(bad) == 0) return;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        dk[t] = k[t] + 0.0f * v[t];
-        dv[t] = fabsf(v[t]) < __builtin_inff() ? v[t] : 0.0f;
-    }
+    dk[0] = ks.x, dk[1] = ks.y, dk[2] = ks.z, dk[3] = ks.w;
+    dv[0] = vs.x, dv[1] = vs.y, dv[2] = vs.z, dv[3] = vs.w;
+}
+__device__ __forceinline__ void clean_scales(const uint8_t* scales, int col, float (&dk)[4], float (&dv)[4])
+{
+    ask_scales(scales, col, dk, dv);
+    clean_scales(dk, dv);
 }
 __device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float (&dk)[4], float (&dv)[4])
 {
     clean_scales(rec + kRecordKs, col, dk, dv);
 }
+// Row and head within the KV head of pair p of a tile (p < 16, exact).
+__device__ __forceinline__ int pair_row(const kv8_attn_args& a, int p) { return (p * a.inverse_G) >> 16; }
+
 
 // A score from its digit sums; times the row's factor it is in units of log2.
 __device__ __forceinline__ float score_of(int d0, int d1, int d2, float dk)
@@ -228,61 +233,91 @@ __device__ __forceinline__ float score_of(int d0, int d1, int d2, float dk)
     return digits_value(d0, d1, d2) * dk;
 }
 
-// ---------------------------------------------------------------- a chunk by four waves, a page each
+// ---------------------------------------------------------------- the weights' digits
+
+// One digit of four neighbouring tokens' weights to a word: the weights as integers of 22 bits.
+template <int NP>
+__device__ __forceinline__ void cut_weights(const float (&w)[4][NP], int r, float up, uint32_t (&b)[3])
+{
+    uint32_t y[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(w[t][r], up, 8421504.0f));  // 2^23 + 0x8080
+    gather_bytes(y, b[2], b[1], b[0]);
+    b[1] ^= 0x80808080u;
+    b[2] ^= 0x80808080u;
+}
+
+// The digits of a chunk's weights into a wave's LDS, as the second product takes them: of each digit sixteen rows (pairs) of 256 bytes (tokens), the
+// sixteen-byte pieces of a row swizzled by the pair.  here: the lane, hidden from the compiler, so that it keeps no addresses over a loop.
+constexpr int kChunkDigits = 3 * kPairs * kChunk;
+__device__ __forceinline__ void store_digits(const float (&w)[kChunkPages][4][4], const float (&up)[4], uint8_t* digits, int here)
+{
+    const int g4 = here >> 4, c = here & 15;
+    wave_lds_order();
+#pragma unroll
+    for (int p = 0; p < kChunkPages; ++p) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            uint32_t b[3];
+            cut_weights(w[p], r, up[r], b);
+            // piece (4 p + c / 4) ^ (4 g4 + r) of row 4 g4 + r
+            uint8_t* at = digits + kChunk * (4 * g4 + r) + 64 * (p ^ g4) + 16 * ((c >> 2) ^ r) + 4 * (c & 3);
+#pragma unroll
+            for (int g = 0; g < 3; ++g) *reinterpret_cast<uint32_t*>(at + g * kPairs * kChunk) = b[g];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    wave_lds_order();
+}
+// This lane's operand of digit g, tokens of page p.
+__device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, int here)
+{
+    return *reinterpret_cast<const v4i*>(digits + g * kPairs * kChunk + ((272 * (here & 15)) ^ (16 * (here >> 4) + 64 * p)));
+}
+
+// ---------------------------------------------------------------- a chunk by four waves
 
 // One chunk for a tile of up to sixteen (row, head) pairs that read one KV head.  Rows of a tile may name different slots: those that name the
-// same one go through it together, one slot after the other.  Grid (KV heads, tiles, chunks).
+// same one go through it together, one slot after the other.  Grid (KV heads x tiles, chunks).
+//
+// For the scores a wave takes one of the four pages; the digits of the weights meet in LDS, and for the weighted sums it takes 32 of the 128 columns of
+// all four, so that no sums have to be joined and few are held.  All of a wave's loads (8 KB of K, 8 KB of V) are asked for before the first
+// is used; the workgroups of a compute unit hide one another's way to memory.
 //
 // PACK: up to four pairs (one row of up to four heads a KV head).  Their digits fill the sixteen rows of one operand, row 4 pair + digit, so a
 // product is one instruction instead of three and a lane has all digits of one pair: a quarter of the scores' arithmetic.
-// All of a page's loads are asked for before the first is used; the workgroups of a compute unit hide one another's way to memory.
 template <bool PACK>
 __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
 {
     constexpr int NP = PACK ? 1 : 4;                 // pairs of a lane
     constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
-    constexpr int SUMS = PACK ? 144 : 132;           // words of a pair's sums: lanes of different pairs meet in no bank
-    __shared__ __attribute__((aligned(16))) uint8_t digits[4][DIGITS * kPairs * kDigitStride];
+    __shared__ __attribute__((aligned(1024))) uint8_t digits[DIGITS * kPairs * kChunk];
     __shared__ float top[2][4][PAIRS];               // largest score, largest weight of each wave
     __shared__ float lsum[4][PAIRS][16];
-    __shared__ int sums[PACK ? 4 : 1][2][PAIRS * SUMS];  // digit sums of the values: the high one, the two low ones together
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, group = lane >> 4, col = lane & 15;
-    const int kvh = blockIdx.x, chunk = blockIdx.z;
-    const int row0 = blockIdx.y * a.rows_per_tile;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
+    const int kvh = blockIdx.x % a.c.Hkv, row0 = blockIdx.x / a.c.Hkv * a.rows_per_tile, chunk = blockIdx.y;
     // pair number `col` of the tile
-    const bool live = col < a.rows_per_tile * a.G && row0 + col / a.G < a.R;
+    const bool live = col < a.rows_per_tile * a.G && row0 + pair_row(a, col) < a.R;
     int slot = -1, len = 0;
-    if (live) len = row_length(a, row0 + col / a.G, slot);
+    if (live) len = row_length(a, row0 + pair_row(a, col), slot);
     // chunk 0 also answers for rows that see nothing
     if (chunk == 0) {
         for (int p = wave; p < a.rows_per_tile * a.G; p += 4) {
-            if (row0 + p / a.G < a.R && __builtin_amdgcn_readlane(len, p) == 0)
-                reinterpret_cast<uint32_t*>(a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim)[lane] = 0u;
+            const int r = pair_row(a, p);
+            if (row0 + r < a.R && __builtin_amdgcn_readlane(len, p) == 0)
+                reinterpret_cast<uint32_t*>(a.out + ((size_t)(row0 + r) * a.Hq + kvh * a.G + p - r * a.G) * kHeadDim)[lane] = 0u;
         }
     }
     unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
     if (todo == 0) return;
 
-    const int qp = PACK ? col >> 2 : col;  // the pair of this lane's operand row
+    const int qp = PACK ? col >> 2 : col, qrow = pair_row(a, qp);  // the pair of this lane's operand row
+    uint32_t words[16];
+    ask_query(qp < a.rows_per_tile * a.G && row0 + qrow < a.R ? a.q + ((size_t)(row0 + qrow) * a.Hq + kvh * a.G + qp - qrow * a.G) * kHeadDim : nullptr, words);
     q_digits qd[2];
-    float factor;
-    load_query(qp < a.rows_per_tile * a.G && row0 + qp / a.G < a.R ? a.q + ((size_t)(row0 + qp / a.G) * a.Hq + kvh * a.G + qp % a.G) * kHeadDim : nullptr,
-               a.scale_log2, qd, factor);
     float factors[NP];
-#pragma unroll
-    for (int r = 0; r < NP; ++r) factors[r] = __shfl(factor, PACK ? 4 * group : 4 * group + r, kWave);
-    if constexpr (PACK) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int dg = col & 3;
-                qd[h].d[0][i] = dg == 0 ? qd[h].d[0][i] : dg == 1 ? qd[h].d[1][i] : dg == 2 ? qd[h].d[2][i] : 0;
-            }
-    }
-
     const v4i zero = {0, 0, 0, 0};
-    const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col;
+    const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col + 512 * wave;
     bool first = true;
     while (todo != 0) {
         const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
@@ -292,39 +327,62 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
         int longest = mine;
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+        longest = __builtin_amdgcn_readfirstlane(longest);
         int lens[NP];
 #pragma unroll
         for (int r = 0; r < NP; ++r) lens[r] = __shfl(mine, PACK ? group : 4 * group + r, kWave);
-        const int page = chunk * kChunkPages + wave;
-        const uint8_t* rec = page * kPage < __builtin_amdgcn_readfirstlane(longest) ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
-        if (!first) __syncthreads();  // the last slot's sums have been read
-        first = false;
+        // the chunk's pages; where one is missing, any record (its tokens weigh nothing)
+        const uint8_t *rec[kChunkPages], *keys = nullptr;
+#pragma unroll
+        for (int p = 0; p < kChunkPages; ++p) {
+            const int page = chunk * kChunkPages + p;
+            const uint8_t* at = page * kPage < longest ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
+            keys = p == wave ? at : keys;
+            rec[p] = at ? at : a.c.pool;
+        }
+        if (!first) __syncthreads();  // the last slot's digits have been read
 
-        float s[4][NP], dv[4] = {};
-        v4i vc[8];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
-        if (rec) {
-            v4i kc[4][2];
-            float dk[4];
+        v4i kc[4][2], vc[kChunkPages][2];
+        float dk[4], dv[4] = {};
+        if (keys) {
+            ask_scales(keys + kRecordKs, col, dk, dv);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) kc[t][h] = load16(rec, key_at, t * kHeadDim + 64 * h);
-            token_scales(rec, col, dk, dv);
+                for (int h = 0; h < 2; ++h) kc[t][h] = load16(keys, key_at, t * kHeadDim + 64 * h);
+        }
 #pragma unroll
-            for (int n = 0; n < 8; ++n) vc[n] = load16(rec, value_at, 256 * n);
+        for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
+        __builtin_amdgcn_sched_barrier(0);
+        if (first) {  // while they are on their way
+            float factor;
+            cut_query(words, a.scale_log2, qd, factor);
+#pragma unroll
+            for (int r = 0; r < NP; ++r) factors[r] = __shfl(factor, PACK ? 4 * group : 4 * group + r, kWave);
+            if constexpr (PACK) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int dg = col & 3;
+                        qd[h].d[0][i] = dg == 0 ? qd[h].d[0][i] : dg == 1 ? qd[h].d[1][i] : dg == 2 ? qd[h].d[2][i] : 0;
+                    }
+            }
+        }
+        first = false;
+        float s[4][NP];
+        if (keys) {
+            clean_scales(dk, dv);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 v4i d[DIGITS];
 #pragma unroll
-                for (int g = 0; g < DIGITS; ++g) {
-                    d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
-                    d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
-                }
-                const int token = page * kPage + 4 * col + t;
+                for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
+#pragma unroll
+                for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
+                const int token = (chunk * kChunkPages + wave) * kPage + 4 * col + t;
 #pragma unroll
                 for (int r = 0; r < NP; ++r) {
                     float x;
@@ -332,113 +390,91 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
                     else x = score_of(d[0][r], d[1][r], d[2][r], dk[t]);
                     s[t][r] = token < lens[r] ? x : -__builtin_inff();
                 }
+                if constexpr (!PACK) __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
         }
+        // the chunk's largest score, then its largest weight, over the waves
+        float mc[NP], unit[NP], up[NP];
 #pragma unroll
         for (int r = 0; r < NP; ++r) {
-            const float m = row_max(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r]))) * factors[r];
+            const float m = row_max(max2(max3(s[0][r], s[1][r], s[2][r]), s[3][r])) * factors[r];
             if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
         }
-        if constexpr (!PACK) {
-            for (int i = tid; i < PAIRS * SUMS; i += 256) sums[0][0][i] = sums[0][1][i] = 0;
-        }
         __syncthreads();
-        float mc[NP];
 #pragma unroll
         for (int r = 0; r < NP; ++r) {
             const int p = PACK ? group : 4 * group + r;
             mc[r] = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
             const float safe = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
-            float e[4], w = 0.0f;
+            float e[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factors[r], -safe));
                 s[t][r] = e[t] * dv[t];
-                w = fmaxf(w, s[t][r]);
             }
             lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
-            w = row_max(w);
+            const float w = row_max(max3(max3(0.0f, s[0][r], s[1][r]), s[2][r], s[3][r]));
             if (col == 0) top[1][wave][p] = w;
         }
         __syncthreads();
-        float up[NP];
 #pragma unroll
         for (int r = 0; r < NP; ++r) {
             const int p = PACK ? group : 4 * group + r;
-            up[r] = pow2i(22 - exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))));
-        }
-        v4i acc[DIGITS][8];
-        if (rec) {
+            const int e = exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p])));
+            up[r] = pow2i(22 - e);
+            unit[r] = pow2i(e - 22);
+            uint32_t b[3];
+            cut_weights(s, r, up[r], b);
+            // operand rows: PACK 4 pair + digit; else one operand a digit, row = pair.  Pieces swizzled by the row (see store_digits).
+            if constexpr (PACK) {
 #pragma unroll
-            for (int r = 0; r < NP; ++r) {
-                uint32_t y[4], b[3];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(s[t][r], up[r], 8421504.0f));  // 2^23 + 0x8080
-                gather_bytes(y, b[2], b[1], b[0]);
-                b[1] ^= 0x80808080u;
-                b[2] ^= 0x80808080u;
-                // operand rows: PACK 4 pair + digit; else one operand a digit, row = pair
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<uint32_t*>(digits + kChunk * (4 * group + g) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ g) + 4 * (col & 3)) = g < 3 ? b[g] : 0u;
+            } else {
 #pragma unroll
                 for (int g = 0; g < 3; ++g)
-                    *reinterpret_cast<uint32_t*>(digits[wave] + (PACK ? 4 * group + g : g * kPairs + 4 * group + r) * kDigitStride + 4 * col) = b[g];
-                if constexpr (PACK) *reinterpret_cast<uint32_t*>(digits[wave] + (4 * group + 3) * kDigitStride + 4 * col) = 0u;
-            }
-            wave_lds_order();
-            v4i w[DIGITS];
-#pragma unroll
-            for (int g = 0; g < DIGITS; ++g) w[g] = *reinterpret_cast<const v4i*>(digits[wave] + (g * kPairs + col) * kDigitStride + 16 * group);
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int g = 0; g < DIGITS; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], vc[n], zero, 0, 0, 0);
-            if constexpr (!PACK) {
-#pragma unroll
-                for (int n = 0; n < 8; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {  // integers: the order of these additions changes nothing
-                        const int at = (4 * group + r) * SUMS + 16 * n + col;
-                        atomicAdd(&sums[0][0][at], acc[0][n][r]);
-                        atomicAdd(&sums[0][1][at], acc[1][n][r] * 256 + acc[2][n][r]);
-                    }
-            }
-        }
-        if constexpr (PACK) {
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                sums[wave][0][group * SUMS + 16 * n + col] = rec ? acc[0][n][0] : 0;
-                sums[wave][1][group * SUMS + 16 * n + col] = rec ? acc[0][n][1] * 256 + acc[0][n][2] : 0;
+                    *reinterpret_cast<uint32_t*>(digits + kChunk * (g * kPairs + 4 * group + r) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ r) + 4 * (col & 3)) = b[g];
             }
         }
         __syncthreads();
+        v4i acc[DIGITS][2];
+#pragma unroll
+        for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+            for (int g = 0; g < DIGITS; ++g) {
+                const v4i w = load_digits(digits, g, p, lane);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, vc[p][n], p == 0 ? zero : acc[g][n], 0, 0, 0);
+            }
 
-        // the chunk's result: a wave takes a pair at a time, a lane two columns
-        for (int p = wave; p < PAIRS; p += 4) {
-            if (!((members >> p) & 1u)) continue;
+        // of each pair two columns a lane
+#pragma unroll
+        for (int r = 0; r < NP; ++r) {
+            const int p = PACK ? group : 4 * group + r;
             const float lc = row_sum((lsum[0][p][col] + lsum[1][p][col]) + (lsum[2][p][col] + lsum[3][p][col]));
-            const float m = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
-            const float unit = pow2i(exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p]))) - 22);
+            const int pair_len = __shfl(len, p, kWave);
+            if (!((members >> p) & 1u)) continue;
+            const int row = pair_row(a, p);
+            const size_t head = (size_t)(row0 + row) * a.Hq + kvh * a.G + p - row * a.G;
             float o[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                int hi = 0, lo = 0;
-#pragma unroll
-                for (int w = 0; w < (PACK ? 4 : 1); ++w) {
-                    hi += sums[w][0][p * SUMS + 2 * lane + k];
-                    lo += sums[w][1][p * SUMS + 2 * lane + k];
-                }
-                o[k] = __builtin_fmaf((float)hi, 65536.0f, (float)lo);
-            }
-            const size_t head = (size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G;
-            if (__builtin_amdgcn_readlane(len, p) <= kChunk) {  // the row's only chunk
+            for (int n = 0; n < 2; ++n) o[n] = PACK ? digits_value(acc[0][n][0], acc[0][n][1], acc[0][n][2]) : digits_value(acc[0][n][r], acc[PACK ? 0 : 1][n][r], acc[PACK ? 0 : 2][n][r]);
+            if (pair_len <= kChunk) {  // the row's only chunk
                 float fm = -__builtin_inff(), l = 0.0f, fa, fb;
-                fold_step(fm, l, m, lc, unit, fa, fb);
+                fold_step(fm, l, mc[r], lc, unit[r], fa, fb);
                 const float by = row_factor(l);
-                reinterpret_cast<uint32_t*>(a.out + head * kHeadDim)[lane] =
-                    to_bf16(fold_value(0.0f, o[0], fa, fb) * by) | ((uint32_t)to_bf16(fold_value(0.0f, o[1], fa, fb) * by) << 16);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) a.out[head * kHeadDim + 32 * wave + 16 * n + col] = to_bf16(fold_value(0.0f, o[n], fa, fb) * by);
             } else {
                 const size_t at = head * a.chunks + chunk;
-                if (lane == 0) a.part[at] = make_float4(m, lc, unit, 0.0f);
-                reinterpret_cast<float2*>(a.part_o + at * kHeadDim)[lane] = make_float2(o[0], o[1]);
+                if (wave == 0 && col == 0) a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) a.part_o[at * kHeadDim + 32 * wave + 16 * n + col] = o[n];
             }
         }
     }
@@ -478,17 +514,6 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
 }
 
 // ---------------------------------------------------------------- a chunk by one wave: what both walks share
-
-// One digit of four neighbouring tokens' weights to a word: the weights as integers of 22 bits.
-__device__ __forceinline__ void cut_weights(const float (&w)[4][4], int r, float up, uint32_t (&b)[3])
-{
-    uint32_t y[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) y[t] = __float_as_uint(__builtin_fmaf(w[t][r], up, 8421504.0f));  // 2^23 + 0x8080
-    gather_bytes(y, b[2], b[1], b[0]);
-    b[1] ^= 0x80808080u;
-    b[2] ^= 0x80808080u;
-}
 
 // Scores to weights e d^V, in place, and what the fold needs of the chunk.  scales(p, dk, dv): those of this lane's tokens of page p.
 template <class Scales>
@@ -533,34 +558,6 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
     }
 }
 
-// The digits of a chunk's weights into a wave's LDS, as the second product takes them: of each digit sixteen rows (pairs) of 256 bytes (tokens), the
-// sixteen-byte pieces of a row swizzled by the pair.  here: the lane, hidden from the compiler, so that it keeps no addresses over a loop.
-constexpr int kChunkDigits = 3 * kPairs * kChunk;
-__device__ __forceinline__ void store_digits(const float (&w)[kChunkPages][4][4], const float (&up)[4], uint8_t* digits, int here)
-{
-    const int g4 = here >> 4, c = here & 15;
-    wave_lds_order();
-#pragma unroll
-    for (int p = 0; p < kChunkPages; ++p) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            uint32_t b[3];
-            cut_weights(w[p], r, up[r], b);
-            // piece (4 p + c / 4) ^ (4 g4 + r) of row 4 g4 + r
-            uint8_t* at = digits + kChunk * (4 * g4 + r) + 64 * (p ^ g4) + 16 * ((c >> 2) ^ r) + 4 * (c & 3);
-#pragma unroll
-            for (int g = 0; g < 3; ++g) *reinterpret_cast<uint32_t*>(at + g * kPairs * kChunk) = b[g];
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    wave_lds_order();
-}
-// This lane's operand of digit g, tokens of page p.
-__device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, int here)
-{
-    return *reinterpret_cast<const v4i*>(digits + g * kPairs * kChunk + ((272 * (here & 15)) ^ (16 * (here >> 4) + 64 * p)));
-}
-
 __device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int kvh, unsigned members, const float (&l)[4], const float (&o)[8][4])
 {
     const int lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
@@ -568,7 +565,8 @@ __device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int
     for (int r = 0; r < 4; ++r) {
         const int p = 4 * group + r;
         if (!((members >> p) & 1u)) continue;
-        uint16_t* out = a.out + ((size_t)(row0 + p / a.G) * a.Hq + kvh * a.G + p % a.G) * kHeadDim;
+        const int row = pair_row(a, p);
+        uint16_t* out = a.out + ((size_t)(row0 + row) * a.Hq + kvh * a.G + p - row * a.G) * kHeadDim;
         const float by = row_factor(l[r]);
 #pragma unroll
         for (int n = 0; n < 8; ++n) out[16 * n + col] = to_bf16(o[n][r] * by);
@@ -582,12 +580,15 @@ __device__ __forceinline__ void walk_alone(const kv8_attn_args& a, int kvh, int 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
     uint8_t* digits = digits_of + wave * kChunkDigits;
     const int row0 = tile * a.rows_per_tile;
-    const bool live = col < a.rows_per_tile * a.G && row0 + col / a.G < a.R;
+    const bool live = col < a.rows_per_tile * a.G && row0 + pair_row(a, col) < a.R;
     int slot = -1, len = 0;
-    if (live) len = row_length(a, row0 + col / a.G, slot);
+    if (live) len = row_length(a, row0 + pair_row(a, col), slot);
+    const int my_pair_row = pair_row(a, col);
+    uint32_t words[16];
+    ask_query(live ? a.q + ((size_t)(row0 + my_pair_row) * a.Hq + kvh * a.G + col - my_pair_row * a.G) * kHeadDim : nullptr, words);
     q_digits qd[2];
     float factor, factors[4];
-    load_query(live ? a.q + ((size_t)(row0 + col / a.G) * a.Hq + kvh * a.G + col % a.G) * kHeadDim : nullptr, a.scale_log2, qd, factor);
+    cut_query(words, a.scale_log2, qd, factor);
 #pragma unroll
     for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
     const v4i zero = {0, 0, 0, 0};
@@ -701,12 +702,12 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
     __shared__ __attribute__((aligned(1024))) uint8_t digits_of[4 * kChunkDigits];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, group = lane >> 4, col = lane & 15;
     uint8_t* digits = digits_of + wave * kChunkDigits;
-    const int kvh = blockIdx.x, tile0 = 4 * (gridDim.y - 1 - blockIdx.y);  // the last rows, which have most to read, begin
+    const int kvh = blockIdx.x % a.c.Hkv, tile0 = 4 * ((gridDim.x - 1 - blockIdx.x) / a.c.Hkv);  // the last rows, which have most to read, begin
     // lane: pair `col` of tile `group`; every wave knows all four tiles
-    const int pair_row = (tile0 + group) * a.rows_per_tile + col / a.G;
-    const bool live = col < a.rows_per_tile * a.G && pair_row < a.R;
+    const int in_tile = pair_row(a, col), lane_row = (tile0 + group) * a.rows_per_tile + in_tile;
+    const bool live = col < a.rows_per_tile * a.G && lane_row < a.R;
     int slot = -1, len = 0;
-    if (live) len = row_length(a, pair_row, slot);
+    if (live) len = row_length(a, lane_row, slot);
 
     int kinds = 0;
     for (unsigned long long left = __ballot(live); left != 0 && kinds <= kWalkSlots; ++kinds) {
@@ -719,11 +720,13 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
     }
 
     const int my_row0 = (tile0 + wave) * a.rows_per_tile;
+    uint32_t words[16];
+    ask_query(col < a.rows_per_tile * a.G && my_row0 + in_tile < a.R
+                  ? a.q + ((size_t)(my_row0 + in_tile) * a.Hq + kvh * a.G + col - in_tile * a.G) * kHeadDim : nullptr,
+              words);
     q_digits qd[2];
     float factor, factors[4];
-    load_query(col < a.rows_per_tile * a.G && my_row0 + col / a.G < a.R
-                   ? a.q + ((size_t)(my_row0 + col / a.G) * a.Hq + kvh * a.G + col % a.G) * kHeadDim : nullptr,
-               a.scale_log2, qd, factor);
+    cut_query(words, a.scale_log2, qd, factor);
 #pragma unroll
     for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
     const v4i zero = {0, 0, 0, 0};
@@ -835,21 +838,23 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
                 }
                 float dk[4], dv[4];
                 clean_scales(chunk_scales + 512 * p, col, dk, dv);
+                v4i d[4][3];
 #pragma unroll
-                for (int two = 0; two < 2; ++two) {
-                    v4i d[2][3];
+                for (int two = 0; two < 4; two += 2) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            const v4i k = *reinterpret_cast<const v4i*>(codes + (h ? key_at ^ 64u : key_at) + 2048 * (2 * two + t));
+                        for (int t = two; t < two + 2; ++t) {
+                            const v4i k = *reinterpret_cast<const v4i*>(codes + (h ? key_at ^ 64u : key_at) + 2048 * t);
 #pragma unroll
                             for (int g = 0; g < 3; ++g) d[t][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[h].d[g], k, h ? d[t][g] : zero, 0, 0, 0);
                         }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < 4; ++t) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[p][2 * two + t][r] = score_of(d[t][0][r], d[t][1][r], d[t][2][r], dk[2 * two + t]);
+                    for (int r = 0; r < 4; ++r) s[p][t][r] = score_of(d[t][0][r], d[t][1][r], d[t][2][r], dk[t]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
@@ -941,6 +946,7 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.Hq = Hq;
     a.G = Hq / cache.Hkv;
     const bool packed = !slots && a.G <= 4;  // rows that share nothing, one to a tile
+    a.inverse_G = 65536 / a.G + 1;
     a.rows_per_tile = slots ? kPairs / a.G : 1;
     a.len_offset = len_offset;
     a.chunks = (cache.max_pages + kChunkPages - 1) / kChunkPages;
@@ -949,12 +955,12 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.part_o = static_cast<float*>(ws);
     a.part = reinterpret_cast<float4*>(a.part_o + pairs * kHeadDim);
     const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
+    if (tiles * cache.Hkv > 0x7FFFFFFFll / 256 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
     if (slots && tiles * cache.Hkv >= 2048) {
-        hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3(cache.Hkv, (unsigned)((tiles + 3) / 4)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3((unsigned)((tiles + 3) / 4 * cache.Hkv)), dim3(256), 0, s, a);
         return check_launch();
     }
-    if (tiles > 65535 || a.chunks > 65535 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
-    const dim3 grid(cache.Hkv, (unsigned)tiles, a.chunks);
+    const dim3 grid((unsigned)(tiles * cache.Hkv), a.chunks);
     if (packed) hipLaunchKernelGGL(kv8_attn_chunk_kernel<true>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(kv8_attn_chunk_kernel<false>, grid, dim3(256), 0, s, a);
     if (a.chunks > 1) hipLaunchKernelGGL(kv8_attn_combine_kernel, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);
