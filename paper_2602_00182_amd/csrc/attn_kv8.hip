@@ -287,7 +287,7 @@ __device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, 
 // PACK: up to four pairs (one row of up to four heads a KV head).  Their digits fill the sixteen rows of one operand, row 4 pair + digit, so a
 // product is one instruction instead of three and a lane has all digits of one pair: a quarter of the scores' arithmetic.
 template <bool PACK>
-__global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
+__global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
 {
     constexpr int NP = PACK ? 1 : 4;                 // pairs of a lane
     constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
         const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
         const int mine = slot == now ? len : 0;
         const unsigned members = (unsigned)(__ballot(mine > chunk * kChunk) & 0xFFFFull);
-        todo &= ~members;
+        todo = PACK ? 0u : todo & ~members;  // PACK: one row, one slot
         int longest = mine;
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
             keys = p == wave ? at : keys;
             rec[p] = at ? at : a.c.pool;
         }
-        if (!first) __syncthreads();  // the last slot's digits have been read
+        if (!PACK && !first) __syncthreads();  // the last slot's digits have been read
 
         v4i kc[4][2], vc[kChunkPages][2];
         float dk[4], dv[4] = {};
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
 #pragma unroll
             for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
         __builtin_amdgcn_sched_barrier(0);
-        if (first) {  // while they are on their way
+        if (PACK || first) {  // while they are on their way
             float factor;
             cut_query(words, a.scale_log2, qd, factor);
 #pragma unroll
