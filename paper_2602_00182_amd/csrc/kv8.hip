@@ -3,77 +3,192 @@
 
 namespace det {
 
-// One row's heads of qkv, sixteen lanes a head: lane i holds the rotation pairs 4i..4i+3, i.e. columns 4i..4i+3 and 64+4i..64+4i+3.
-// Query heads are rotated into qbuf; key heads are rotated, rounded to bf16 and quantized, value heads quantized as they are.
-// Block (256): sixteen heads.  Grid (R, ceil((Hq + 2 Hkv) / 16)).
-__global__ __launch_bounds__(256) void kv8_append_kernel(const uint16_t* __restrict__ qkv, int ldqkv, uint16_t* __restrict__ qbuf, kv8_cache c,
-                                                         const int32_t* __restrict__ positions, const int32_t* __restrict__ slots,
-                                                         const float* __restrict__ cos_t, const float* __restrict__ sin_t, int Hq, int Lrope)
+// The quantizer on 128 values that eight neighbouring lanes hold, sixteen each: d = max|v| / 127, codes clamp(rint(v / d)); a row that is not finite
+// has no codes and the scale NaN.
+__device__ __forceinline__ float quantize_row(const float (&v)[16], uint32_t (&codes)[4])
 {
-    const int r = blockIdx.x, head = blockIdx.y * 16 + (int)(threadIdx.x >> 4), i0 = 4 * (int)(threadIdx.x & 15);
-    if (head >= Hq + 2 * c.Hkv) return;
-    const int pos = positions[r];
-    const uint16_t* x = qkv + (size_t)r * ldqkv + head * kHeadDim;
-    const uint2 lo = *reinterpret_cast<const uint2*>(x + i0), hi = *reinterpret_cast<const uint2*>(x + 64 + i0);
-    uint16_t y[8] = {(uint16_t)lo.x, (uint16_t)(lo.x >> 16), (uint16_t)lo.y, (uint16_t)(lo.y >> 16),
-                     (uint16_t)hi.x, (uint16_t)(hi.x >> 16), (uint16_t)hi.y, (uint16_t)(hi.y >> 16)};
-    if (head < Hq + c.Hkv) {
-        const int p = pos < 0 ? 0 : (pos >= Lrope ? Lrope - 1 : pos);
-        const float4 cs = *reinterpret_cast<const float4*>(cos_t + (size_t)p * 64 + i0);
-        const float4 sn = *reinterpret_cast<const float4*>(sin_t + (size_t)p * 64 + i0);
-        const float cv[4] = {cs.x, cs.y, cs.z, cs.w}, sv[4] = {sn.x, sn.y, sn.z, sn.w};
+    uint32_t big = 0u;  // magnitudes order like the integers of their bits, NaN and infinities are the largest
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint16_t a, b;
-            rope_pair(y[k], y[4 + k], cv[k], sv[k], a, b);
-            y[k] = a;
-            y[4 + k] = b;
-        }
-    }
-    if (head < Hq) {
-        uint16_t* q = qbuf + ((size_t)r * Hq + head) * kHeadDim;
-        *reinterpret_cast<uint2*>(q + i0) = make_uint2(y[0] | ((uint32_t)y[1] << 16), y[2] | ((uint32_t)y[3] << 16));
-        *reinterpret_cast<uint2*>(q + 64 + i0) = make_uint2(y[4] | ((uint32_t)y[5] << 16), y[6] | ((uint32_t)y[7] << 16));
-        return;
-    }
-
-    // The quantizer: d = max|y| / 127, codes clamp(rint(y / d)); a row that is not finite has no codes and the scale NaN.
-    float v[8], amax = 0.0f;
-    bool bad = false;
+    for (int k = 0; k < 16; ++k) big = max(big, __float_as_uint(v[k]) & 0x7FFFFFFFu);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        v[k] = bf16_to_f32(y[k]);
-        bad |= !(fabsf(v[k]) < __builtin_inff());
-        amax = fmaxf(amax, fabsf(v[k]));
-    }
-    amax = bad ? __builtin_inff() : amax;
+    for (int off = 1; off < 8; off <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, off, kWave));
+    const float d = big < 0x7F800000u ? __uint_as_float(big) / 127.0f : __builtin_nanf("");
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, kWave));
-    const bool finite = amax < __builtin_inff();
-    const float d = finite ? amax / 127.0f : __builtin_nanf("");
-    uint32_t codes[2] = {0u, 0u};
+    for (int k = 0; k < 4; ++k) codes[k] = 0u;
     if (d > 0.0f) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 16; ++k) {
             const float n = rintf(v[k] / d);
             const int code = n < -127.0f ? -127 : (n > 127.0f ? 127 : (int)n);
             codes[k >> 2] |= (uint32_t)(code & 0xFF) << (8 * (k & 3));
         }
     }
-    if (pos < 0) return;
-    const bool key = head < Hq + c.Hkv;
-    uint8_t* rec = kv8_record(c, slots ? slots[r] : r, pos / kPage, key ? head - Hq : head - Hq - c.Hkv);
-    if (!rec) return;
-    const int t = pos % kPage;
-    if (key) {
-        *reinterpret_cast<uint32_t*>(rec + t * kHeadDim + i0) = codes[0];
-        *reinterpret_cast<uint32_t*>(rec + t * kHeadDim + 64 + i0) = codes[1];
-    } else {
-        uint8_t* dst = rec + kRecordV + (t >> 4) * (16 * kHeadDim) + (t & 15);
+    return d;
+}
+__device__ __forceinline__ void widen(const uint4& lo, const uint4& hi, float (&v)[16])
+{
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dst[16 * ((k < 4 ? 0 : 60) + i0 + k)] = (uint8_t)(codes[k >> 2] >> (8 * (k & 3)));
+    for (int k = 0; k < 8; ++k) {
+        v[2 * k] = bf16lo_to_f32(w[k]);
+        v[2 * k + 1] = bf16hi_to_f32(w[k]);
     }
-    if (i0 == 0) *reinterpret_cast<float*>(rec + (key ? kRecordKs : kRecordVs) + 4 * t) = d;
+}
+
+struct append_args {
+    const uint16_t* qkv;
+    uint16_t* qbuf;
+    kv8_cache c;
+    const int32_t* positions;
+    const int32_t* slots;
+    const float* cos_t;
+    const float* sin_t;
+    int ldqkv, Hq, Lrope, R;
+    uint32_t items, item_blocks;
+};
+
+// V heads of 64 rows: their codes meet in LDS, and a thread puts sixteen tokens of one column side by side, as the record has them, so that a run of
+// neighbouring tokens is stored in pieces of sixteen bytes (3332 rows of 32/8 heads 30 -> 24 us against a byte at a time).
+constexpr int kValueRows = 64;
+__device__ __forceinline__ void append_values(const append_args& a, uint32_t block, uint8_t (&codes_of)[kValueRows][kHeadDim + 4],
+                                              unsigned long long (&place)[kValueRows])
+{
+    const int kvh = (int)(block % a.c.Hkv), row0 = (int)(block / a.c.Hkv) * kValueRows, i0 = 8 * (int)(threadIdx.x & 7);
+#pragma unroll
+    for (int u = 0; u < kValueRows / 32; ++u) {
+        const int in = 32 * u + (int)(threadIdx.x >> 3), row = min(row0 + in, a.R - 1);
+        const int pos = a.positions[row], slot = a.slots ? a.slots[row] : row;
+        const uint16_t* x = a.qkv + (size_t)row * a.ldqkv + (a.Hq + a.c.Hkv + kvh) * kHeadDim;
+        float v[16];
+        widen(*reinterpret_cast<const uint4*>(x + i0), *reinterpret_cast<const uint4*>(x + 64 + i0), v);
+        uint32_t codes[4];
+        const float d = quantize_row(v, codes);
+        *reinterpret_cast<uint32_t*>(&codes_of[in][i0]) = codes[0];
+        *reinterpret_cast<uint32_t*>(&codes_of[in][i0 + 4]) = codes[1];
+        *reinterpret_cast<uint32_t*>(&codes_of[in][64 + i0]) = codes[2];
+        *reinterpret_cast<uint32_t*>(&codes_of[in][68 + i0]) = codes[3];
+        if (i0 == 0) {
+            // sixteen tokens' codes are aligned to sixteen bytes: the address of theirs and, in its low bits, the token's place among them
+            uint8_t* rec = row0 + in < a.R && pos >= 0 ? kv8_record(a.c, slot, pos / kPage, kvh) : nullptr;
+            const int t = pos % kPage;
+            place[in] = rec ? (unsigned long long)(rec + kRecordV + (t >> 4) * (16 * kHeadDim)) + (t & 15) : 0ull;
+            if (rec) *reinterpret_cast<float*>(rec + kRecordVs + 4 * t) = d;
+        }
+    }
+    __syncthreads();
+    const int column = threadIdx.x & 127, half = threadIdx.x >> 7;
+    uint32_t piece[4] = {0u, 0u, 0u, 0u}, have = 0u;
+    unsigned long long at = 0ull;
+    for (int k = 0; k <= kValueRows / 2; ++k) {
+        const unsigned long long next = k < kValueRows / 2 ? place[half * (kValueRows / 2) + k] : 0ull;
+        if ((next & ~15ull) != at) {
+            uint8_t* dst = reinterpret_cast<uint8_t*>(at) + 16 * column;
+            if (have == 0xFFFFu) {
+                *reinterpret_cast<uint4*>(dst) = make_uint4(piece[0], piece[1], piece[2], piece[3]);
+            } else if (have != 0u) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t bits = (have >> (4 * w)) & 15u;
+                    if (bits == 15u) *reinterpret_cast<uint32_t*>(dst + 4 * w) = piece[w];
+                    else
+                        for (int e = 0; e < 4; ++e)
+                            if ((bits >> e) & 1u) dst[4 * w + e] = (uint8_t)(piece[w] >> (8 * e));
+                }
+            }
+            have = 0u;
+            at = next & ~15ull;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) piece[w] = 0u;
+        }
+        if (next != 0ull) {
+            const int t = (int)(next & 15ull);
+            const uint32_t byte = (uint32_t)codes_of[half * (kValueRows / 2) + k][column] << (8 * (t & 3));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) piece[w] |= (t >> 2) == w ? byte : 0u;
+            have |= 1u << t;
+        }
+    }
+}
+
+// Heads of projection rows, eight lanes a (row, head): lane i holds the rotation pairs 8i..8i+7, i.e. columns 8i..8i+7 and 64+8i..64+8i+7.
+// Query heads are rotated into qbuf; key heads are rotated, rounded to bf16 and quantized, value heads quantized as they are.
+// Block (256): 32 heads at a time, kAppendTurns times, everything that can be asked for asked for first: the way is position, then its angles; what
+// bounds a prompt is that chain and the bytes (rows in, queries and codes out).  TILED: the value heads in blocks of their own (append_values), from
+// item_blocks on.
+constexpr int kAppendTurns = 2;
+constexpr int kTiledRows = 128;  // rows of a call from which its value heads are stored in runs
+template <bool TILED>
+__global__ __launch_bounds__(256) void kv8_append_kernel(append_args a)
+{
+    const kv8_cache& c = a.c;
+    if constexpr (TILED) {
+        __shared__ uint8_t codes_of[kValueRows][kHeadDim + 4];
+        __shared__ unsigned long long place[kValueRows];
+        if (blockIdx.x >= a.item_blocks) {
+            append_values(a, blockIdx.x - a.item_blocks, codes_of, place);
+            return;
+        }
+    }
+    const uint32_t heads = a.Hq + (TILED ? 1 : 2) * c.Hkv, first = blockIdx.x * (32 * kAppendTurns) + (threadIdx.x >> 3);
+    const int i0 = 8 * (int)(threadIdx.x & 7);
+    uint4 lo[kAppendTurns], hi[kAppendTurns];
+    int pos[kAppendTurns], slot[kAppendTurns], row[kAppendTurns], head[kAppendTurns];
+#pragma unroll
+    for (int u = 0; u < kAppendTurns; ++u) {
+        const uint32_t item = min(first + 32 * u, a.items - 1);
+        row[u] = (int)(item / heads);
+        head[u] = (int)(item % heads);
+        pos[u] = a.positions[row[u]];
+        slot[u] = a.slots ? a.slots[row[u]] : row[u];
+        const uint16_t* x = a.qkv + (size_t)row[u] * a.ldqkv + head[u] * kHeadDim;
+        lo[u] = *reinterpret_cast<const uint4*>(x + i0);
+        hi[u] = *reinterpret_cast<const uint4*>(x + 64 + i0);
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendTurns; ++u) {
+        if (first + 32 * u >= a.items) return;
+        float v[16];
+        widen(lo[u], hi[u], v);
+        const bool value = !TILED && head[u] >= a.Hq + c.Hkv;
+        if (!value) {
+            const int p = pos[u] < 0 ? 0 : (pos[u] >= a.Lrope ? a.Lrope - 1 : pos[u]);
+            const float4* cp = reinterpret_cast<const float4*>(a.cos_t + (size_t)p * 64 + i0);
+            const float4* sp = reinterpret_cast<const float4*>(a.sin_t + (size_t)p * 64 + i0);
+            const float4 c0 = cp[0], c1 = cp[1], s0 = sp[0], s1 = sp[1];
+            const float cv[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, sv[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {  // rope_pair (common.h) on fp32 operands
+                const float l = v[k] * cv[k], h = v[8 + k] * cv[k];
+                const float x = __builtin_fmaf(-v[8 + k], sv[k], l), y = __builtin_fmaf(v[k], sv[k], h);
+                v[k] = bf16_to_f32(f32_to_bf16_rne(x));
+                v[8 + k] = bf16_to_f32(f32_to_bf16_rne(y));
+            }
+            if (head[u] < a.Hq) {
+                uint32_t o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = (__float_as_uint(v[2 * k]) >> 16) | (__float_as_uint(v[2 * k + 1]) & 0xFFFF0000u);
+                uint16_t* q = a.qbuf + ((size_t)row[u] * a.Hq + head[u]) * kHeadDim;
+                *reinterpret_cast<uint4*>(q + i0) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(q + 64 + i0) = make_uint4(o[4], o[5], o[6], o[7]);
+                continue;
+            }
+        }
+        uint32_t codes[4];
+        const float d = quantize_row(v, codes);
+        if (pos[u] < 0) continue;
+        uint8_t* rec = kv8_record(c, slot[u], pos[u] / kPage, value ? head[u] - a.Hq - c.Hkv : head[u] - a.Hq);
+        if (!rec) continue;
+        const int t = pos[u] % kPage;
+        if (!value) {
+            *reinterpret_cast<uint2*>(rec + t * kHeadDim + i0) = make_uint2(codes[0], codes[1]);
+            *reinterpret_cast<uint2*>(rec + t * kHeadDim + 64 + i0) = make_uint2(codes[2], codes[3]);
+        } else {
+            uint8_t* dst = rec + kRecordV + (t >> 4) * (16 * kHeadDim) + (t & 15) + 16 * i0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) dst[16 * ((k < 8 ? 0 : 56) + k)] = (uint8_t)(codes[k >> 2] >> (8 * (k & 3)));
+        }
+        if (i0 == 0) *reinterpret_cast<float*>(rec + (value ? kRecordVs : kRecordKs) + 4 * t) = d;
+    }
 }
 
 // bf16 values of rows of the cache, sixteen lanes a (row, KV head), lane i the columns 8i..8i+7; zeros where there is no page.
@@ -142,9 +257,15 @@ extern "C" int det_kv8_rope_append(const void* qkv, int ldqkv, void* qbuf, void*
     if (ldqkv < (Hq + 2 * Hkv) * D) return DET_EINVAL;
     if (!aligned16(qkv) || !aligned16(qbuf) || !aligned16(rope_cos) || !aligned16(rope_sin) || ldqkv % 8) return DET_EALIGN;
     const kv8_cache c{static_cast<uint8_t*>(pool), page_table, n_pages, n_slots, max_pages, Hkv};
-    hipLaunchKernelGGL(kv8_append_kernel, dim3(R, (Hq + 2 * Hkv + 15) / 16), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       static_cast<const uint16_t*>(qkv), ldqkv, static_cast<uint16_t*>(qbuf), c, positions, slots, rope_cos, rope_sin, Hq,
-                       Lrope);
+    const bool tiled = R >= kTiledRows;
+    const long long items = (long long)R * (Hq + (tiled ? 1 : 2) * Hkv), per_block = 32 * kAppendTurns, item_blocks = (items + per_block - 1) / per_block;
+    const long long blocks = item_blocks + (tiled ? (long long)((R + kValueRows - 1) / kValueRows) * Hkv : 0);
+    if (items > 0x7FFFFFFFll || blocks > 0x7FFFFFFFll / 256) return DET_ESHAPE;
+    const append_args a{static_cast<const uint16_t*>(qkv), static_cast<uint16_t*>(qbuf), c, positions, slots, rope_cos, rope_sin, ldqkv, Hq, Lrope, R,
+                        (uint32_t)items, (uint32_t)item_blocks};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (tiled) hipLaunchKernelGGL(kv8_append_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(kv8_append_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, s, a);
     return check_launch();
 }
 

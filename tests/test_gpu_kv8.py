@@ -76,6 +76,47 @@ def test_append_writes_the_quantizers_bytes_and_nothing_else(d, R, Hq, Hkv):
     assert np.array_equal(down_bf16(v), ds.f32_to_bf16_bits(vc.astype(np.float32) * vd[..., None]))
 
 
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_append_of_many_rows_in_runs_and_in_no_order(d, seed):
+    """Some hundred rows: runs of neighbouring positions that begin anywhere, single rows, rows without a page, every one where it belongs."""
+    rng = np.random.default_rng(seed)
+    Hq, Hkv, S, pages = 3, 1, 9, 5
+    P = S * pages + 2
+    table = rng.permutation(P)[:S * pages].reshape(S, pages).astype(np.int32)
+    table[3, 1] = -1
+    spots = []
+    for s in range(S):
+        at = int(rng.integers(0, 30))
+        while at < pages * PAGE:
+            run = int(rng.choice([1, 2, 5, 16, 33, 70]))
+            spots.append([(s, p) for p in range(at, min(at + run, pages * PAGE))])
+            at += run + int(rng.integers(0, 40))
+    spots = [x for i in rng.permutation(len(spots)) for x in (spots[i] if rng.integers(2) else spots[i][::-1])]
+    spots.insert(100, (2, -1))
+    spots.insert(101, (S, 3))
+    slots, pos = (np.array([x[i] for x in spots], dtype=np.int32) for i in (0, 1))
+    R = len(spots)
+    x = ds.normal_bf16(7050 + seed, (R, (Hq + 2 * Hkv) * D))
+    cos, sin = ds.rope_tables(pages * PAGE, D)
+    pool0 = rng.integers(0, 256, (P, Hkv, RECORD), dtype=np.uint8)
+    pool, q = up(pool0.copy()), torch.empty((R, Hq, D), dtype=torch.bfloat16, device=DEV)
+    step(f"{R} rows in runs")
+    d.det_kv8_rope_append(up_bf16(x), q, pool, up(table), up(pos), up(slots), up(cos), up(sin))
+    torch.cuda.synchronize()
+    heads = up_bf16(np.ascontiguousarray(x.reshape(R, Hq + 2 * Hkv, D)[:, :Hq + Hkv]))
+    turned = torch.empty_like(heads)
+    d.det_rope(heads, turned, up(pos), up(cos), up(sin))
+    turned = down_bf16(turned)
+    assert np.array_equal(down_bf16(q), turned[:, :Hq])
+    kc, kd = quantize(turned[:, Hq:])
+    vc, vd = quantize(x.reshape(R, Hq + 2 * Hkv, D)[:, Hq + Hkv:])
+    want = pool0.copy()
+    for r in range(R):
+        if 0 <= slots[r] < S and pos[r] >= 0 and table[slots[r], pos[r] // PAGE] >= 0:
+            store(want, table[slots[r], pos[r] // PAGE], 0, pos[r] % PAGE, kc[r, 0], kd[r, 0], vc[r, 0], vd[r, 0])
+    assert np.array_equal(pool.cpu().numpy(), want)
+
+
 def test_append_of_rows_without_a_place_and_rows_that_are_not_finite(d):
     Hq, Hkv, P = 2, 1, 3
     table = np.array([[2, -1], [0, 7]], dtype=np.int32)  # page 7 does not exist
