@@ -503,6 +503,23 @@ int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_tab
                         int max_pages, const int32_t *seqlens, const int32_t *slots, void *out, void *ws, size_t ws_bytes,
                         int R, int Hq, int Hkv, int D, float scale, void *stream);
 
+/* The decoder layers on the 8-bit cache: the steps of det_decoder_layer_rows and det_qdecoder_layer in the same order, with qkv in bf16,
+ * det_kv8_rope_append and det_attn_decode_kv8 in place of the fused projection and the attention over a bf16 cache (the quantized layer's attention
+ * output goes through det_quant_act_q8).  slots may be NULL: row r is the sequence in slot r.
+ * Weights: wqkv from det_gemm_pack_b (det_quant_pack_w4 for the quantized layer), columns query, key and value heads; the others as there.
+ * cfg->Lmax: rows of the rope tables.  A row whose position has no page attends to what is there.  Same invariance: a row's bytes do not depend on R,
+ * on the other rows or on where the pages lie, and T tokens of a prompt in one call are the T calls of one. */
+size_t det_decoder_layer_kv8_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
+int det_decoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
+                          const int32_t *page_table, int n_pages, int n_slots, int max_pages, const int32_t *positions,
+                          const int32_t *slots, const float *rope_cos, const float *rope_sin, void *ws,
+                          size_t ws_bytes, int R, void *stream);
+size_t det_qdecoder_layer_kv8_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
+int det_qdecoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
+                           const int32_t *page_table, int n_pages, int n_slots, int max_pages, const int32_t *positions,
+                           const int32_t *slots, const float *rope_cos, const float *rope_sin, void *ws,
+                           size_t ws_bytes, int R, void *stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Verification of drafted tokens against the target's probabilities, from given random numbers (section 6.6: the tokens are a function of
  * what is given; nothing is drawn here).  For sequence b with n = n_drafts[b] drafts (n_drafts NULL: N; clamped to 0..N):

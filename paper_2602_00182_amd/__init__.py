@@ -5,3 +5,4 @@ tensors in place of raw pointers.  Every computation runs in the library's HIP k
 used for device memory and streams only."""
 from .api import *  # noqa: F401,F403
 from .api import __all__  # noqa: F401
+from .pages import KVPages, OutOfPages  # noqa: F401

@@ -26,7 +26,8 @@ __all__ = [
     "det_qdecoder_layer_workspace_bytes", "det_qdecoder_layer", "det_attn_decode_quant_q8",
     "det_qgemm_w4a8_swiglu_quant_supported", "det_qgemm_w4a8_swiglu_quant",
     "KV8_PAGE", "KV8_RECORD", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
-    "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8", "det_verify_drafts",
+    "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8", "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8",
+    "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -788,6 +789,33 @@ def det_attn_decode_kv8(q, pool, page_table, seqlens, slots, out, ws, scale: flo
     _check("det_attn_decode_kv8", lib().det_attn_decode_kv8(
         _contig(q, torch.bfloat16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, page_table.shape[0]),
         _contig(out, torch.bfloat16), _contig(ws), ws.numel() * ws.element_size(), R, Hq, Hkv, D, scale, _stream(stream)))
+
+
+def det_decoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
+    return lib().det_decoder_layer_kv8_workspace_bytes(C.byref(cfg), R, max_pages)
+
+
+def det_qdecoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
+    return lib().det_qdecoder_layer_kv8_workspace_bytes(C.byref(cfg), R, max_pages)
+
+
+def det_decoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream=None,
+                          _entry: str = "det_decoder_layer_kv8") -> None:
+    """One decoder layer on rows x over one layer's pool of the 8-bit cache; wqkv packed by pack_weight; slots None: row r uses slot r."""
+    R = x.shape[0]
+    cache, Hkv = _kv8(pool, page_table)
+    if x.shape != (R, cfg.H) or Hkv != cfg.Hkv or positions.shape != (R,):
+        raise ValueError("bad layer shapes")
+    if rope_cos.shape != (cfg.Lmax, cfg.D // 2) or rope_sin.shape != rope_cos.shape:
+        raise ValueError("bad layer shapes")
+    _check(_entry, getattr(lib(), _entry)(
+        C.byref(w), C.byref(cfg), _contig(x, torch.bfloat16), *cache, _contig(positions, torch.int32), _slots(slots, R, page_table.shape[0]),
+        _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), _contig(ws), ws.numel() * ws.element_size(), R, _stream(stream)))
+
+
+def det_qdecoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream=None) -> None:
+    """det_decoder_layer_kv8 on quantized weights; wqkv packed by quant_pack_weight."""
+    det_decoder_layer_kv8(w, cfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream, _entry="det_qdecoder_layer_kv8")
 
 
 def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, stream=None) -> None:

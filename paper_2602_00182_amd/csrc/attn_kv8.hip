@@ -10,6 +10,7 @@
 // brought together are powers of two.  Chunks are folded in ascending order.
 #include <type_traits>
 
+#include "geometry.h"
 #include "kv8.h"
 #include "stream.h"
 
@@ -926,7 +927,7 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
     }
 }
 
-static size_t workspace_bytes(int R, int Hq, int max_pages)
+size_t attn_decode_kv8_workspace(int R, int Hq, int max_pages)
 {
     const size_t chunks = ((size_t)max_pages + kChunkPages - 1) / kChunkPages;
     return (size_t)R * Hq * chunks * (kHeadDim + 4) * sizeof(float);
@@ -942,7 +943,7 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     if (Hq % cache.Hkv != 0 || Hq / cache.Hkv > kPairs || cache.Hkv > 65535) return DET_ESHAPE;
     if (!slots && cache.n_slots < R) return DET_ESHAPE;
     if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return DET_EALIGN;
-    if (ws_bytes < workspace_bytes(R, Hq, cache.max_pages)) return DET_EWORKSPACE;
+    if (ws_bytes < attn_decode_kv8_workspace(R, Hq, cache.max_pages)) return DET_EWORKSPACE;
     kv8_attn_args a{};
     a.q = static_cast<const uint16_t*>(q);
     a.c = cache;
@@ -963,7 +964,7 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.part = reinterpret_cast<float4*>(a.part_o + pairs * kHeadDim);
     const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
     if (tiles * cache.Hkv > 0x7FFFFFFFll / 256 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
-    if (slots && tiles * cache.Hkv >= 2048) {
+    if (slots && tiles * cache.Hkv >= DET_KV8_WALK_TILES) {
         hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3((unsigned)((tiles + 3) / 4 * cache.Hkv)), dim3(256), 0, s, a);
         return check_launch();
     }
@@ -982,7 +983,7 @@ using namespace det;
 extern "C" size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages)
 {
     if (R < 1 || Hq < 1 || Hkv < 1 || D != kHeadDim || max_pages < 1 || max_pages > DET_KV8_MAX_PAGES || Hq % Hkv != 0) return 0;
-    return workspace_bytes(R, Hq, max_pages);
+    return attn_decode_kv8_workspace(R, Hq, max_pages);
 }
 
 extern "C" int det_attn_decode_kv8(const void* q, const void* pool, const int32_t* page_table, int n_pages, int n_slots, int max_pages,

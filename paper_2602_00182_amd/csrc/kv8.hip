@@ -1,6 +1,8 @@
 // Rows into and out of the 8-bit paged cache, and copies of its pages.
 #include "kv8.h"
 
+#include "geometry.h"
+
 namespace det {
 
 // The quantizer on 128 values that eight neighbouring lanes hold, sixteen each: d = max|v| / 127, codes clamp(rint(v / d)); a row that is not finite
@@ -116,7 +118,6 @@ __device__ __forceinline__ void append_values(const append_args& a, uint32_t blo
 // bounds a prompt is that chain and the bytes (rows in, queries and codes out).  TILED: the value heads in blocks of their own (append_values), from
 // item_blocks on.
 constexpr int kAppendTurns = 2;
-constexpr int kTiledRows = 128;  // rows of a call from which its value heads are stored in runs
 template <bool TILED>
 __global__ __launch_bounds__(256) void kv8_append_kernel(append_args a)
 {
@@ -257,7 +258,7 @@ extern "C" int det_kv8_rope_append(const void* qkv, int ldqkv, void* qbuf, void*
     if (ldqkv < (Hq + 2 * Hkv) * D) return DET_EINVAL;
     if (!aligned16(qkv) || !aligned16(qbuf) || !aligned16(rope_cos) || !aligned16(rope_sin) || ldqkv % 8) return DET_EALIGN;
     const kv8_cache c{static_cast<uint8_t*>(pool), page_table, n_pages, n_slots, max_pages, Hkv};
-    const bool tiled = R >= kTiledRows;
+    const bool tiled = R >= DET_KV8_RUN_ROWS;
     const long long items = (long long)R * (Hq + (tiled ? 1 : 2) * Hkv), per_block = 32 * kAppendTurns, item_blocks = (items + per_block - 1) / per_block;
     const long long blocks = item_blocks + (tiled ? (long long)((R + kValueRows - 1) / kValueRows) * Hkv : 0);
     if (items > 0x7FFFFFFFll || blocks > 0x7FFFFFFFll / 256) return DET_ESHAPE;
