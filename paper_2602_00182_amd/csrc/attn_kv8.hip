@@ -471,12 +471,12 @@ __global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_a
                 fold_step(fm, l, mc[r], lc, unit[r], fa, fb);
                 const float by = row_factor(l);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) a.out[head * kHeadDim + 32 * wave + 16 * n + col] = to_bf16(fold_value(0.0f, o[n], fa, fb) * by);
+                for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(to_bf16(fold_value(0.0f, o[n], fa, fb) * by), &a.out[head * kHeadDim + 32 * wave + 16 * n + col]);
             } else {
                 const size_t at = head * a.chunks + chunk;
                 if (wave == 0 && col == 0) a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) a.part_o[at * kHeadDim + 32 * wave + 16 * n + col] = o[n];
+                for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(o[n], &a.part_o[at * kHeadDim + 32 * wave + 16 * n + col]);
             }
         }
     }
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
         if (c0 + 2 * kFoldBlock < chunks) ask(x[0], c0 + 2 * kFoldBlock);
         fold(x[1], c0 + kFoldBlock);
     }
-    a.out[at * kHeadDim + threadIdx.x] = to_bf16(o * row_factor(l));
+    __builtin_nontemporal_store(to_bf16(o * row_factor(l)), &a.out[at * kHeadDim + threadIdx.x]);
 }
 
 // Scores to weights e d^V, in place, and what the fold needs of the chunk.  scales(p, dk, dv): those of this lane's tokens of page p.
@@ -577,7 +577,7 @@ __device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int
         uint16_t* out = a.out + ((size_t)(row0 + row) * a.Hq + kvh * a.G + p - row * a.G) * kHeadDim;
         const float by = row_factor(l[r]);
 #pragma unroll
-        for (int n = 0; n < 8; ++n) out[16 * n + col] = to_bf16(o[n][r] * by);
+        for (int n = 0; n < 8; ++n) __builtin_nontemporal_store(to_bf16(o[n][r] * by), &out[16 * n + col]);
     }
 }
 

@@ -24,6 +24,16 @@ struct kv8_cache {
     int n_pages, n_slots, max_pages, Hkv;
 };
 
+// Stores of results that this kernel does not read again, past the caches: a line that an XCD's cache holds changed is written back when the kernel ends,
+// and the kernel ends no sooner (copies of 16 pages in 8 layers 17.0 -> 5.6 us, of 400 pages 174 -> 167).
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+__device__ __forceinline__ void stream_store(void* to, const uint4& x)
+{
+    __builtin_nontemporal_store(u32x4{x.x, x.y, x.z, x.w}, static_cast<u32x4*>(to));
+}
+__device__ __forceinline__ void stream_store(void* to, const uint2& x) { __builtin_nontemporal_store(u32x2{x.x, x.y}, static_cast<u32x2*>(to)); }
+
 // Record of the page that holds position p of a slot (p within the table), or null where the slot is none or the table names no page.
 __device__ __forceinline__ uint8_t* kv8_record(const kv8_cache& c, int slot, int page_of_slot, int kvh)
 {

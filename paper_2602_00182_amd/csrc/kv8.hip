@@ -86,7 +86,7 @@ __device__ __forceinline__ void append_values(const append_args& a, uint32_t blo
         if ((next & ~15ull) != at) {
             uint8_t* dst = reinterpret_cast<uint8_t*>(at) + 16 * column;
             if (have == 0xFFFFu) {
-                *reinterpret_cast<uint4*>(dst) = make_uint4(piece[0], piece[1], piece[2], piece[3]);
+                stream_store(dst, make_uint4(piece[0], piece[1], piece[2], piece[3]));
             } else if (have != 0u) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(append_args a)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[k] = (__float_as_uint(v[2 * k]) >> 16) | (__float_as_uint(v[2 * k + 1]) & 0xFFFF0000u);
                 uint16_t* q = a.qbuf + ((size_t)row[u] * a.Hq + head[u]) * kHeadDim;
-                *reinterpret_cast<uint4*>(q + i0) = make_uint4(o[0], o[1], o[2], o[3]);
-                *reinterpret_cast<uint4*>(q + 64 + i0) = make_uint4(o[4], o[5], o[6], o[7]);
+                stream_store(q + i0, make_uint4(o[0], o[1], o[2], o[3]));
+                stream_store(q + 64 + i0, make_uint4(o[4], o[5], o[6], o[7]));
                 continue;
             }
         }
@@ -181,8 +181,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(append_args a)
         if (!rec) continue;
         const int t = pos[u] % kPage;
         if (!value) {
-            *reinterpret_cast<uint2*>(rec + t * kHeadDim + i0) = make_uint2(codes[0], codes[1]);
-            *reinterpret_cast<uint2*>(rec + t * kHeadDim + 64 + i0) = make_uint2(codes[2], codes[3]);
+            stream_store(rec + t * kHeadDim + i0, make_uint2(codes[0], codes[1]));
+            stream_store(rec + t * kHeadDim + 64 + i0, make_uint2(codes[2], codes[3]));
         } else {
             uint8_t* dst = rec + kRecordV + (t >> 4) * (16 * kHeadDim) + (t & 15) + 16 * i0;
 #pragma unroll
@@ -216,8 +216,8 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(kv8_cache c, const int32_
             o[4 + e] = pack_bf16x2((float)(int8_t)vp[32 * e] * dv, (float)(int8_t)vp[32 * e + 16] * dv);
         }
     }
-    k[at * 16 + i] = make_uint4(o[0], o[1], o[2], o[3]);
-    v[at * 16 + i] = make_uint4(o[4], o[5], o[6], o[7]);
+    stream_store(k + at * 16 + i, make_uint4(o[0], o[1], o[2], o[3]));
+    stream_store(v + at * 16 + i, make_uint4(o[4], o[5], o[6], o[7]));
 }
 
 // Pages src[i] -> dst[i] of every layer, 16 KB a workgroup.  Grid (pairs, pieces of a page, layers).
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void kv8_copy_kernel(uint4* __restrict__ pool,
     for (int k = 0; k < 4; ++k) x[k] = from[min(first + 256 * k, vectors - 1)];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        if (first + 256 * k < vectors) to[first + 256 * k] = x[k];
+        if (first + 256 * k < vectors) stream_store(to + first + 256 * k, x[k]);
 }
 
 }  // namespace det
