@@ -49,9 +49,9 @@ struct append_args {
     uint32_t items, item_blocks;
 };
 
-// V heads of 64 rows: their codes meet in LDS, and a thread puts sixteen tokens of one column side by side, as the record has them, so that a run of
-// neighbouring tokens is stored in pieces of sixteen bytes (3332 rows of 32/8 heads 30 -> 24 us against a byte at a time).
-constexpr int kValueRows = 64;
+// V heads of 32 rows: their codes meet in LDS, and a thread puts sixteen tokens of one column side by side, as the record has them, so that a run of
+// neighbouring tokens is stored in pieces of sixteen bytes (3332 rows of 32/8 heads 30 -> 20 us against a byte at a time and half as many heads a thread).
+constexpr int kValueRows = 32;
 __device__ __forceinline__ void append_values(const append_args& a, uint32_t block, uint8_t (&codes_of)[kValueRows][kHeadDim + 4],
                                               unsigned long long (&place)[kValueRows])
 {
@@ -114,13 +114,14 @@ __device__ __forceinline__ void append_values(const append_args& a, uint32_t blo
 
 // Heads of projection rows, eight lanes a (row, head): lane i holds the rotation pairs 8i..8i+7, i.e. columns 8i..8i+7 and 64+8i..64+8i+7.
 // Query heads are rotated into qbuf; key heads are rotated, rounded to bf16 and quantized, value heads quantized as they are.
-// Block (256): 32 heads at a time, kAppendTurns times, everything that can be asked for asked for first: the way is position, then its angles; what
-// bounds a prompt is that chain and the bytes (rows in, queries and codes out).  TILED: the value heads in blocks of their own (append_values), from
+// Block (256): 32 heads at a time, append_turns times (few rows once: they are all latency, 5.7 -> 4.6 us against twice), everything that can be asked
+// for asked for first: the way is position, then its angles; what bounds a prompt is that chain and the bytes (rows in, queries and codes out).  TILED: the value heads in blocks of their own (append_values), from
 // item_blocks on.
-constexpr int kAppendTurns = 2;
+constexpr int append_turns(bool tiled) { return tiled ? 4 : 1; }
 template <bool TILED>
 __global__ __launch_bounds__(256) void kv8_append_kernel(append_args a)
 {
+    constexpr int kAppendTurns = append_turns(TILED);
     const kv8_cache& c = a.c;
     if constexpr (TILED) {
         __shared__ uint8_t codes_of[kValueRows][kHeadDim + 4];
@@ -259,7 +260,7 @@ extern "C" int det_kv8_rope_append(const void* qkv, int ldqkv, void* qbuf, void*
     if (!aligned16(qkv) || !aligned16(qbuf) || !aligned16(rope_cos) || !aligned16(rope_sin) || ldqkv % 8) return DET_EALIGN;
     const kv8_cache c{static_cast<uint8_t*>(pool), page_table, n_pages, n_slots, max_pages, Hkv};
     const bool tiled = R >= DET_KV8_RUN_ROWS;
-    const long long items = (long long)R * (Hq + (tiled ? 1 : 2) * Hkv), per_block = 32 * kAppendTurns, item_blocks = (items + per_block - 1) / per_block;
+    const long long items = (long long)R * (Hq + (tiled ? 1 : 2) * Hkv), per_block = 32 * append_turns(tiled), item_blocks = (items + per_block - 1) / per_block;
     const long long blocks = item_blocks + (tiled ? (long long)((R + kValueRows - 1) / kValueRows) * Hkv : 0);
     if (items > 0x7FFFFFFFll || blocks > 0x7FFFFFFFll / 256) return DET_ESHAPE;
     const append_args a{static_cast<const uint16_t*>(qkv), static_cast<uint16_t*>(qbuf), c, positions, slots, rope_cos, rope_sin, ldqkv, Hq, Lrope, R,
