@@ -724,9 +724,11 @@ def kv8_pool(n_layers: int, n_pages: int, Hkv: int, D: int = 128, device="cuda")
 
 def _kv8(pool, page_table):
     """(pool, page_table, n_pages, n_slots, max_pages) of a call, and Hkv."""
-    if pool.dim() != 3 or pool.shape[2] != KV8_RECORD or page_table.dim() != 2:
-        raise ValueError("bad page pool or table")
-    return (_contig(pool, torch.uint8), _contig(page_table, torch.int32), pool.shape[0], page_table.shape[0], page_table.shape[1]), pool.shape[1]
+    n_pages, Hkv, record = pool.shape   # another number of dimensions raises ValueError here
+    n_slots, max_pages = page_table.shape
+    if record != KV8_RECORD:
+        raise ValueError("bad page pool")
+    return (_contig(pool, torch.uint8), _contig(page_table, torch.int32), n_pages, n_slots, max_pages), Hkv
 
 
 def _slots(slots, R: int, n_slots: int):
@@ -745,25 +747,25 @@ def det_kv8_rope_append(qkv, qbuf, pool, page_table, positions, slots, rope_cos,
     R, Hq, D = qbuf.shape
     cache, Hkv = _kv8(pool, page_table)
     n = (Hq + 2 * Hkv) * D
-    if qkv.shape != (R, n) or qkv.stride(1) != 1 or positions.shape != (R,):
+    table = Lrope, half = rope_cos.shape
+    if qkv.shape != (R, n) or positions.shape != (R,) or qkv.stride(1) != 1:
         raise ValueError("bad projection rows")
-    if rope_cos.dim() != 2 or rope_cos.shape[1] != D // 2 or rope_sin.shape != rope_cos.shape:
+    if half * 2 != D or rope_sin.shape != table:
         raise ValueError("bad rope tables")
     _check("det_kv8_rope_append", lib().det_kv8_rope_append(
         _ptr(qkv, torch.bfloat16), _ld(qkv, n), _contig(qbuf, torch.bfloat16), *cache, _contig(positions, torch.int32),
-        _slots(slots, R, page_table.shape[0]), _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), R, Hq, Hkv, D,
-        rope_cos.shape[0], _stream(stream)))
+        _slots(slots, R, cache[3]), _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), R, Hq, Hkv, D, Lrope, _stream(stream)))
 
 
 def det_kv8_read(pool, page_table, positions, slots, k, v, stream=None) -> None:
     """k, v [R, Hkv, 128] bf16: the cache's values at (slot, position); slots None: row r reads slot r."""
-    R, Hkv, D = k.shape
+    shape = R, Hkv, D = k.shape
     cache, heads = _kv8(pool, page_table)
-    if heads != Hkv or v.shape != k.shape or positions.shape != (R,):
+    if heads != Hkv or v.shape != shape or positions.shape != (R,):
         raise ValueError("bad cache rows")
     _check("det_kv8_read", lib().det_kv8_read(
-        *cache, _contig(positions, torch.int32), _slots(slots, R, page_table.shape[0]), _contig(k, torch.bfloat16),
-        _contig(v, torch.bfloat16), R, Hkv, D, _stream(stream)))
+        *cache, _contig(positions, torch.int32), _slots(slots, R, cache[3]), _contig(k, torch.bfloat16), _contig(v, torch.bfloat16), R, Hkv, D,
+        _stream(stream)))
 
 
 def det_kv8_copy_pages(pool, src, dst, stream=None) -> None:
@@ -782,13 +784,14 @@ def det_attn_decode_kv8_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_p
 
 def det_attn_decode_kv8(q, pool, page_table, seqlens, slots, out, ws, scale: float, stream=None) -> None:
     """out [R, Hq, 128] = attention of q over the first seqlens[r] tokens of slot slots[r] (None: slot r) of the 8-bit cache."""
-    R, Hq, D = q.shape
+    shape = R, Hq, D = q.shape
     cache, Hkv = _kv8(pool, page_table)
-    if out.shape != q.shape or seqlens.shape != (R,):
+    if out.shape != shape or seqlens.shape != (R,):
         raise ValueError("bad attention shapes")
+    bf16 = torch.bfloat16
     _check("det_attn_decode_kv8", lib().det_attn_decode_kv8(
-        _contig(q, torch.bfloat16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, page_table.shape[0]),
-        _contig(out, torch.bfloat16), _contig(ws), ws.numel() * ws.element_size(), R, Hq, Hkv, D, scale, _stream(stream)))
+        _contig(q, bf16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, cache[3]), _contig(out, bf16), _contig(ws), ws.nbytes, R, Hq,
+        Hkv, D, scale, _stream(stream)))
 
 
 def det_decoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
@@ -809,8 +812,8 @@ def det_decoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, p
     if rope_cos.shape != (cfg.Lmax, cfg.D // 2) or rope_sin.shape != rope_cos.shape:
         raise ValueError("bad layer shapes")
     _check(_entry, getattr(lib(), _entry)(
-        C.byref(w), C.byref(cfg), _contig(x, torch.bfloat16), *cache, _contig(positions, torch.int32), _slots(slots, R, page_table.shape[0]),
-        _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), _contig(ws), ws.numel() * ws.element_size(), R, _stream(stream)))
+        C.byref(w), C.byref(cfg), _contig(x, torch.bfloat16), *cache, _contig(positions, torch.int32), _slots(slots, R, cache[3]),
+        _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), _contig(ws), ws.nbytes, R, _stream(stream)))
 
 
 def det_qdecoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream=None) -> None:
