@@ -530,9 +530,10 @@ int det_qdecoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg,
  *   tokens[b] = x_0 .. x_{a-1}, the token, then -1.
  * q NULL: the drafts were certain (q = 1 at x_i, 0 elsewhere).
  *   p [B, N+1, V], q [B, N, V], u [B, N+1] fp32, u in [0, 1);  drafts [B, N], accepted [B], tokens [B, N+1] int32.  p, q 16-byte aligned.
- *   1 <= N <= 63. */
+ *   1 <= N <= 63, B <= 65535, V <= 2^30;  ws: det_verify_drafts_workspace_bytes(B, V) bytes, 16-byte aligned. */
+size_t det_verify_drafts_workspace_bytes(int B, int V);
 int det_verify_drafts(const float *p, const float *q, const int32_t *drafts, const int32_t *n_drafts, const float *u,
-                      int32_t *accepted, int32_t *tokens, int B, int N, int V, void *stream);
+                      int32_t *accepted, int32_t *tokens, void *ws, size_t ws_bytes, int B, int N, int V, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Output commitment (the paper's section 6.7 records SHA256(prompt || logits || tokens) for every

@@ -95,7 +95,8 @@ SIGNATURES = {
     "det_qdecoder_layer_kv8_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_qdecoder_layer_kv8": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
                                     _vp, _sz, _i, _vp]),
-    "det_verify_drafts": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
+    "det_verify_drafts_workspace_bytes": (_sz, [_i, _i]),
+    "det_verify_drafts": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _vp]),
     "det_sha256_init": (_i, [C.POINTER(Sha256Ctx)]),
     "det_sha256_update": (_i, [C.POINTER(Sha256Ctx), _vp, _sz]),
     "det_sha256_final": (_i, [C.POINTER(Sha256Ctx), _vp]),

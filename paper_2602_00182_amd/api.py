@@ -4,6 +4,7 @@ Tensors must live on the GPU and be contiguous where the C call says so; nothing
 converted here, and no arithmetic of the method happens in Python."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import torch
@@ -27,7 +28,7 @@ __all__ = [
     "det_qgemm_w4a8_swiglu_quant_supported", "det_qgemm_w4a8_swiglu_quant",
     "KV8_PAGE", "KV8_RECORD", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
     "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8", "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8",
-    "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts",
+    "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts_workspace_bytes", "det_verify_drafts",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -821,16 +822,25 @@ def det_qdecoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, 
     det_decoder_layer_kv8(w, cfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream, _entry="det_qdecoder_layer_kv8")
 
 
-def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, stream=None) -> None:
+def det_verify_drafts_workspace_bytes(B: int, V: int) -> int:
+    return lib().det_verify_drafts_workspace_bytes(B, V)
+
+
+def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, ws=None, stream=None) -> None:
     """Drafted tokens [B, N] against the target's probabilities p [B, N+1, V] and the draft's q [B, N, V] (None: the drafts were certain)
-    with the random numbers u [B, N+1]; n_drafts [B] or None (all N).  accepted [B]; tokens [B, N+1]: the accepted drafts, one more, -1."""
+    with the random numbers u [B, N+1]; n_drafts [B] or None (all N).  accepted [B]; tokens [B, N+1]: the accepted drafts, one more, -1.
+    ws: det_verify_drafts_workspace_bytes(B, V) bytes; None: allocated here (16 bytes for 2048 tokens of a sequence)."""
     B, N = drafts.shape
-    V = p.shape[-1]
-    if p.shape != (B, N + 1, V) or u.shape != (B, N + 1) or accepted.shape != (B,) or tokens.shape != (B, N + 1):
+    b, rows, V = p.shape
+    if (b, rows) != (B, N + 1) or u.shape != (B, N + 1) or accepted.shape != (B,) or tokens.shape != (B, N + 1):
         raise ValueError("bad verification shapes")
     if (q is not None and q.shape != (B, N, V)) or (n_drafts is not None and n_drafts.shape != (B,)):
         raise ValueError("bad verification shapes")
+    if ws is None:
+        # on the call's own stream, so that memory another stream still uses is not taken
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            ws = torch.empty(max(1, det_verify_drafts_workspace_bytes(B, V)), dtype=torch.uint8, device=p.device)
     _check("det_verify_drafts", lib().det_verify_drafts(
         _contig(p, torch.float32), None if q is None else _contig(q, torch.float32), _contig(drafts, torch.int32),
         None if n_drafts is None else _contig(n_drafts, torch.int32), _contig(u, torch.float32), _contig(accepted, torch.int32),
-        _contig(tokens, torch.int32), B, N, V, _stream(stream)))
+        _contig(tokens, torch.int32), _contig(ws), ws.nbytes, B, N, V, _stream(stream)))

@@ -3,11 +3,77 @@
 //
 // A product of two fp32 numbers is exact in fp64, so the acceptance is decided without rounding.  What is left, max(p - q, 0), and its sums are
 // held in fp64: a sum of 10^5 terms moves the borders between tokens by about 1e-16 of the total.
+//
+// Two launches: parts of 2048 tokens are summed by a workgroup each, then one workgroup a sequence finds the part that holds the target and reads it
+// again.  One workgroup for a whole row (one launch) is bound by what one compute unit can ask for: 64 sequences of 128000 tokens 36 us, 8 of them 33.
 #include "internal.h"
 
 namespace det {
 
-constexpr int kVerifyThreads = 1024, kVerifyWaves = kVerifyThreads / kWave, kVerifyDrafts = 64;
+constexpr int kVerifyDrafts = 64, kPartTokens = 2048, kRunTokens = kPartTokens / kBlock;
+
+struct verify_args {
+    const float* p;           // [B, N+1, V]
+    const float* q;           // [B, N, V] or null
+    const int32_t* drafts;    // [B, N]
+    const int32_t* n_drafts;  // [B] or null
+    const float* u;           // [B, N+1]
+    int32_t* accepted;
+    int32_t* tokens;
+    double2* parts;           // [B, n_parts]: the sums of max(p - q, 0) and of max(p, 0)
+    int N, V, n_parts;
+};
+
+// What a sequence's last token is drawn from: p_j - q_j (q null: p_j) where that is positive, else 0 (NaN too); nothing of token `barred`, which
+// is one only where q is null: without the draft's probabilities a rejected draft was certain.
+struct left_over {
+    const float* p;
+    const float* q;
+    int barred;
+    __device__ __forceinline__ double of(float pj, float qj, int j) const { return j == barred ? 0.0 : __builtin_fmax((double)pj - (double)qj, 0.0); }
+};
+
+// The number of accepted drafts (lane i of a wave decides draft i) and this lane's draft.
+__device__ __forceinline__ int accept_drafts(const verify_args& a, int b, int32_t& draft, left_over& left)
+{
+    const int lane = threadIdx.x & 63, n = min(max(a.n_drafts ? a.n_drafts[b] : a.N, 0), a.N);
+    bool ok = false;
+    draft = -1;
+    if (lane < n) {
+        draft = a.drafts[(size_t)b * a.N + lane];
+        if ((unsigned)draft < (unsigned)a.V) {
+            const double px = a.p[((size_t)b * (a.N + 1) + lane) * a.V + draft];
+            const double qx = a.q ? a.q[((size_t)b * a.N + lane) * a.V + draft] : 1.0;
+            ok = (double)a.u[(size_t)b * (a.N + 1) + lane] * qx < px;
+        }
+    }
+    const int take = __builtin_ctzll(~__ballot(ok) | (1ull << n));
+    left.p = a.p + ((size_t)b * (a.N + 1) + take) * a.V;
+    left.q = a.q && take < n ? a.q + ((size_t)b * a.N + take) * a.V : nullptr;
+    left.barred = !a.q && take < n ? __builtin_amdgcn_readlane(draft, take) : -1;
+    return take;
+}
+
+// Eight neighbouring tokens of a row from j on, zeros past V.  VEC: rows lie on 16 bytes.
+template <bool VEC>
+__device__ __forceinline__ void load_run(const float* row, int j, int V, float (&x)[kRunTokens])
+{
+    if (VEC && j + kRunTokens <= V) {
+        const float4 a = *reinterpret_cast<const float4*>(row + j), b = *reinterpret_cast<const float4*>(row + j + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < kRunTokens; ++k) x[k] = j + k < V ? row[j + k] : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void load_left(const left_over& left, int j, int V, float (&p)[kRunTokens], float (&q)[kRunTokens])
+{
+    load_run<VEC>(left.p, j, V, p);
+#pragma unroll
+    for (int k = 0; k < kRunTokens; ++k) q[k] = 0.0f;
+    if (left.q) load_run<VEC>(left.q, j, V, q);
+}
 
 __device__ __forceinline__ double wave_sum_f64(double v)
 {
@@ -16,166 +82,168 @@ __device__ __forceinline__ double wave_sum_f64(double v)
     return v;
 }
 
-// What the token is drawn from: p_j - q_j (q null: p_j) where that is positive, else 0 (NaN too); nothing of token `barred`.
-struct left_over {
-    const float* p;
-    const float* q;
-    int barred;
-    __device__ __forceinline__ double of(float pj, float qj, int j) const
-    {
-        const double d = (double)pj - (double)qj;
-        return d > 0.0 && j != barred ? d : 0.0;
-    }
-    __device__ __forceinline__ double operator()(int j) const { return of(p[j], q ? q[j] : 0.0f, j); }
-};
-
-// Sum over the tokens from..to-1 (VEC: rows lie on 16 bytes, `from` is a multiple of four), the same in every lane.  A lane asks for sixteen values
-// of either row before it uses the first.
+// Grid (parts, B).
 template <bool VEC>
-__device__ __forceinline__ double wave_sum(const left_over& left, int from, int to)
+__global__ __launch_bounds__(kBlock) void verify_parts_kernel(verify_args a)
 {
-    constexpr int W = VEC ? 4 : 1, AHEAD = VEC ? 4 : 16;
-    const int lane = threadIdx.x & 63;
-    double s = 0.0;
-    int j = from;
-    for (; j + 64 * W * AHEAD <= to; j += 64 * W * AHEAD) {
-        float p[AHEAD * W], q[AHEAD * W];
+    __shared__ double2 sums[kBlock / kWave];
+    const int b = blockIdx.y, j = blockIdx.x * kPartTokens + kRunTokens * (int)threadIdx.x;
+    int32_t draft;
+    left_over left;
+    accept_drafts(a, b, draft, left);
+    float p[kRunTokens], q[kRunTokens];
+    load_left<VEC>(left, j, a.V, p, q);
+    double s = 0.0, plain = 0.0;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int at = j + 64 * W * k + W * lane;
-            if constexpr (VEC) {
-                const float4 x = *reinterpret_cast<const float4*>(left.p + at);
-                const float4 y = left.q ? *reinterpret_cast<const float4*>(left.q + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                p[4 * k] = x.x, p[4 * k + 1] = x.y, p[4 * k + 2] = x.z, p[4 * k + 3] = x.w;
-                q[4 * k] = y.x, q[4 * k + 1] = y.y, q[4 * k + 2] = y.z, q[4 * k + 3] = y.w;
-            } else {
-                p[k] = left.p[at];
-                q[k] = left.q ? left.q[at] : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD * W; ++k) s = s + left.of(p[k], q[k], j + 64 * W * (k / W) + W * lane + k % W);
+    for (int k = 0; k < kRunTokens; ++k) {
+        s = s + left.of(p[k], q[k], j + k);
+        plain = plain + __builtin_fmax((double)p[k], 0.0);
     }
-    for (j += lane; j < to; j += 64) s = s + left(j);
-    return wave_sum_f64(s);
+    s = wave_sum_f64(s);
+    plain = wave_sum_f64(plain);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = make_double2(s, plain);
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.parts[(size_t)b * a.n_parts + blockIdx.x] = make_double2((sums[0].x + sums[1].x) + (sums[2].x + sums[3].x), (sums[0].y + sums[1].y) + (sums[2].y + sums[3].y));
 }
 
-// One workgroup a sequence.  Each wave sums a contiguous sixteenth of the row; the sixteenth that holds the target is cut into sixteenths again until
-// one wave can hold what is left.  Bound by how fast one compute unit reads two rows: where there are few sequences most of the chip idles, which a
-// second launch over parts of rows would cost more than it gives below some hundred thousand tokens.
-template <bool VEC>
-__global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const float* __restrict__ p, const float* __restrict__ q,
-                                                                const int32_t* __restrict__ drafts, const int32_t* __restrict__ n_drafts,
-                                                                const float* __restrict__ u, int32_t* __restrict__ accepted,
-                                                                int32_t* __restrict__ tokens, int N, int V)
+// The thread of the workgroup whose run holds the target: the first with before + (sums of the runs up to its own) > target, else the last whose run
+// is not empty, else thread 0.  start: the sum in front of the run of the calling thread.
+__device__ __forceinline__ int find_run(double mine, double before, double target, double& start, double (&wave_sums)[kBlock / kWave],
+                                        int (&firsts)[kBlock / kWave], int (&lasts)[kBlock / kWave])
 {
-    __shared__ double sums[2][kVerifyWaves];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n = min(max(n_drafts ? n_drafts[b] : N, 0), N);
-
-    // every wave decides the acceptance for itself: lane i has draft i
-    bool ok = false;
-    int32_t draft = -1;
-    if (lane < n) {
-        draft = drafts[(size_t)b * N + lane];
-        if ((unsigned)draft < (unsigned)V) {
-            const double px = p[((size_t)b * (N + 1) + lane) * V + draft];
-            const double qx = q ? q[((size_t)b * N + lane) * V + draft] : 1.0;
-            ok = (double)u[(size_t)b * (N + 1) + lane] * qx < px;
-        }
-    }
-    const int take = __builtin_ctzll(~__ballot(ok) | (1ull << n));
-    // without the draft's probabilities the drafted token was certain: it takes no part in the second draw
-    left_over left{p + ((size_t)b * (N + 1) + take) * V, q && take < n ? q + ((size_t)b * N + take) * V : nullptr,
-                   !q && take < n ? __builtin_amdgcn_readlane(draft, take) : -1};
-
-    // from..to-1 holds the target; before: the sum of what lies in front of it
-    int from = 0, to = V;
-    double before = 0.0, target = 0.0;
-    bool plain = false, first = true;
-    for (int level = 0;; ++level) {
-        if (!first && to - from <= 512) break;
-        const int part = ((to - from + kVerifyWaves - 1) / kVerifyWaves + 3) & ~3;
-        const int begin = min(from + wave * part, to);
-        const double s = wave_sum<VEC>(left, begin, min(begin + part, to));
-        double* mine = sums[level & 1];  // the other half is still read by waves that are behind
-        if (lane == 0) mine[wave] = s;
-        __syncthreads();
-        if (first) {
-            double total = 0.0;
-            for (int w = 0; w < kVerifyWaves; ++w) total = total + mine[w];
-            if (!(total > 0.0) && !plain) {  // nothing is left of p - q: the token comes from p itself
-                plain = true;
-                left.q = nullptr;
-                left.barred = -1;
-                continue;
-            }
-            target = (double)u[(size_t)b * (N + 1) + N] * total;
-            first = false;
-        }
-        // the first part whose end lies beyond the target, else the last that is not empty
-        int at = 0;
-        double start = before, sum = before;
-        for (int w = 0; w < kVerifyWaves; ++w) {
-            if (mine[w] > 0.0) {
-                at = w;
-                start = sum;
-            }
-            sum = sum + mine[w];
-            if (sum > target) break;
-        }
-        before = start;
-        from = min(from + at * part, to);
-        to = min(from + part, to);
-    }
-    if (wave != 0) return;
-
-    // a run of up to eight tokens a lane
-    const int run = (to - from + 63) / 64, mine = min(from + lane * run, to), end = min(mine + run, to);
-    double x[8], own = 0.0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        x[k] = mine + k < end ? left(mine + k) : 0.0;
-        own = own + x[k];
-    }
-    double c = own;  // sums of the lanes up to this one
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double up = mine;  // sums of the lanes up to this one
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
-        const double other = __shfl_up(c, off, kWave);
-        if (lane >= off) c = other + c;
+        const double other = __shfl_up(up, off, kWave);
+        if (lane >= off) up = other + up;
     }
-    c = before + (c - own);
-    int best = 0x7FFFFFFF, rest = -1;  // the lowest token whose end lies beyond the target; the highest that is not empty
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        c = c + x[k];
-        if (x[k] > 0.0) {
-            rest = mine + k;
-            if (c > target) best = min(best, mine + k);
+    __syncthreads();  // earlier readers are done
+    if (lane == kWave - 1) wave_sums[wave] = up;
+    __syncthreads();
+    double front = before;
+    for (int w = 0; w < wave; ++w) front = front + wave_sums[w];
+    start = front + (up - mine);
+    const unsigned long long past = __ballot(front + up > target), full = __ballot(mine > 0.0);
+    if (lane == 0) {
+        firsts[wave] = past ? 64 * wave + __builtin_ctzll(past) : -1;
+        lasts[wave] = full ? 64 * wave + 63 - __builtin_clzll(full) : -1;
+    }
+    __syncthreads();
+    int at = 0;
+    for (int w = 0; w < kBlock / kWave; ++w) at = lasts[w] >= 0 ? lasts[w] : at;
+    for (int w = kBlock / kWave - 1; w >= 0; --w) at = firsts[w] >= 0 ? firsts[w] : at;
+    return at;
+}
+
+// Grid (B).
+template <bool VEC>
+__global__ __launch_bounds__(kBlock) void verify_pick_kernel(verify_args a)
+{
+    __shared__ double wave_sums[kBlock / kWave], found_start;
+    __shared__ int firsts[kBlock / kWave], lasts[kBlock / kWave], found_part;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    int32_t draft;
+    left_over left;
+    const int take = accept_drafts(a, b, draft, left);
+
+    // a run of parts for each thread
+    const double2* parts = a.parts + (size_t)b * a.n_parts;
+    const int per = (a.n_parts + kBlock - 1) / kBlock, from = min(tid * per, a.n_parts), to = min(from + per, a.n_parts);
+    double s = 0.0, plain = 0.0;
+    for (int i = from; i < to; ++i) {
+        s = s + parts[i].x;
+        plain = plain + parts[i].y;
+    }
+    auto total_of = [&](double x) {
+        x = wave_sum_f64(x);
+        __syncthreads();
+        if (lane == 0) wave_sums[tid >> 6] = x;
+        __syncthreads();
+        return (wave_sums[0] + wave_sums[1]) + (wave_sums[2] + wave_sums[3]);
+    };
+    double total = total_of(s);
+    const bool from_p = !(total > 0.0);  // nothing is left of p - q: the token comes from p itself
+    if (from_p) {
+        total = total_of(plain);
+        s = plain;
+        left.q = nullptr;
+        left.barred = -1;
+    }
+    const double target = (double)a.u[(size_t)b * (a.N + 1) + a.N] * total;
+    double start;
+    if (tid == find_run(s, 0.0, target, start, wave_sums, firsts, lasts)) {
+        int part = from < a.n_parts ? from : 0;  // the first whose end lies beyond the target, else the last that is not empty
+        double c = start, front = start;
+        for (int i = from; i < to; ++i) {
+            const double x = from_p ? parts[i].y : parts[i].x;
+            if (x > 0.0) {
+                part = i;
+                front = c;
+            }
+            c = c + x;
+            if (c > target) break;
         }
+        found_part = part;
+        found_start = front;
     }
+    __syncthreads();
+
+    // eight tokens of it for each thread
+    const int j = found_part * kPartTokens + kRunTokens * tid;
+    float p[kRunTokens], q[kRunTokens];
+    load_left<VEC>(left, j, a.V, p, q);
+    double x[kRunTokens], mine = 0.0;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        best = min(best, __shfl_xor(best, off, kWave));
-        rest = max(rest, __shfl_xor(rest, off, kWave));
+    for (int k = 0; k < kRunTokens; ++k) {
+        x[k] = left.of(p[k], q[k], j + k);
+        mine = mine + x[k];
     }
-    const int token = best < 0x7FFFFFFF ? best : max(rest, 0);
-    if (lane == 0) accepted[b] = take;
-    if (lane <= N) tokens[(size_t)b * (N + 1) + lane] = lane < take ? draft : (lane == take ? token : -1);
+    if (tid == find_run(mine, found_start, target, start, wave_sums, firsts, lasts)) {
+        int token = -1;
+        double c = start;
+        bool past = false;
+#pragma unroll
+        for (int k = 0; k < kRunTokens; ++k) {
+            c = c + x[k];
+            if (x[k] > 0.0 && !past) {
+                token = j + k;
+                past = c > target;
+            }
+        }
+        a.tokens[(size_t)b * (a.N + 1) + take] = max(token, 0);
+        a.accepted[b] = take;
+    }
+    if (tid <= a.N && tid != take) a.tokens[(size_t)b * (a.N + 1) + tid] = tid < take ? draft : -1;
 }
 
 }  // namespace det
 
 using namespace det;
 
-extern "C" int det_verify_drafts(const float* p, const float* q, const int32_t* drafts, const int32_t* n_drafts, const float* u,
-                                 int32_t* accepted, int32_t* tokens, int B, int N, int V, void* stream)
+extern "C" size_t det_verify_drafts_workspace_bytes(int B, int V)
 {
-    if (!p || !drafts || !u || !accepted || !tokens || B < 1 || N < 1 || V < 1) return DET_EINVAL;
-    if (N >= kVerifyDrafts || V > (1 << 30)) return DET_ESHAPE;
-    if (!aligned16(p) || (q && !aligned16(q))) return DET_EALIGN;
+    if (B < 1 || V < 1 || V > (1 << 30)) return 0;
+    return (size_t)B * ((V + kPartTokens - 1) / kPartTokens) * sizeof(double2);
+}
+
+extern "C" int det_verify_drafts(const float* p, const float* q, const int32_t* drafts, const int32_t* n_drafts, const float* u,
+                                 int32_t* accepted, int32_t* tokens, void* ws, size_t ws_bytes, int B, int N, int V, void* stream)
+{
+    if (!p || !drafts || !u || !accepted || !tokens || !ws || B < 1 || N < 1 || V < 1) return DET_EINVAL;
+    if (N >= kVerifyDrafts || V > (1 << 30) || B > 65535) return DET_ESHAPE;
+    if (!aligned16(p) || (q && !aligned16(q)) || !aligned16(ws)) return DET_EALIGN;
+    if (ws_bytes < det_verify_drafts_workspace_bytes(B, V)) return DET_EWORKSPACE;
+    const verify_args a{p, q, drafts, n_drafts, u, accepted, tokens, static_cast<double2*>(ws), N, V, (V + kPartTokens - 1) / kPartTokens};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (V % 4 == 0) hipLaunchKernelGGL(verify_kernel<true>, dim3(B), dim3(kVerifyThreads), 0, s, p, q, drafts, n_drafts, u, accepted, tokens, N, V);
-    else hipLaunchKernelGGL(verify_kernel<false>, dim3(B), dim3(kVerifyThreads), 0, s, p, q, drafts, n_drafts, u, accepted, tokens, N, V);
+    const dim3 grid(a.n_parts, B);
+    if (V % 4 == 0) {
+        hipLaunchKernelGGL(verify_parts_kernel<true>, grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL(verify_pick_kernel<true>, dim3(B), dim3(kBlock), 0, s, a);
+    } else {
+        hipLaunchKernelGGL(verify_parts_kernel<false>, grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL(verify_pick_kernel<false>, dim3(B), dim3(kBlock), 0, s, a);
+    }
     return check_launch();
 }

@@ -341,12 +341,13 @@ def _speculative_decode(model, draft, prompts, prompt_lens, n_new, n_draft, unif
     drafts, drawn, none = torch.empty((B, N), **i32), torch.empty((B, 2), **i32), torch.zeros(B, **i32)
     accepted, tokens = torch.empty(B, **i32), torch.empty((B, N + 1), **i32)
     first = torch.empty((B, 2, V), **f32)
+    ws = torch.empty(api.det_verify_drafts_workspace_bytes(B, V), dtype=torch.uint8, device=dev)
 
     def draw(st, probabilities, u, out):
         """One token of each sequence from st.logits: a verification without drafts.  u [B, 2], the second is used."""
         api.det_softmax_f32(st.logits, width[:B], probabilities, sums[0, :B], sums[1, :B], stream)
         first[:, 0].copy_(probabilities)
-        api.det_verify_drafts(first, None, none[:, None], none, u, accepted, drawn, stream)
+        api.det_verify_drafts(first, None, none[:, None], none, u, accepted, drawn, ws, stream)
         out.copy_(drawn[:, 0])
 
     _fill_prompts(model, target, prompts, lens_host, stream)
@@ -371,7 +372,7 @@ def _speculative_decode(model, draft, prompts, prompt_lens, n_new, n_draft, unif
         rows.positions.copy_((at[:, None] + step_numbers).flatten())
         rows.forward(stream)
         api.det_softmax_f32(rows.logits, width, p.view(B * (N + 1), V), sums[0], sums[1], stream)
-        api.det_verify_drafts(p, q.transpose(0, 1).contiguous(), drafts, None, uniforms(turn, (B, N + 1)), accepted, tokens, stream)
+        api.det_verify_drafts(p, q.transpose(0, 1).contiguous(), drafts, None, uniforms(turn, (B, N + 1)), accepted, tokens, ws, stream)
         host, took = tokens.cpu(), accepted.cpu()
         counts.append(took)
         on = [len(m) < n_new for m in made]

@@ -36,13 +36,10 @@ class KVPages:
         """The pages of a slot, in order."""
         return list(self._pages[slot])
 
-    def _copy(self, pairs, stream) -> None:
+    def _copy(self, pairs, stream) -> None:  # with `stream` the current one: the pairs' tensors live in its memory
         if pairs:
             src, dst = (torch.tensor(x, dtype=torch.int32).to(self.pool.device) for x in zip(*pairs))
             api.det_kv8_copy_pages(self.pool, src, dst, stream)
-            if stream is not None:  # the pairs may be freed by the host before the stream has read them
-                src.record_stream(stream)
-                dst.record_stream(stream)
 
     def _write_table(self) -> None:
         for slot, pages in enumerate(self._pages):

@@ -18,7 +18,7 @@ READ = dict(pool=P, table=P, n_pages=4, n_slots=2, max_pages=2, positions=P, slo
 COPY = dict(pool=P, n_layers=1, n_pages=4, Hkv=2, D=128, src=P, dst=P, n=1, stream=0)
 ATTN = dict(q=P, pool=P, table=P, n_pages=4, n_slots=2, max_pages=2, seqlens=P, slots=0, out=P, ws=P, ws_bytes=1 << 40, R=1, Hq=4, Hkv=2, D=128,
             scale=0.1, stream=0)
-VERIFY = dict(p=P, q=P, drafts=P, n_drafts=P, u=P, accepted=P, tokens=P, B=1, N=2, V=100, stream=0)
+VERIFY = dict(p=P, q=P, drafts=P, n_drafts=P, u=P, accepted=P, tokens=P, ws=P, ws_bytes=1 << 40, B=1, N=2, V=100, stream=0)
 
 CASES = [("det_kv8_rope_append", APPEND, change, code) for change, code in [
     (dict(qkv=0), EINVAL), (dict(qbuf=0), EINVAL), (dict(pool=0), EINVAL), (dict(table=0), EINVAL), (dict(positions=0), EINVAL), (dict(cos=0), EINVAL),
@@ -39,7 +39,8 @@ CASES += [("det_attn_decode_kv8", ATTN, change, code) for change, code in [
     (dict(ws=P + 8), EALIGN), (dict(ws_bytes=0), EWORKSPACE)]]
 CASES += [("det_verify_drafts", VERIFY, change, code) for change, code in [
     (dict(p=0), EINVAL), (dict(drafts=0), EINVAL), (dict(u=0), EINVAL), (dict(accepted=0), EINVAL), (dict(tokens=0), EINVAL), (dict(B=0), EINVAL),
-    (dict(N=0), EINVAL), (dict(V=0), EINVAL), (dict(N=64), ESHAPE), (dict(V=(1 << 30) + 1), ESHAPE), (dict(p=P + 4), EALIGN), (dict(q=P + 4), EALIGN)]]
+    (dict(N=0), EINVAL), (dict(V=0), EINVAL), (dict(N=64), ESHAPE), (dict(V=(1 << 30) + 1), ESHAPE), (dict(B=65536), ESHAPE),
+    (dict(ws=0), EINVAL), (dict(ws=P + 8), EALIGN), (dict(ws_bytes=15), EWORKSPACE), (dict(p=P + 4), EALIGN), (dict(q=P + 4), EALIGN)]]
 
 
 @pytest.mark.parametrize("name,args,change,code", CASES, ids=lambda x: str(x) if isinstance(x, dict) and len(x) == 1 else "")
@@ -53,6 +54,7 @@ POINTERS = {"qkv", "qbuf", "pool", "table", "positions", "slots", "cos", "sin", 
 
 
 def test_sizes():
+    assert d.det_verify_drafts_workspace_bytes(3, 2049) == 3 * 2 * 16 and d.det_verify_drafts_workspace_bytes(1, 0) == 0
     assert d.det_kv8_pool_bytes(10, 8) == 10 * 8 * d.KV8_RECORD
     assert d.det_kv8_pool_bytes(0, 8) == 0 and d.det_kv8_pool_bytes(1, 8, 64) == 0
     assert d.det_attn_decode_kv8_workspace_bytes(1, 32, 8, 64, 4) == 0
