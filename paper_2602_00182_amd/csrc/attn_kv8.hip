@@ -31,7 +31,7 @@ struct kv8_attn_args {
     uint16_t* out;  // [R, Hq, 128]
     float* part_o;  // [R, Hq, chunks, 128]: a chunk's weighted sums, in units of its 2^(E-22)
     float4* part;   // [R, Hq, chunks]: its m, l, 2^(E-22)
-    int R, Hq, G, rows_per_tile, len_offset, chunks, inverse_G;
+    int R, Hq, G, rows_per_tile, len_offset, chunks, chunk_step, inverse_G;
     float scale_log2;  // scale * log2(e)
 };
 
@@ -279,8 +279,9 @@ __device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, 
 // ---------------------------------------------------------------- a chunk by four waves
 
 // One chunk for a tile of up to sixteen (row, head) pairs that read one KV head.  Rows of a tile may name different slots: those that name the
-// same one go through it together, one slot after the other.  Grid (KV heads x chunks, tiles): neighbouring workgroups read
-// one page's records, which lie side by side (16 rows of up to 32768 tokens 200 -> 190 us against tiles in front of chunks).
+// same one go through it together, one slot after the other.  Grid (KV heads x chunk_step, tiles): neighbouring workgroups read
+// one page's records, which lie side by side (16 rows of up to 32768 tokens 200 -> 190 us against tiles in front of chunks).  A workgroup takes every
+// chunk_step-th chunk: a table much wider than its sequences are long costs no workgroups that find nothing.
 //
 // For the scores a wave takes one of the four pages; the digits of the weights meet in LDS, and for the weighted sums it takes 32 of the 128 columns of
 // all four, so that no sums have to be joined and few are held.  All of a wave's loads (8 KB of K, 8 KB of V) are asked for before the first
@@ -289,7 +290,7 @@ __device__ __forceinline__ v4i load_digits(const uint8_t* digits, int g, int p, 
 // PACK: up to four pairs (one row of up to four heads a KV head).  Their digits fill the sixteen rows of one operand, row 4 pair + digit, so a
 // product is one instruction instead of three and a lane has all digits of one pair: a quarter of the scores' arithmetic.
 template <bool PACK>
-__global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
+__global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_attn_args a)
 {
     constexpr int NP = PACK ? 1 : 4;                 // pairs of a lane
     constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
@@ -297,30 +298,48 @@ __global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_a
     __shared__ float top[2][4][PAIRS];               // largest score, largest weight of each wave
     __shared__ float lsum[4][PAIRS][16];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
-    const int kvh = blockIdx.x % a.c.Hkv, chunk = blockIdx.x / a.c.Hkv, row0 = blockIdx.y * a.rows_per_tile;
+    const int kvh = blockIdx.x % a.c.Hkv, first_chunk = blockIdx.x / a.c.Hkv, row0 = blockIdx.y * a.rows_per_tile;
     // pair number `col` of the tile
     const bool live = col < a.rows_per_tile * a.G && row0 + pair_row(a, col) < a.R;
     int slot = -1, len = 0;
     if (live) len = row_length(a, row0 + pair_row(a, col), slot);
     // chunk 0 also answers for rows that see nothing
-    if (chunk == 0) {
+    if (first_chunk == 0) {
         for (int p = wave; p < a.rows_per_tile * a.G; p += 4) {
             const int r = pair_row(a, p);
             if (row0 + r < a.R && __builtin_amdgcn_readlane(len, p) == 0)
                 reinterpret_cast<uint32_t*>(a.out + ((size_t)(row0 + r) * a.Hq + kvh * a.G + p - r * a.G) * kHeadDim)[lane] = 0u;
         }
     }
-    unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
-    if (todo == 0) return;
+    if (__ballot(len > first_chunk * kChunk) == 0) return;
 
     const int qp = PACK ? col >> 2 : col, qrow = pair_row(a, qp);  // the pair of this lane's operand row
     uint32_t words[16];
     ask_query(qp < a.rows_per_tile * a.G && row0 + qrow < a.R ? a.q + ((size_t)(row0 + qrow) * a.Hq + kvh * a.G + qp - qrow * a.G) * kHeadDim : nullptr, words);
     q_digits qd[2];
     float factors[NP];
+    auto cut = [&] {
+        float factor;
+        cut_query(words, a.scale_log2, qd, factor);
+#pragma unroll
+        for (int r = 0; r < NP; ++r) factors[r] = __shfl(factor, PACK ? 4 * group : 4 * group + r, kWave);
+        if constexpr (PACK) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int dg = col & 3;
+                    qd[h].d[0][i] = dg == 0 ? qd[h].d[0][i] : dg == 1 ? qd[h].d[1][i] : dg == 2 ? qd[h].d[2][i] : 0;
+                }
+        }
+    };
+    if constexpr (!PACK) cut();
     const v4i zero = {0, 0, 0, 0};
     const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col + 512 * wave;
     bool first = true;
+    for (int chunk = first_chunk;; chunk += a.chunk_step) {
+    unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
+    if (todo == 0) return;
     while (todo != 0) {
         const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
         const int mine = slot == now ? len : 0;
@@ -342,7 +361,7 @@ __global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_a
             keys = p == wave ? at : keys;
             rec[p] = at ? at : a.c.pool;
         }
-        if (!PACK && !first) __syncthreads();  // the last slot's digits have been read
+        if (!first) __syncthreads();  // the last slot's digits have been read
 
         v4i kc[4][2], vc[kChunkPages][2];
         float dk[4], dv[4] = {};
@@ -358,21 +377,7 @@ __global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_a
 #pragma unroll
             for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
         __builtin_amdgcn_sched_barrier(0);
-        if (PACK || first) {  // while they are on their way
-            float factor;
-            cut_query(words, a.scale_log2, qd, factor);
-#pragma unroll
-            for (int r = 0; r < NP; ++r) factors[r] = __shfl(factor, PACK ? 4 * group : 4 * group + r, kWave);
-            if constexpr (PACK) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int dg = col & 3;
-                        qd[h].d[0][i] = dg == 0 ? qd[h].d[0][i] : dg == 1 ? qd[h].d[1][i] : dg == 2 ? qd[h].d[2][i] : 0;
-                    }
-            }
-        }
+        if (PACK && first) cut();  // while they are on their way
         first = false;
         float s[4][NP];
         if (keys) {
@@ -479,6 +484,7 @@ __global__ __launch_bounds__(256, PACK ? 4 : 2) void kv8_attn_chunk_kernel(kv8_a
                 for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(o[n], &a.part_o[at * kHeadDim + 32 * wave + 16 * n + col]);
             }
         }
+    }
     }
 }
 
@@ -968,8 +974,10 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3((unsigned)((tiles + 3) / 4 * cache.Hkv)), dim3(256), 0, s, a);
         return check_launch();
     }
-    if (tiles > 65535 || (long long)a.chunks * cache.Hkv > 0x7FFFFFFFll / 256) return DET_ESHAPE;
-    const dim3 grid((unsigned)(a.chunks * cache.Hkv), (unsigned)tiles);
+    if (tiles > 65535) return DET_ESHAPE;
+    const long long room = DET_KV8_CHUNK_WGS / (tiles * cache.Hkv);
+    a.chunk_step = room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
+    const dim3 grid((unsigned)(a.chunk_step * cache.Hkv), (unsigned)tiles);
     if (packed) hipLaunchKernelGGL(kv8_attn_chunk_kernel<true>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(kv8_attn_chunk_kernel<false>, grid, dim3(256), 0, s, a);
     if (a.chunks > 1) hipLaunchKernelGGL(kv8_attn_combine_kernel, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);

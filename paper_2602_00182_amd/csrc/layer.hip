@@ -231,8 +231,9 @@ static int kv8_layer_check(const det_layer_weights* w, const det_layer_cfg* cfg,
     if (!layer_cfg_ok(cfg)) return DET_ESHAPE;
     const int rc = kv8_check(pool, table, n_pages, n_slots, max_pages, cfg->Hkv, cfg->D);
     if (rc != DET_OK) return rc;
-    if (!slots && n_slots < R) return DET_ESHAPE;
-    if (!aligned16(ws) || !aligned16(x)) return DET_EALIGN;
+    if (cfg->Hq / cfg->Hkv > 16 || (!slots && (n_slots < R || R > 65535))) return DET_ESHAPE;
+    if (!(cfg->scale > 0.0f) || !(cfg->scale < __builtin_inff())) return DET_EINVAL;
+    if (!aligned16(ws) || !aligned16(x) || !aligned16(rope_cos) || !aligned16(rope_sin)) return DET_EALIGN;
     return DET_OK;
 }
 

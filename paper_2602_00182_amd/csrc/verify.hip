@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kBlock) void verify_parts_kernel(verify_args a)
         a.parts[(size_t)b * a.n_parts + blockIdx.x] = make_double2((sums[0].x + sums[1].x) + (sums[2].x + sums[3].x), (sums[0].y + sums[1].y) + (sums[2].y + sums[3].y));
 }
 
-// The thread of the workgroup whose run holds the target: the first with before + (sums of the runs up to its own) > target, else the last whose run
+// The thread of the workgroup whose run holds the target: the first that is not empty with before + (sums of the runs up to its own) > target, else the last whose run
 // is not empty, else thread 0.  start: the sum in front of the run of the calling thread.
 __device__ __forceinline__ int find_run(double mine, double before, double target, double& start, double (&wave_sums)[kBlock / kWave],
                                         int (&firsts)[kBlock / kWave], int (&lasts)[kBlock / kWave])
@@ -125,7 +125,8 @@ __device__ __forceinline__ int find_run(double mine, double before, double targe
     double front = before;
     for (int w = 0; w < wave; ++w) front = front + wave_sums[w];
     start = front + (up - mine);
-    const unsigned long long past = __ballot(front + up > target), full = __ballot(mine > 0.0);
+    // (an empty run is never taken: sums that take another way through the scan may differ in their last bit)
+    const unsigned long long past = __ballot(front + up > target && mine > 0.0), full = __ballot(mine > 0.0);
     if (lane == 0) {
         firsts[wave] = past ? 64 * wave + __builtin_ctzll(past) : -1;
         lasts[wave] = full ? 64 * wave + 63 - __builtin_clzll(full) : -1;
@@ -178,10 +179,9 @@ __global__ __launch_bounds__(kBlock) void verify_pick_kernel(verify_args a)
         double c = start, front = start;
         for (int i = from; i < to; ++i) {
             const double x = from_p ? parts[i].y : parts[i].x;
-            if (x > 0.0) {
-                part = i;
-                front = c;
-            }
+            if (!(x > 0.0)) continue;
+            part = i;
+            front = c;
             c = c + x;
             if (c > target) break;
         }

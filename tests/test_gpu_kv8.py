@@ -294,6 +294,29 @@ def test_many_rows_of_many_slots_in_no_order(d):
         assert np.array_equal(down_bf16(one)[0], got[r]), r
 
 
+@pytest.mark.parametrize("R,Hq,Hkv,named", [(600, 32, 8, False), (600, 64, 8, False), (1400, 16, 16, True)])
+def test_workgroups_that_take_several_chunks(d, R, Hq, Hkv, named):
+    """So many rows that a workgroup goes on from chunk to chunk, in a table much wider than the sequences are long; slots that share pages."""
+    lengths = [1500, 40, 1290, 700]
+    cache = Cache(7347, lengths, Hkv)
+    rng = np.random.default_rng(R + Hq)
+    slots = np.sort(rng.integers(0, 4, R)).astype(np.int32) if named else (np.arange(R) % 4).astype(np.int32)
+    lens = np.array([rng.integers(0, lengths[s] + 1) for s in slots], dtype=np.int32)
+    wide = np.full((4 if named else R, 500), -1, dtype=np.int32)
+    for s in range(wide.shape[0]):
+        wide[s, :cache.table.shape[1]] = cache.table[s % 4]
+    q = ds.normal_bf16(7348, (R, Hq, D), 1.5)
+    step(f"{R} rows, {Hq}/{Hkv} heads, a table of 500 pages")
+    pool, qd = up(cache.pool), up_bf16(q)
+    got = down_bf16(attn(d, qd, pool, up(wide), up(lens), up(slots) if named else None))
+    pick = list(range(0, R, 61)) + [R - 1]
+    ref, tol = attend(cache, q[pick], lens[pick], slots[pick])
+    assert (np.abs(bits_to_f64(got[pick]) - ref) <= tol).all()
+    for r in pick:
+        one = attn(d, qd[r:r + 1], pool, up(cache.table), up(lens[r:r + 1]), up(slots[r:r + 1]))
+        assert np.array_equal(down_bf16(one)[0], got[r]), r
+
+
 def test_extreme_scores_and_values(d):
     """One weight that is all (scores in the hundreds), equal scores, values of very different sizes, zero queries and zero keys."""
     def edit(k, v):

@@ -131,6 +131,22 @@ def test_rows_with_nothing_left_and_rows_that_are_no_probabilities(d):
     check(d, p, None, drafts, n, u, "odd rows, certain drafts")
 
 
+def test_many_parts_and_few_tokens_that_count(d):
+    """Rows of several hundred parts in which nearly all tokens weigh nothing: whatever the target, a token that weighs something is drawn."""
+    rng = np.random.default_rng(9)
+    B, V = 40, 700001
+    p = np.zeros((B, 2, V), np.float32)
+    for b in range(B):
+        at = rng.integers(0, V, 3)
+        p[b, :, at] = rng.random((3, 1), dtype=np.float32) + np.float32(1e-3)
+    q = np.zeros((B, 1, V), np.float32)
+    drafts = rng.integers(0, V, (B, 1)).astype(np.int32)
+    u = rng.random((B, 2), dtype=np.float32)
+    u[:4, 1] = [0.0, 1 - 2.0 ** -24, 0.5, 1e-30]
+    want = check(d, p, q, drafts, None, u, "few tokens that count")
+    assert all(p[b, 0, want[1][b, 0]] > 0 for b in range(B) if want[0][b] == 0)
+
+
 def test_graph_replays(d):
     rng = np.random.default_rng(8)
     B, N, V = 3, 3, 32000
