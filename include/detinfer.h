@@ -458,7 +458,8 @@ int det_qdecoder_layer(const det_layer_weights *w, const det_layer_cfg *cfg, voi
  * A pool is [n_pages, Hkv] records of DET_KV8_RECORD bytes; a record holds DET_KV8_PAGE = 64 tokens of one KV head of D = 128:
  *     K codes [64][128] int8,  V codes [4][128][16] int8 (token 16 g + i, column d at [g][d][i]),  K scales [64] fp32,  V scales [64] fp32.
  * The scale's block is one token of one KV head:  amax = max|x|;  d = amax / 127 (fp32);  code = clamp(rint(x / d), -127, 127), 0 if
- * d == 0;  value = code * d.  A row with an infinity or NaN has codes 0 and the scale NaN.  page_table [n_slots, max_pages] int32 names the
+ * d == 0;  value = code * d.  A row with an infinity or NaN has codes 0 and the scale NaN.  Scales are what the append writes: NaN or from 0 to 2^90 (a
+ * key beyond that may overflow a score), never negative.  page_table [n_slots, max_pages] int32 names the
  * page of tokens 64 i .. 64 i + 63 of a slot; an entry outside 0..n_pages-1 names none.  Pages may be shared between slots and may be
  * anywhere; what lies in them past a row's length is never used.
  *   Shapes: D == 128, max_pages <= DET_KV8_MAX_PAGES; pool 16-byte aligned. */
@@ -492,11 +493,13 @@ int det_kv8_copy_pages(void *pool, int n_layers, int n_pages, int Hkv, int D, co
  * 0..64 max_pages) of slot slots[r] (NULL: slot r; a slot outside 0..n_slots-1 has no tokens).  Tokens without a page are left out; a row
  * without any token gives zeros.  Several rows may share a slot (a prompt's rows at lengths 1..T, the rows of drafted tokens).
  *   s_j = scale * (q . c_j) d^K_j,   out = bf16( sum_j p_j d^V_j c^V_j ),   p = softmax(s).
- * The order: q's (row, head) as integers n_d = rint(q_d 2^(22-E)), 2^E the power of two above its largest magnitude; n . c_j exact, brought to
+ * The order: q's (row, head) as integers n_d = rint(q_d 2^(22-E)), 2^E the power of two above its largest magnitude (E >= -100); n . c_j exact, brought to
  * fp32 from its digits to base 256.  Chunk c = tokens [256 c, 256 c + 256): in units of log2, m_c = ceil(max s_j), e_j = 2^(s_j - m_c) by the
  * hardware's exponential, l_c their sum in a fixed order; weights e_j d^V_j as integers rint(w 2^(22-E_c)), 2^E_c above the chunk's largest;
  * their products with the codes exact.  Chunks are folded in ascending order, relative to the largest m so far.  A row's bytes do not depend
  * on R, on the other rows, on the pages it lies in or on the call's max_pages.
+ * Up to 2047 (tile, KV head) pairs, a tile being 16 / (Hq/Hkv) rows, and wherever slots is NULL, chunks go to workgroups of their own and meet in ws in a
+ * second launch; beyond, a tile of rows that name slots walks its chunks in one launch.  Rows that name slots are best given slot by slot.
  *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  scale > 0 and finite;  R <= 65535 if slots is NULL;  ws: det_attn_decode_kv8_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
 int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,

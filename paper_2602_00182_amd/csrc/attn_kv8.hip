@@ -8,6 +8,10 @@
 //            the cache holds to half a code only.
 // Softmax: a chunk's reference m_c is an integer (the ceiling of its largest score in units of log2), so the factors by which chunks are
 // brought together are powers of two.  Chunks are folded in ascending order.
+//
+// Three forms, the same bytes: a row (or a tile of rows that name slots) a chunk at a time by four waves with the chunks' sums in memory and a second launch;
+// calls of DET_KV8_WALK_TILES tiles and more, where the tiles alone fill the chip, walk their chunks in one launch.  (Below that line most of the
+// chip would idle behind long rows: one of 64 rows and 8000 tokens has 128 tiles, a chunk each takes 66 us.)
 #include <type_traits>
 
 #include "geometry.h"
