@@ -4,7 +4,6 @@ Tensors must live on the GPU and be contiguous where the C call says so; nothing
 converted here, and no arithmetic of the method happens in Python."""
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 
 import torch
@@ -55,10 +54,14 @@ def _ptr(t: torch.Tensor, dtype=None) -> int:
     return t.data_ptr()
 
 
-def _contig(t: torch.Tensor, dtype=None) -> int:
+def _contig(t: torch.Tensor, dtype=None) -> int:  # _ptr again instead of a call of it: a call of the library takes some nine of these
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    return _ptr(t, dtype)
+    if not t.is_cuda:
+        raise ValueError("libdetinfer takes device tensors")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
 def _stream(stream) -> int:
@@ -837,9 +840,12 @@ def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, ws=None, stre
     if (q is not None and q.shape != (B, N, V)) or (n_drafts is not None and n_drafts.shape != (B,)):
         raise ValueError("bad verification shapes")
     if ws is None:
-        # on the call's own stream, so that memory another stream still uses is not taken
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            ws = torch.empty(max(1, det_verify_drafts_workspace_bytes(B, V)), dtype=torch.uint8, device=p.device)
+        size = max(4, det_verify_drafts_workspace_bytes(B, V)) // 4
+        if stream is None:
+            ws = p.new_empty(size)
+        else:  # on the call's own stream, so that memory another stream still uses is not taken
+            with torch.cuda.stream(stream):
+                ws = p.new_empty(size)
     _check("det_verify_drafts", lib().det_verify_drafts(
         _contig(p, torch.float32), None if q is None else _contig(q, torch.float32), _contig(drafts, torch.int32),
         None if n_drafts is None else _contig(n_drafts, torch.int32), _contig(u, torch.float32), _contig(accepted, torch.int32),
