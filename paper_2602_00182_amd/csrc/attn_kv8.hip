@@ -342,153 +342,153 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
     const uint32_t key_at = 512 * col + 16 * group, value_at = kRecordV + 2048 * group + 16 * col + 512 * wave;
     bool first = true;
     for (int chunk = first_chunk;; chunk += a.chunk_step) {
-    unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
-    if (todo == 0) return;
-    while (todo != 0) {
-        const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
-        const int mine = slot == now ? len : 0;
-        const unsigned members = (unsigned)(__ballot(mine > chunk * kChunk) & 0xFFFFull);
-        todo = PACK ? 0u : todo & ~members;  // PACK: one row, one slot
-        int longest = mine;
+        unsigned todo = (unsigned)(__ballot(len > chunk * kChunk) & 0xFFFFull);
+        if (todo == 0) return;
+        while (todo != 0) {
+            const int now = __builtin_amdgcn_readlane(slot, __builtin_ctz(todo));
+            const int mine = slot == now ? len : 0;
+            const unsigned members = (unsigned)(__ballot(mine > chunk * kChunk) & 0xFFFFull);
+            todo = PACK ? 0u : todo & ~members;  // PACK: one row, one slot
+            int longest = mine;
 #pragma unroll
-        for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
-        longest = __builtin_amdgcn_readfirstlane(longest);
-        int lens[NP];
+            for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+            longest = __builtin_amdgcn_readfirstlane(longest);
+            int lens[NP];
 #pragma unroll
-        for (int r = 0; r < NP; ++r) lens[r] = __shfl(mine, PACK ? group : 4 * group + r, kWave);
-        // the chunk's pages; where one is missing, any record (its tokens weigh nothing)
-        const uint8_t *rec[kChunkPages], *keys = nullptr;
+            for (int r = 0; r < NP; ++r) lens[r] = __shfl(mine, PACK ? group : 4 * group + r, kWave);
+            // the chunk's pages; where one is missing, any record (its tokens weigh nothing)
+            const uint8_t *rec[kChunkPages], *keys = nullptr;
 #pragma unroll
-        for (int p = 0; p < kChunkPages; ++p) {
-            const int page = chunk * kChunkPages + p;
-            const uint8_t* at = page * kPage < longest ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
-            keys = p == wave ? at : keys;
-            rec[p] = at ? at : a.c.pool;
-        }
-        if (!first) __syncthreads();  // the last slot's digits have been read
+            for (int p = 0; p < kChunkPages; ++p) {
+                const int page = chunk * kChunkPages + p;
+                const uint8_t* at = page * kPage < longest ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
+                keys = p == wave ? at : keys;
+                rec[p] = at ? at : a.c.pool;
+            }
+            if (!first) __syncthreads();  // the last slot's digits have been read
 
-        v4i kc[4][2], vc[kChunkPages][2];
-        float dk[4], dv[4] = {};
-        if (keys) {
-            ask_scales(keys + kRecordKs, col, dk, dv);
+            v4i kc[4][2], vc[kChunkPages][2];
+            float dk[4], dv[4] = {};
+            if (keys) {
+                ask_scales(keys + kRecordKs, col, dk, dv);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) kc[t][h] = load16(keys, key_at, t * kHeadDim + 64 * h);
-        }
+                    for (int h = 0; h < 2; ++h) kc[t][h] = load16(keys, key_at, t * kHeadDim + 64 * h);
+            }
 #pragma unroll
-        for (int p = 0; p < kChunkPages; ++p)
+            for (int p = 0; p < kChunkPages; ++p)
 #pragma unroll
-            for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
-        __builtin_amdgcn_sched_barrier(0);
-        if (PACK && first) cut();  // while they are on their way
-        first = false;
-        float s[4][NP];
-        if (keys) {
-            clean_scales(dk, dv);
+                for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
+            __builtin_amdgcn_sched_barrier(0);
+            if (PACK && first) cut();  // while they are on their way
+            first = false;
+            float s[4][NP];
+            if (keys) {
+                clean_scales(dk, dv);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                v4i d[DIGITS];
+                for (int t = 0; t < 4; ++t) {
+                    v4i d[DIGITS];
 #pragma unroll
-                for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
+                    for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[0].d[g], kc[t][0], zero, 0, 0, 0);
 #pragma unroll
-                for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
-                const int token = (chunk * kChunkPages + wave) * kPage + 4 * col + t;
+                    for (int g = 0; g < DIGITS; ++g) d[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[1].d[g], kc[t][1], d[g], 0, 0, 0);
+                    const int token = (chunk * kChunkPages + wave) * kPage + 4 * col + t;
 #pragma unroll
-                for (int r = 0; r < NP; ++r) {
-                    float x;
-                    if constexpr (PACK) x = score_of(d[0][0], d[0][1], d[0][2], dk[t]);
-                    else x = score_of(d[0][r], d[1][r], d[2][r], dk[t]);
-                    s[t][r] = token < lens[r] ? x : -__builtin_inff();
+                    for (int r = 0; r < NP; ++r) {
+                        float x;
+                        if constexpr (PACK) x = score_of(d[0][0], d[0][1], d[0][2], dk[t]);
+                        else x = score_of(d[0][r], d[1][r], d[2][r], dk[t]);
+                        s[t][r] = token < lens[r] ? x : -__builtin_inff();
+                    }
+                    if constexpr (!PACK) __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (!PACK) __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
-        }
-        // the chunk's largest score, then its largest weight, over the waves
-        float mc[NP], unit[NP], up[NP];
-#pragma unroll
-        for (int r = 0; r < NP; ++r) {
-            const float m = row_max(max2(max3(s[0][r], s[1][r], s[2][r]), s[3][r])) * factors[r];
-            if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < NP; ++r) {
-            const int p = PACK ? group : 4 * group + r;
-            mc[r] = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
-            const float safe = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
-            float e[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factors[r], -safe));
-                s[t][r] = e[t] * dv[t];
-            }
-            lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
-            const float w = row_max(max3(max3(0.0f, s[0][r], s[1][r]), s[2][r], s[3][r]));
-            if (col == 0) top[1][wave][p] = w;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < NP; ++r) {
-            const int p = PACK ? group : 4 * group + r;
-            const int e = exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p])));
-            up[r] = pow2i(22 - e);
-            unit[r] = pow2i(e - 22);
-            uint32_t b[3];
-            cut_weights(s, r, up[r], b);
-            // operand rows: PACK 4 pair + digit; else one operand a digit, row = pair.  Pieces swizzled by the row (see store_digits).
-            if constexpr (PACK) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<uint32_t*>(digits + kChunk * (4 * group + g) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ g) + 4 * (col & 3)) = g < 3 ? b[g] : 0u;
             } else {
 #pragma unroll
-                for (int g = 0; g < 3; ++g)
-                    *reinterpret_cast<uint32_t*>(digits + kChunk * (g * kPairs + 4 * group + r) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ r) + 4 * (col & 3)) = b[g];
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
             }
-        }
-        __syncthreads();
-        v4i acc[DIGITS][2];
+            // the chunk's largest score, then its largest weight, over the waves
+            float mc[NP], unit[NP], up[NP];
 #pragma unroll
-        for (int p = 0; p < kChunkPages; ++p)
-#pragma unroll
-            for (int g = 0; g < DIGITS; ++g) {
-                const v4i w = load_digits(digits, g, p, lane);
-#pragma unroll
-                for (int n = 0; n < 2; ++n) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, vc[p][n], p == 0 ? zero : acc[g][n], 0, 0, 0);
+            for (int r = 0; r < NP; ++r) {
+                const float m = row_max(max2(max3(s[0][r], s[1][r], s[2][r]), s[3][r])) * factors[r];
+                if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
             }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < NP; ++r) {
+                const int p = PACK ? group : 4 * group + r;
+                mc[r] = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
+                const float safe = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+                float e[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factors[r], -safe));
+                    s[t][r] = e[t] * dv[t];
+                }
+                lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
+                const float w = row_max(max3(max3(0.0f, s[0][r], s[1][r]), s[2][r], s[3][r]));
+                if (col == 0) top[1][wave][p] = w;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < NP; ++r) {
+                const int p = PACK ? group : 4 * group + r;
+                const int e = exponent_above(fmaxf(fmaxf(top[1][0][p], top[1][1][p]), fmaxf(top[1][2][p], top[1][3][p])));
+                up[r] = pow2i(22 - e);
+                unit[r] = pow2i(e - 22);
+                uint32_t b[3];
+                cut_weights(s, r, up[r], b);
+                // operand rows: PACK 4 pair + digit; else one operand a digit, row = pair.  Pieces swizzled by the row (see store_digits).
+                if constexpr (PACK) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        *reinterpret_cast<uint32_t*>(digits + kChunk * (4 * group + g) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ g) + 4 * (col & 3)) = g < 3 ? b[g] : 0u;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 3; ++g)
+                        *reinterpret_cast<uint32_t*>(digits + kChunk * (g * kPairs + 4 * group + r) + 64 * (wave ^ group) + 16 * ((col >> 2) ^ r) + 4 * (col & 3)) = b[g];
+                }
+            }
+            __syncthreads();
+            v4i acc[DIGITS][2];
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                for (int g = 0; g < DIGITS; ++g) {
+                    const v4i w = load_digits(digits, g, p, lane);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, vc[p][n], p == 0 ? zero : acc[g][n], 0, 0, 0);
+                }
 
-        // of each pair two columns a lane
+            // of each pair two columns a lane
 #pragma unroll
-        for (int r = 0; r < NP; ++r) {
-            const int p = PACK ? group : 4 * group + r;
-            const float lc = row_sum((lsum[0][p][col] + lsum[1][p][col]) + (lsum[2][p][col] + lsum[3][p][col]));
-            const int pair_len = __shfl(len, p, kWave);
-            if (!((members >> p) & 1u)) continue;
-            const int row = pair_row(a, p);
-            const size_t head = (size_t)(row0 + row) * a.Hq + kvh * a.G + p - row * a.G;
-            float o[2];
+            for (int r = 0; r < NP; ++r) {
+                const int p = PACK ? group : 4 * group + r;
+                const float lc = row_sum((lsum[0][p][col] + lsum[1][p][col]) + (lsum[2][p][col] + lsum[3][p][col]));
+                const int pair_len = __shfl(len, p, kWave);
+                if (!((members >> p) & 1u)) continue;
+                const int row = pair_row(a, p);
+                const size_t head = (size_t)(row0 + row) * a.Hq + kvh * a.G + p - row * a.G;
+                float o[2];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) o[n] = PACK ? digits_value(acc[0][n][0], acc[0][n][1], acc[0][n][2]) : digits_value(acc[0][n][r], acc[PACK ? 0 : 1][n][r], acc[PACK ? 0 : 2][n][r]);
-            if (pair_len <= kChunk) {  // the row's only chunk
-                float fm = -__builtin_inff(), l = 0.0f, fa, fb;
-                fold_step(fm, l, mc[r], lc, unit[r], fa, fb);
-                const float by = row_factor(l);
+                for (int n = 0; n < 2; ++n) o[n] = PACK ? digits_value(acc[0][n][0], acc[0][n][1], acc[0][n][2]) : digits_value(acc[0][n][r], acc[PACK ? 0 : 1][n][r], acc[PACK ? 0 : 2][n][r]);
+                if (pair_len <= kChunk) {  // the row's only chunk
+                    float fm = -__builtin_inff(), l = 0.0f, fa, fb;
+                    fold_step(fm, l, mc[r], lc, unit[r], fa, fb);
+                    const float by = row_factor(l);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(to_bf16(fold_value(0.0f, o[n], fa, fb) * by), &a.out[head * kHeadDim + 32 * wave + 16 * n + col]);
-            } else {
-                const size_t at = head * a.chunks + chunk;
-                if (wave == 0 && col == 0) a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
+                    for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(to_bf16(fold_value(0.0f, o[n], fa, fb) * by), &a.out[head * kHeadDim + 32 * wave + 16 * n + col]);
+                } else {
+                    const size_t at = head * a.chunks + chunk;
+                    if (wave == 0 && col == 0) a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(o[n], &a.part_o[at * kHeadDim + 32 * wave + 16 * n + col]);
+                    for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(o[n], &a.part_o[at * kHeadDim + 32 * wave + 16 * n + col]);
+                }
             }
         }
-    }
     }
 }
 
