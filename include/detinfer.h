@@ -498,7 +498,7 @@ int det_kv8_copy_pages(void *pool, int n_layers, int n_pages, int Hkv, int D, co
  * hardware's exponential, l_c their sum in a fixed order; weights e_j d^V_j as integers rint(w 2^(22-E_c)), 2^E_c above the chunk's largest;
  * their products with the codes exact.  Chunks are folded in ascending order, relative to the largest m so far.  A row's bytes do not depend
  * on R, on the other rows, on the pages it lies in or on the call's max_pages.
- * Up to 2047 (tile, KV head) pairs, a tile being 16 / (Hq/Hkv) rows, and wherever slots is NULL, chunks go to workgroups of their own and meet in ws in a
+ * Up to 895 (tile, KV head) pairs, a tile being 16 / (Hq/Hkv) rows, and wherever slots is NULL, chunks go to workgroups of their own and meet in ws in a
  * second launch; beyond, a tile of rows that name slots walks its chunks in one launch.  Rows that name slots are best given slot by slot.
  *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  scale > 0 and finite;  R <= 65535 if slots is NULL;  ws: det_attn_decode_kv8_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);

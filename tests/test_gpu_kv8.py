@@ -294,10 +294,10 @@ def test_many_rows_of_many_slots_in_no_order(d):
         assert np.array_equal(down_bf16(one)[0], got[r]), r
 
 
-@pytest.mark.parametrize("R,Hq,Hkv,named", [(600, 32, 8, False), (600, 64, 8, False), (1400, 16, 16, True)])
+@pytest.mark.parametrize("R,Hq,Hkv,named", [(600, 32, 8, False), (600, 64, 8, False), (1700, 8, 8, True)])
 def test_workgroups_that_take_several_chunks(d, R, Hq, Hkv, named):
     """So many rows that a workgroup goes on from chunk to chunk, in a table much wider than the sequences are long; slots that share pages."""
-    lengths = [1500, 40, 1290, 700]
+    lengths = [4000, 40, 2900, 700]
     cache = Cache(7347, lengths, Hkv)
     rng = np.random.default_rng(R + Hq)
     slots = np.sort(rng.integers(0, 4, R)).astype(np.int32) if named else (np.arange(R) % 4).astype(np.int32)
