@@ -4,7 +4,7 @@
 //   scores   q of a (row, head) as a fixed-point number of 23 bits relative to its largest element, in three signed digits of base 256; digit
 //            sums are below 2^21 and exact in fp32.
 //   values   the weights w_j = e_j d^V_j of a chunk of 256 tokens as fixed-point numbers of 22 bits relative to the chunk's largest, three
-//            digits; a chunk's digit sums are below 2^22.  What a weight loses is at most 2^-23 of the largest one, whose own value
+//            digits; a chunk's digit sums are below 2^22.  What a weight loses is at most 2^-22 of the largest one, whose own value
 //            the cache holds to half a code only.
 // Softmax: a chunk's reference m_c is an integer (the ceiling of its largest score in units of log2), so the factors by which chunks are
 // brought together are powers of two.  Chunks are folded in ascending order.
