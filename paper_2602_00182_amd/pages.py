@@ -25,6 +25,7 @@ class KVPages:
         self.table = torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=device)
         self._host = torch.full((n_slots, max_pages), -1, dtype=torch.int32)
         self._pages = [[] for _ in range(n_slots)]  # of each slot, in order
+        self._forked = [0] * n_slots                # tokens of each slot up to which a fork shared its pages: it goes on behind them
         self._refs = [0] * n_pages
         self._free = list(range(n_pages))           # a heap: the lowest page first
 
@@ -53,8 +54,9 @@ class KVPages:
             heapq.heappush(self._free, page)
 
     def reserve(self, slots, lengths, write_from=None, stream=None) -> None:
-        """Makes room for the first lengths[i] tokens of slots[i], and the pages from token write_from[i] on (default: where the slot's pages end)
-        the slot's own: a shared page among them is copied where tokens in front of write_from[i] lie in it, else replaced."""
+        """Makes room for the first lengths[i] tokens of slots[i], and the pages from token write_from[i] on the slot's own: a shared page among
+        them is copied where tokens in front of write_from[i] lie in it, else replaced.  Default: the slot is written behind the tokens that the longest of
+        its forks shared (or that a truncation left of them), if lengths[i] reaches beyond them; a slot that writes further in front says so."""
         slots, lengths = list(slots), list(lengths)
         if len(set(slots)) != len(slots) or len(lengths) != len(slots) or (write_from is not None and len(write_from) != len(slots)):
             raise ValueError("one length for each of several different slots")
@@ -63,7 +65,10 @@ class KVPages:
             have, count = self._pages[slot], -(-length // api.KV8_PAGE)
             if length < 0 or count > self.table.shape[1]:
                 raise ValueError("a length outside the page table")
-            begin = len(have) * api.KV8_PAGE if write_from is None else int(write_from[i])
+            if write_from is not None:
+                begin = int(write_from[i])
+            else:
+                begin = self._forked[slot] if length > self._forked[slot] else len(have) * api.KV8_PAGE
             if begin < 0:
                 raise ValueError("bad write_from")
             want.append((slot, begin, count))
@@ -106,6 +111,8 @@ class KVPages:
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             for s in dsts:
                 self._pages[s] = self._pages[src][:count]
+                self._forked[s] = length
+                self._forked[src] = max(self._forked[src], length)
                 for page in self._pages[s]:
                     self._refs[page] += 1
             self._write_table()
@@ -119,6 +126,7 @@ class KVPages:
             for page in self._pages[slot][keep:]:
                 self._drop(page)
             del self._pages[slot][keep:]
+            self._forked[slot] = min(self._forked[slot], length)
             self._write_table()
 
     def release(self, slot: int, stream=None) -> None:

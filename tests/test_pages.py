@@ -128,3 +128,45 @@ def test_random_histories(seed):
             assert read(p, s, len(tokens)) == tokens
         assert p.free_pages == 14 - len({x for s in range(4) for x in p.pages(s)})
     assert isinstance(p, pages.KVPages)
+
+
+@pytest.mark.parametrize("shared", [1, 63, 64, 65, 100, 128])
+def test_a_shared_last_page_is_copied_without_write_from_too(shared):
+    """The source had room for more than it shared, a first copy holds just the shared tokens, a second is cut before it goes on."""
+    p = make()
+    p.reserve([0], [shared + 40])
+    for t in range(shared):
+        write(p, 0, t, t % 251)
+    p.fork(0, [1, 2], shared)
+    cut = max(1, shared - 30)
+    p.truncate(2, cut)
+    p.reserve([0, 1], [shared + 1] * 2)
+    p.reserve([2], [cut + 1])
+    for s, n in ((0, shared), (1, shared), (2, cut)):
+        write(p, s, n, 200 + s)
+    for s, n in ((0, shared), (1, shared), (2, cut)):
+        assert read(p, s, n + 1) == [t % 251 for t in range(n)] + [200 + s]
+    full = shared // 64
+    assert p.pages(0)[:full] == p.pages(1)[:full]  # pages that no one writes stay shared
+
+
+def test_the_longest_fork_of_a_slot_is_what_it_goes_on_behind():
+    p = make(n_pages=20)
+    p.reserve([0], [200])
+    for t in range(200):
+        write(p, 0, t, t % 251)
+    p.fork(0, [1], 200)
+    p.fork(0, [2], 70)
+    p.reserve([0, 2], [201, 71])
+    write(p, 0, 200, 201)
+    write(p, 2, 70, 202)
+    p.reserve([1], [200])                     # no longer than what is shared: nothing is written
+    assert p.free_pages == 20 - 4 - 2 and p.pages(1)[:3] == p.pages(0)[:3] and p.pages(2)[0] == p.pages(0)[0]
+    p.reserve([1], [201])
+    write(p, 1, 200, 203)
+    p.release(2)
+    p.fork(1, [2], 10)
+    p.reserve([2], [20])
+    write(p, 2, 10, 204)
+    text = [t % 251 for t in range(200)]
+    assert read(p, 0, 201) == text + [201] and read(p, 1, 201) == text + [203] and read(p, 2, 11) == text[:10] + [204]
