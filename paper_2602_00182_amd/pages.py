@@ -33,8 +33,15 @@ class KVPages:
     def free_pages(self) -> int:
         return len(self._free)
 
+    def _slots(self, *slots) -> None:
+        """Refuses slots that are none; a negative index would name another slot from the end."""
+        for slot in slots:
+            if not 0 <= slot < len(self._pages):
+                raise ValueError(f"slot {slot} of {len(self._pages)}")
+
     def pages(self, slot: int) -> list[int]:
         """The pages of a slot, in order."""
+        self._slots(slot)
         return list(self._pages[slot])
 
     def _copy(self, pairs, stream) -> None:  # with `stream` the current one: the pairs' tensors live in its memory
@@ -58,6 +65,7 @@ class KVPages:
         them is copied where tokens in front of write_from[i] lie in it, else replaced.  Default: the slot is written behind the tokens that the longest of
         its forks shared (or that a truncation left of them), if lengths[i] reaches beyond them; a slot that writes further in front says so."""
         slots, lengths = list(slots), list(lengths)
+        self._slots(*slots)
         if len(set(slots)) != len(slots) or len(lengths) != len(slots) or (write_from is not None and len(write_from) != len(slots)):
             raise ValueError("one length for each of several different slots")
         want, need = [], 0
@@ -106,6 +114,7 @@ class KVPages:
         """Each of the empty slots `dsts` shares the pages of the first `length` tokens of slot src.  Whoever writes into one of them reserves first."""
         count = -(-length // api.KV8_PAGE)
         dsts = list(dsts)
+        self._slots(src, *dsts)
         if length < 0 or count > len(self._pages[src]) or len(set(dsts)) != len(dsts) or any(self._pages[s] for s in dsts) or src in dsts:
             raise ValueError("fork takes tokens that are there to different empty slots")
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
@@ -119,6 +128,7 @@ class KVPages:
 
     def truncate(self, slot: int, length: int, stream=None) -> None:
         """Gives back the pages behind the first `length` tokens of a slot (0: all of them)."""
+        self._slots(slot)
         if length < 0:
             raise ValueError("a length outside the page table")
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():

@@ -170,3 +170,15 @@ def test_the_longest_fork_of_a_slot_is_what_it_goes_on_behind():
     write(p, 2, 10, 204)
     text = [t % 251 for t in range(200)]
     assert read(p, 0, 201) == text + [201] and read(p, 1, 201) == text + [203] and read(p, 2, 11) == text[:10] + [204]
+
+
+def test_slots_that_are_none_are_refused():
+    p = make()
+    p.reserve([0, 3], [70, 5])
+    before = (p.table.clone(), p.free_pages)
+    for call in (lambda: p.reserve([3, -1], [10, 300]), lambda: p.reserve([-4], [300]), lambda: p.reserve([4], [1]), lambda: p.fork(-4, [1], 10),
+                 lambda: p.fork(0, [-2], 10), lambda: p.fork(0, [2, -2], 10), lambda: p.fork(4, [1], 0), lambda: p.truncate(-1, 0), lambda: p.release(4),
+                 lambda: p.release(-4), lambda: p.pages(-1), lambda: p.pages(4)):
+        with pytest.raises(ValueError):
+            call()
+    assert torch.equal(p.table, before[0]) and p.free_pages == before[1]
