@@ -296,9 +296,9 @@ def speculative_decode(model: DecodeModel, draft: DecodeModel, prompts: torch.Te
     """Draws n_new tokens for each sequence from the model's own distribution (temperature 1), n_draft at a time proposed by `draft` (a model of the
     same vocabulary) and verified in one pass of `model` over n_draft + 1 rows of each sequence (det_verify_drafts).
 
-    uniforms: a function (round, shape) -> fp32 numbers in [0, 1) on the device, called twice a round, for (B, n_draft) draws of the draft model and
-    (B, n_draft + 1) of the verification; round -1 gives the (B, 2) numbers of the first token, of which the second is used.  The tokens are a
-    function of the models, the prompts and these numbers; what a sequence gets does not depend on the batch.
+    uniforms: a function (round, shape) -> independent fp32 numbers in [0, 1) on the device, called once a round for (B, 2 n_draft + 1): n_draft
+    draws of the draft model, then n_draft + 1 of the verification.  Round -1 gives the (B, 2) numbers of the first token, of which the second is used.
+    The tokens are a function of the models, the prompts and these numbers; what a sequence gets does not depend on the batch.
 
     Rejected drafts need no undoing: a sequence's length ends in front of them and their places in the caches are written again.
 
@@ -360,7 +360,7 @@ def _speculative_decode(model, draft, prompts, prompt_lens, n_new, n_draft, unif
     two = torch.zeros((B, 2), **f32)
     while min(map(len, made)) < n_new:
         # the draft model's own tokens; one step more, so that its cache has the last of them too.  A sequence that has its tokens stays where it is.
-        u = uniforms(turn, (B, N))
+        u = uniforms(turn, (B, 2 * N + 1))
         for i in range(N + 1):
             small.tokens.copy_(current if i == 0 else drafts[:, i - 1])
             small.positions.copy_(at + i)
@@ -372,7 +372,7 @@ def _speculative_decode(model, draft, prompts, prompt_lens, n_new, n_draft, unif
         rows.positions.copy_((at[:, None] + step_numbers).flatten())
         rows.forward(stream)
         api.det_softmax_f32(rows.logits, width, p.view(B * (N + 1), V), sums[0], sums[1], stream)
-        api.det_verify_drafts(p, q.transpose(0, 1).contiguous(), drafts, None, uniforms(turn, (B, N + 1)), accepted, tokens, ws, stream)
+        api.det_verify_drafts(p, q.transpose(0, 1).contiguous(), drafts, None, u[:, N:].contiguous(), accepted, tokens, ws, stream)
         host, took = tokens.cpu(), accepted.cpu()
         counts.append(took)
         on = [len(m) < n_new for m in made]
