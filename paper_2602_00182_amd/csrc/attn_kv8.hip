@@ -199,7 +199,7 @@ __device__ __forceinline__ int row_length(const kv8_attn_args& a, int row, int& 
 }
 
 // What a score's token contributes with: d^K, poisoned where the token's V row is not finite (the rows that see the token become NaN, the others
-// do not), and d^V, 0 there // (scales: the page's K scales, its V scales behind them).
+// do not), and d^V, 0 there.  scales: the page's K scales, its V scales behind them.
 __device__ __forceinline__ void clean_scales(float (&dk)[4], float (&dv)[4])
 {
     bool bad = false;
@@ -232,6 +232,9 @@ __device__ __forceinline__ void token_scales(const uint8_t* rec, int col, float 
 // Row and head within the KV head of pair p of a tile (p < 16, exact).
 __device__ __forceinline__ int pair_row(const kv8_attn_args& a, int p) { return (p * a.inverse_G) >> 16; }
 
+// The row's factor for scores whose largest is x.  Where none is above -inf they are masked or NaN, and a query's NaN would make NaN of the masked ones:
+// 1 leaves both what they are.
+__device__ __forceinline__ float seen_factor(float x, float factor) { return x == -__builtin_inff() ? 1.0f : factor; }
 
 // A score from its digit sums; times the row's factor it is in units of log2.
 __device__ __forceinline__ float score_of(int d0, int d1, int d2, float dk)
@@ -411,11 +414,12 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
                     for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
             }
             // the chunk's largest score, then its largest weight, over the waves
-            float mc[NP], unit[NP], up[NP];
+            float mc[NP], unit[NP], up[NP], f[NP];
 #pragma unroll
             for (int r = 0; r < NP; ++r) {
-                const float m = row_max(max2(max3(s[0][r], s[1][r], s[2][r]), s[3][r])) * factors[r];
-                if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = m;
+                const float x = row_max(max2(max3(s[0][r], s[1][r], s[2][r]), s[3][r]));
+                f[r] = seen_factor(x, factors[r]);
+                if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = x * f[r];
             }
             __syncthreads();
 #pragma unroll
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
                 float e[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], factors[r], -safe));
+                    e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], f[r], -safe));
                     s[t][r] = e[t] * dv[t];
                 }
                 lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
@@ -539,7 +543,7 @@ template <class Scales>
 __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], const float (&factors)[4], Scales scales, float (&mc)[4],
                                                 float (&lc)[4], float (&up)[4], float (&unit)[4])
 {
-    float safe[4], sum[kChunkPages][4], top[4];
+    float safe[4], sum[kChunkPages][4], top[4], f[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         float x = -__builtin_inff();
@@ -547,7 +551,9 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
         for (int p = 0; p < kChunkPages; ++p)
 #pragma unroll
             for (int t = 0; t < 4; t += 2) x = max3(x, s[p][t][r], s[p][t + 1][r]);
-        mc[r] = __builtin_ceilf(row_max(x) * factors[r]);
+        x = row_max(x);
+        f[r] = seen_factor(x, factors[r]);
+        mc[r] = __builtin_ceilf(x * f[r]);
         safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
         top[r] = 0.0f;
     }
@@ -560,7 +566,7 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
             float e[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][t][r], factors[r], -safe[r]));
+                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][t][r], f[r], -safe[r]));
                 s[p][t][r] = e[t] * dv[t];
             }
             top[r] = max3(max3(top[r], s[p][0][r], s[p][1][r]), s[p][2][r], s[p][3][r]);
