@@ -236,6 +236,16 @@ __device__ __forceinline__ int pair_row(const kv8_attn_args& a, int p) { return 
 // 1 leaves both what they are.
 __device__ __forceinline__ float seen_factor(float x, float factor) { return x == -__builtin_inff() ? 1.0f : factor; }
 
+// From 2^24 on a score's product with the factor is rounded by a unit and more, and an fma that keeps it exact would leave the largest score anywhere
+// within 2^7 units of m at 2^31: its weight 0 or infinite.  There the product is rounded first, so that the largest is m itself.  (An infinite m stays one:
+// the row becomes NaN.)
+constexpr float kFarScore = 0x1p24f;
+__device__ __forceinline__ void far_scores(float (&s)[4], float f, float m)
+{
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = fabsf(m) >= kFarScore ? s[t] * f - m : s[t];
+}
+
 // A score from its digit sums; times the row's factor it is in units of log2.
 __device__ __forceinline__ float score_of(int d0, int d1, int d2, float dk)
 {
@@ -422,15 +432,31 @@ __global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_attn_chunk_kernel(kv8_a
                 if (col == 0) top[0][wave][PACK ? group : 4 * group + r] = x * f[r];
             }
             __syncthreads();
+            float safe[NP], most = 0.0f;
 #pragma unroll
             for (int r = 0; r < NP; ++r) {
                 const int p = PACK ? group : 4 * group + r;
                 mc[r] = __builtin_ceilf(fmaxf(fmaxf(top[0][0][p], top[0][1][p]), fmaxf(top[0][2][p], top[0][3][p])));
-                const float safe = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+                safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
+                most = max2(most, fabsf(safe[r]));
+            }
+            if (__builtin_expect(__ballot(most >= kFarScore) != 0, 0)) {
+#pragma unroll
+                for (int r = 0; r < NP; ++r) {
+                    float x[4] = {s[0][r], s[1][r], s[2][r], s[3][r]};
+                    far_scores(x, f[r], safe[r]);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) s[t][r] = x[t];
+                    if (fabsf(safe[r]) >= kFarScore) f[r] = 1.0f, safe[r] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < NP; ++r) {
+                const int p = PACK ? group : 4 * group + r;
                 float e[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], f[r], -safe));
+                    e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], f[r], -safe[r]));
                     s[t][r] = e[t] * dv[t];
                 }
                 lsum[wave][p][col] = (e[0] + e[1]) + (e[2] + e[3]);
@@ -556,6 +582,19 @@ __device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], c
         mc[r] = __builtin_ceilf(x * f[r]);
         safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
         top[r] = 0.0f;
+    }
+    if (__builtin_expect(__ballot(max3(max2(fabsf(safe[0]), fabsf(safe[1])), fabsf(safe[2]), fabsf(safe[3])) >= kFarScore) != 0, 0)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                float x[4] = {s[p][0][r], s[p][1][r], s[p][2][r], s[p][3][r]};
+                far_scores(x, f[r], safe[r]);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) s[p][t][r] = x[t];
+            }
+            if (fabsf(safe[r]) >= kFarScore) f[r] = 1.0f, safe[r] = 0.0f;
+        }
     }
 #pragma unroll
     for (int p = 0; p < kChunkPages; ++p) {
