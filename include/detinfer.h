@@ -501,8 +501,11 @@ int det_kv8_copy_pages(void *pool, int n_layers, int n_pages, int Hkv, int D, co
  * on R, on the other rows, on the pages it lies in or on the call's max_pages.
  * Up to 895 (tile, KV head) pairs, a tile being 16 / (Hq/Hkv) rows, and wherever slots is NULL, chunks go to workgroups of their own and meet in ws in a
  * second launch; beyond, a tile of rows that name slots walks its chunks in one launch.  Rows that name slots are best given slot by slot.
- *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  scale > 0 and finite;  R <= 65535 if slots is NULL;  ws: det_attn_decode_kv8_workspace_bytes bytes. */
+ *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  scale > 0 and finite;  R <= 65535 if slots is NULL;  ws: det_attn_decode_kv8_workspace_bytes bytes, or
+ *   for rows that name slots det_attn_decode_kv8_rows_workspace_bytes: enough for a call of up to R such rows, and no more for thousands of them
+ *   than for those 895 pairs (a call in one launch keeps nothing in ws and does not look at ws_bytes). */
 size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
+size_t det_attn_decode_kv8_rows_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
 int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
                         int max_pages, const int32_t *seqlens, const int32_t *slots, void *out, void *ws, size_t ws_bytes,
                         int R, int Hq, int Hkv, int D, float scale, void *stream);
@@ -512,13 +515,16 @@ int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_tab
  * output goes through det_quant_act_q8).  slots may be NULL: row r is the sequence in slot r.
  * Weights: wqkv from det_gemm_pack_b (det_quant_pack_w4 for the quantized layer), columns query, key and value heads; the others as there.
  * cfg->Lmax: rows of the rope tables.  A row whose position has no page attends to what is there.  Same invariance: a row's bytes do not depend on R,
- * on the other rows or on where the pages lie, and T tokens of a prompt in one call are the T calls of one. */
+ * on the other rows or on where the pages lie, and T tokens of a prompt in one call are the T calls of one.
+ * Workspace: *_kv8_workspace_bytes, or *_kv8_rows_workspace_bytes where slots is not NULL (enough for up to R rows). */
 size_t det_decoder_layer_kv8_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
+size_t det_decoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
 int det_decoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
                           const int32_t *page_table, int n_pages, int n_slots, int max_pages, const int32_t *positions,
                           const int32_t *slots, const float *rope_cos, const float *rope_sin, void *ws,
                           size_t ws_bytes, int R, void *stream);
 size_t det_qdecoder_layer_kv8_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
+size_t det_qdecoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages);
 int det_qdecoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
                            const int32_t *page_table, int n_pages, int n_slots, int max_pages, const int32_t *positions,
                            const int32_t *slots, const float *rope_cos, const float *rope_sin, void *ws,

@@ -88,11 +88,14 @@ SIGNATURES = {
     "det_kv8_read": (_i, [_vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
     "det_kv8_copy_pages": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _i, _vp]),
     "det_attn_decode_kv8_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "det_attn_decode_kv8_rows_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "det_attn_decode_kv8": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _i, _f, _vp]),
     "det_decoder_layer_kv8_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
+    "det_decoder_layer_kv8_rows_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_decoder_layer_kv8": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
                                    _vp, _sz, _i, _vp]),
     "det_qdecoder_layer_kv8_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
+    "det_qdecoder_layer_kv8_rows_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_qdecoder_layer_kv8": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
                                     _vp, _sz, _i, _vp]),
     "det_verify_drafts_workspace_bytes": (_sz, [_i, _i]),

@@ -26,8 +26,9 @@ __all__ = [
     "det_qdecoder_layer_workspace_bytes", "det_qdecoder_layer", "det_attn_decode_quant_q8",
     "det_qgemm_w4a8_swiglu_quant_supported", "det_qgemm_w4a8_swiglu_quant",
     "KV8_PAGE", "KV8_RECORD", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
-    "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8", "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8",
-    "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts_workspace_bytes", "det_verify_drafts",
+    "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8_rows_workspace_bytes", "det_attn_decode_kv8",
+    "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8_rows_workspace_bytes", "det_decoder_layer_kv8",
+    "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8_rows_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts_workspace_bytes", "det_verify_drafts",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -786,6 +787,11 @@ def det_attn_decode_kv8_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_p
     return lib().det_attn_decode_kv8_workspace_bytes(R, Hq, Hkv, D, max_pages)
 
 
+def det_attn_decode_kv8_rows_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_pages: int) -> int:
+    """For calls of up to R rows that name slots."""
+    return lib().det_attn_decode_kv8_rows_workspace_bytes(R, Hq, Hkv, D, max_pages)
+
+
 def det_attn_decode_kv8(q, pool, page_table, seqlens, slots, out, ws, scale: float, stream=None) -> None:
     """out [R, Hq, 128] = attention of q over the first seqlens[r] tokens of slot slots[r] (None: slot r) of the 8-bit cache."""
     shape = R, Hq, D = q.shape
@@ -802,8 +808,16 @@ def det_decoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int)
     return lib().det_decoder_layer_kv8_workspace_bytes(C.byref(cfg), R, max_pages)
 
 
+def det_decoder_layer_kv8_rows_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
+    return lib().det_decoder_layer_kv8_rows_workspace_bytes(C.byref(cfg), R, max_pages)
+
+
 def det_qdecoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
     return lib().det_qdecoder_layer_kv8_workspace_bytes(C.byref(cfg), R, max_pages)
+
+
+def det_qdecoder_layer_kv8_rows_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
+    return lib().det_qdecoder_layer_kv8_rows_workspace_bytes(C.byref(cfg), R, max_pages)
 
 
 def det_decoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream=None,

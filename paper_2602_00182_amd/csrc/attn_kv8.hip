@@ -983,10 +983,16 @@ __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
     }
 }
 
-size_t attn_decode_kv8_workspace(int R, int Hq, int max_pages)
+// Whether a call walks its chunks (nothing in the workspace).
+static bool walks(bool named, long long tiles, int Hkv) { return named && tiles * Hkv >= DET_KV8_WALK_TILES; }
+
+size_t attn_decode_kv8_workspace(int R, int Hq, int Hkv, int max_pages, bool named)
 {
     const size_t chunks = ((size_t)max_pages + kChunkPages - 1) / kChunkPages;
-    return (size_t)R * Hq * chunks * (kHeadDim + 4) * sizeof(float);
+    // of more rows than these, only calls that walk
+    const int most = named ? (DET_KV8_WALK_TILES - 1) / Hkv * (kPairs / (Hq / Hkv)) : R;
+    const size_t bytes = (size_t)(R < most ? R : most) * Hq * chunks * (kHeadDim + 4) * sizeof(float);
+    return bytes < 16 ? 16 : bytes;
 }
 
 int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset, void* out,
@@ -999,7 +1005,10 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     if (Hq % cache.Hkv != 0 || Hq / cache.Hkv > kPairs || cache.Hkv > 65535) return DET_ESHAPE;
     if (!slots && cache.n_slots < R) return DET_ESHAPE;
     if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return DET_EALIGN;
-    if (ws_bytes < attn_decode_kv8_workspace(R, Hq, cache.max_pages)) return DET_EWORKSPACE;
+    const int tile_rows = slots ? kPairs / (Hq / cache.Hkv) : 1;
+    const long long tiles = ((long long)R + tile_rows - 1) / tile_rows;
+    const bool walk = walks(slots != nullptr, tiles, cache.Hkv);
+    if (!walk && ws_bytes < attn_decode_kv8_workspace(R, Hq, cache.Hkv, cache.max_pages, false)) return DET_EWORKSPACE;
     kv8_attn_args a{};
     a.q = static_cast<const uint16_t*>(q);
     a.c = cache;
@@ -1011,16 +1020,15 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.G = Hq / cache.Hkv;
     const bool packed = !slots && a.G <= 4;  // rows that share nothing, one to a tile
     a.inverse_G = 65536 / a.G + 1;
-    a.rows_per_tile = slots ? kPairs / a.G : 1;
+    a.rows_per_tile = tile_rows;
     a.len_offset = len_offset;
     a.chunks = (cache.max_pages + kChunkPages - 1) / kChunkPages;
     a.scale_log2 = scale * 1.44269504f;
     const size_t pairs = (size_t)R * Hq * a.chunks;
     a.part_o = static_cast<float*>(ws);
     a.part = reinterpret_cast<float4*>(a.part_o + pairs * kHeadDim);
-    const long long tiles = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile;
     if (tiles * cache.Hkv > 0x7FFFFFFFll / 256 || (long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
-    if (slots && tiles * cache.Hkv >= DET_KV8_WALK_TILES) {
+    if (walk) {
         hipLaunchKernelGGL(kv8_attn_walk_kernel, dim3((unsigned)((tiles + 3) / 4 * cache.Hkv)), dim3(256), 0, s, a);
         return check_launch();
     }
@@ -1041,7 +1049,13 @@ using namespace det;
 extern "C" size_t det_attn_decode_kv8_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages)
 {
     if (R < 1 || Hq < 1 || Hkv < 1 || D != kHeadDim || max_pages < 1 || max_pages > DET_KV8_MAX_PAGES || Hq % Hkv != 0) return 0;
-    return attn_decode_kv8_workspace(R, Hq, max_pages);
+    return attn_decode_kv8_workspace(R, Hq, Hkv, max_pages, false);
+}
+
+extern "C" size_t det_attn_decode_kv8_rows_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages)
+{
+    if (det_attn_decode_kv8_workspace_bytes(R, Hq, Hkv, D, max_pages) == 0 || Hq / Hkv > kPairs) return 0;
+    return attn_decode_kv8_workspace(R, Hq, Hkv, max_pages, true);
 }
 
 extern "C" int det_attn_decode_kv8(const void* q, const void* pool, const int32_t* page_table, int n_pages, int n_slots, int max_pages,

@@ -60,8 +60,8 @@ __device__ __forceinline__ const uint8_t* kv8_record_uniform(const kv8_cache& c,
 int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset, void* out,
                          void* ws, size_t ws_bytes, int R, int Hq, int D, float scale, hipStream_t s);
 
-// Workspace that attn_decode_kv8_impl takes.
-size_t attn_decode_kv8_workspace(int R, int Hq, int max_pages);
+// Workspace for attn_decode_kv8_impl of up to R rows.  named: its rows name slots, and calls of many of them keep nothing there.
+size_t attn_decode_kv8_workspace(int R, int Hq, int Hkv, int max_pages, bool named);
 
 inline int kv8_check(const void* pool, const int32_t* table, int n_pages, int n_slots, int max_pages, int Hkv, int D)
 {

@@ -212,12 +212,12 @@ struct Kv8LayerWs {
     size_t qkv, attn, attn_bytes, total;
 };
 
-static Kv8LayerWs kv8_layer_ws(const det_layer_cfg& c, int R, int max_pages, size_t at)
+static Kv8LayerWs kv8_layer_ws(const det_layer_cfg& c, int R, int max_pages, bool named, size_t at)
 {
     Kv8LayerWs w{};
     w.qkv = at;
     w.attn = w.qkv + up256(2 * (size_t)R * (c.Hq + 2 * c.Hkv) * c.D);
-    w.attn_bytes = attn_decode_kv8_workspace(R, c.Hq, max_pages);
+    w.attn_bytes = attn_decode_kv8_workspace(R, c.Hq, c.Hkv, max_pages, named);
     w.total = w.attn + up256(w.attn_bytes);
     return w;
 }
@@ -237,11 +237,20 @@ static int kv8_layer_check(const det_layer_weights* w, const det_layer_cfg* cfg,
     return DET_OK;
 }
 
+static bool kv8_layer_sizes_ok(const det_layer_cfg* cfg, int R, int max_pages)
+{
+    return layer_cfg_ok(cfg) && R >= 1 && max_pages >= 1 && max_pages <= DET_KV8_MAX_PAGES;
+}
+
 extern "C" size_t det_decoder_layer_kv8_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
-    if (!layer_cfg_ok(cfg) || R < 1 || max_pages < 1 || max_pages > DET_KV8_MAX_PAGES) return 0;
-    const LayerWs l = layer_ws(*cfg, R);
-    return kv8_layer_ws(*cfg, R, max_pages, l.attn).total;
+    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_layer_ws(*cfg, R, max_pages, false, layer_ws(*cfg, R).attn).total : 0;
+}
+
+extern "C" size_t det_decoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
+{
+    if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
+    return kv8_layer_ws(*cfg, R, max_pages, true, layer_ws(*cfg, R).attn).total;
 }
 
 extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
@@ -252,7 +261,7 @@ extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer
     if (bad != DET_OK) return bad;
     const det_layer_cfg c = *cfg;
     const LayerWs l = layer_ws(c, R);
-    const Kv8LayerWs k = kv8_layer_ws(c, R, max_pages, l.attn);
+    const Kv8LayerWs k = kv8_layer_ws(c, R, max_pages, slots != nullptr, l.attn);
     if (ws_bytes < k.total) return DET_EWORKSPACE;
     char* base = static_cast<char*>(ws);
     const int nq = c.Hq * c.D, n = (c.Hq + 2 * c.Hkv) * c.D;
@@ -269,17 +278,23 @@ extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer
 }
 
 // The quantized layer's attention output in bf16 (its rows are quantized for the output projection) lies where the plain layer has none.
-static Kv8LayerWs kv8_qlayer_ws(const det_layer_cfg& c, const QLayerWs& l, int R, int max_pages, size_t& att)
+static Kv8LayerWs kv8_qlayer_ws(const det_layer_cfg& c, const QLayerWs& l, int R, int max_pages, bool named, size_t& att)
 {
     att = l.attn;
-    return kv8_layer_ws(c, R, max_pages, l.attn + up256(2 * (size_t)R * c.Hq * c.D));
+    return kv8_layer_ws(c, R, max_pages, named, l.attn + up256(2 * (size_t)R * c.Hq * c.D));
 }
 
 extern "C" size_t det_qdecoder_layer_kv8_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
-    if (!layer_cfg_ok(cfg) || R < 1 || max_pages < 1 || max_pages > DET_KV8_MAX_PAGES) return 0;
     size_t att;
-    return kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, att).total;
+    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, false, att).total : 0;
+}
+
+extern "C" size_t det_qdecoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
+{
+    size_t att;
+    if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
+    return kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, true, att).total;
 }
 
 extern "C" int det_qdecoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
@@ -291,7 +306,7 @@ extern "C" int det_qdecoder_layer_kv8(const det_layer_weights* w, const det_laye
     const det_layer_cfg c = *cfg;
     const QLayerWs l = qlayer_ws(c, R);
     size_t att;
-    const Kv8LayerWs k = kv8_qlayer_ws(c, l, R, max_pages, att);
+    const Kv8LayerWs k = kv8_qlayer_ws(c, l, R, max_pages, slots != nullptr, att);
     if (ws_bytes < k.total) return DET_EWORKSPACE;
     char* base = static_cast<char*>(ws);
     const int nq = c.Hq * c.D, n = (c.Hq + 2 * c.Hkv) * c.D;

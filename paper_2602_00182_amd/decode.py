@@ -66,9 +66,11 @@ class DecodeModel:
                                        packed["wgu"], packed["wdown"])
             self.layers.append((packed, struct))
 
-    def layer_workspace_bytes(self, lcfg, rows: int) -> int:
+    def layer_workspace_bytes(self, lcfg, rows: int, named: bool = False) -> int:
+        """For steps of `rows` rows; named: rows that name their slots, which takes less of an 8-bit cache."""
         if self.cache8:
-            size = api.det_qdecoder_layer_kv8_workspace_bytes if self.quantized else api.det_decoder_layer_kv8_workspace_bytes
+            kind = "det_qdecoder_layer_kv8" if self.quantized else "det_decoder_layer_kv8"
+            size = getattr(api, kind + ("_rows_workspace_bytes" if named else "_workspace_bytes"))
             return size(lcfg, rows, -(-lcfg.Lmax // api.KV8_PAGE))
         if self.quantized:
             return api.det_qdecoder_layer_workspace_bytes(lcfg, rows)
@@ -132,7 +134,7 @@ class DecodeState:
     def of_rows(self, slots: torch.Tensor) -> "DecodeState":
         """A state over the same caches whose steps take one row for each entry of slots (several rows may name one sequence)."""
         st = copy.copy(self)
-        st.ws = torch.empty(self.model.layer_workspace_bytes(self.lcfg, slots.shape[0]), dtype=torch.uint8, device=slots.device)
+        st.ws = torch.empty(self.model.layer_workspace_bytes(self.lcfg, slots.shape[0], named=True), dtype=torch.uint8, device=slots.device)
         st._buffers(slots.shape[0])
         st.slots = slots
         return st
@@ -263,7 +265,7 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
     last_rows = torch.repeat_interleave(starts + lens_host - 1, samples).to(torch.int32).to(dev)
 
     xr = torch.empty((R, c.H), dtype=torch.bfloat16, device=dev)
-    ws = torch.empty(model.layer_workspace_bytes(st.lcfg, R), dtype=torch.uint8, device=dev)
+    ws = torch.empty(model.layer_workspace_bytes(st.lcfg, R, named=True), dtype=torch.uint8, device=dev)
     api.det_embed_gather(model.embed, row_tokens, xr, stream)
     for i, (_, struct) in enumerate(model.layers):
         model.layer(struct, st.lcfg, xr, st.kcache[i], st.vcache[i], row_pos, row_slots, st.rope_cos, st.rope_sin, ws,
