@@ -16,8 +16,8 @@ def d():
     return d
 
 
-@pytest.mark.parametrize("R,Hq,Hkv,named", [(6, 4, 2, False), (6, 16, 2, False), (6, 4, 2, True), (500, 32, 8, True)])
-@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("R,Hq,Hkv,named,mixed", [(6, 4, 2, False, False), (6, 16, 2, False, False), (6, 4, 2, True, False), (500, 32, 8, True, False),
+                                                  (500, 32, 8, True, True)])  # mixed: tiles that walk alone
 @pytest.mark.parametrize("exponent", [20, 24, 30, 36, 60, 100])
 @pytest.mark.parametrize("sign", [1, -1])
 def test_the_largest_of_large_scores_takes_all(d, R, Hq, Hkv, named, mixed, exponent, sign):
@@ -25,8 +25,6 @@ def test_the_largest_of_large_scores_takes_all(d, R, Hq, Hkv, named, mixed, expo
     of magnitudes, and the query's 2^-22), so its token has the weight 1 and the others 0.  Then the result is the token's value: e <= 1 has two
     roundings of 2^-24 beside its quotient's, the weight as an integer of 22 bits half a step of at most 2^-21, and bf16 rounds by 2^-8.  With sign -1 all
     keys point away from the query: every score is below zero."""
-    if mixed and not (named and R > 16):
-        pytest.skip("only rows that walk go alone or together")
     lengths = [300, 64, 700, 257, 513, 130]
     G = Hq // Hkv
 
