@@ -90,15 +90,15 @@ class DecodeModel:
             api.det_decoder_layer_rows(struct, lcfg, x, kcache, vcache, positions, slots, rope_cos, rope_sin, ws,
                                        stream)
 
-    def new_state(self, B: int, Lmax: int, rope_cos: torch.Tensor, rope_sin: torch.Tensor, reserve: bool = True):
-        return DecodeState(self, B, Lmax, rope_cos, rope_sin, reserve)
+    def new_state(self, B: int, Lmax: int, rope_cos: torch.Tensor, rope_sin: torch.Tensor, reserve: bool = True, n_pages: int | None = None):
+        return DecodeState(self, B, Lmax, rope_cos, rope_sin, reserve, n_pages)
 
 
 class DecodeState:
-    """KV caches, workspace and step buffers for B sequences of up to Lmax tokens.  With an 8-bit cache `pages` holds pages for all of
-    them, reserved at once unless reserve is False."""
+    """KV caches, workspace and step buffers for B sequences of up to Lmax tokens.  With an 8-bit cache `pages` holds n_pages
+    pages (None: room for all of them), reserved at once unless reserve is False."""
 
-    def __init__(self, model: DecodeModel, B: int, Lmax: int, rope_cos, rope_sin, reserve: bool = True):
+    def __init__(self, model: DecodeModel, B: int, Lmax: int, rope_cos, rope_sin, reserve: bool = True, n_pages: int | None = None):
         c = model.cfg
         dev = model.embed.device
         self.model, self.B, self.Lmax = model, B, Lmax
@@ -108,7 +108,7 @@ class DecodeState:
         self.rope_cos, self.rope_sin = rope_cos, rope_sin
         if model.cache8:
             each = -(-Lmax // api.KV8_PAGE)
-            self.pages = KVPages(c.n_layers, B * each, c.Hkv, B, each, c.D, dev)
+            self.pages = KVPages(c.n_layers, B * each if n_pages is None else n_pages, c.Hkv, B, each, c.D, dev)
             if reserve:
                 self.pages.reserve(range(B), [Lmax] * B)
             self.kcache, self.vcache = list(self.pages.pool), [self.pages.table] * c.n_layers
@@ -250,7 +250,11 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
     T = int(lens_host.max()) + n_new - 1
     if rope_cos.shape[0] < T:
         raise ValueError("rope tables shorter than the run")
-    st = model.new_state(B * samples, T, rope_cos[:T].contiguous(), rope_sin[:T].contiguous(), reserve=samples == 1)
+    n_pages = None
+    if samples > 1:  # a prompt's full pages once, what is behind them for each continuation
+        full, each = lens_host // api.KV8_PAGE, -(-T // api.KV8_PAGE)
+        n_pages = int((full + samples * (each - full)).sum())
+    st = model.new_state(B * samples, T, rope_cos[:T].contiguous(), rope_sin[:T].contiguous(), reserve=samples == 1, n_pages=n_pages)
     if samples > 1:
         st.pages.reserve(range(0, B * samples, samples), lens_host.tolist(), stream=stream)
 
