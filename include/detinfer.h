@@ -496,9 +496,9 @@ int det_kv8_copy_pages(void *pool, int n_layers, int n_pages, int Hkv, int D, co
  * The order: q's (row, head) as integers n_d = rint(q_d 2^(22-E)), 2^E the power of two above its largest magnitude (E >= -100); n . c_j exact, brought to
  * fp32 from its digits to base 256.  Chunk c = tokens [256 c, 256 c + 256): in units of log2, m_c = ceil(max s_j), e_j = 2^(s_j - m_c) by the
  * hardware's exponential (the last product of s_j in one fma with the difference; rounded before it where |m_c| >= 2^24), l_c their sum in a fixed
- * order; a row whose largest score passes fp32 is NaN; weights e_j d^V_j as integers rint(w 2^(22-E_c)), 2^E_c above the chunk's largest;
- * their products with the codes exact.  Chunks are folded in ascending order, relative to the largest m so far.  A row's bytes do not depend
- * on R, on the other rows, on the pages it lies in or on the call's max_pages.
+ * order; a row whose largest score passes fp32 is NaN; weights e_j d^V_j as integers rint(w 2^(22-E_c)), 2^E_c above the chunk's largest
+ * (E_c >= -100: weights times scales below 2^-100 lose bits); their products with the codes exact.  Chunks are folded in ascending order, relative to
+ * the largest m so far.  A row's bytes do not depend on R, on the other rows, on the pages it lies in or on the call's max_pages.
  * Up to 895 (tile, KV head) pairs, a tile being 16 / (Hq/Hkv) rows, and wherever slots is NULL, chunks go to workgroups of their own and meet in ws in a
  * second launch; beyond, a tile of rows that name slots walks its chunks in one launch.  Rows that name slots are best given slot by slot.
  *   q, out [R, Hq, D] bf16;  Hq % Hkv == 0, Hq/Hkv <= 16;  scale > 0 and finite;  R <= 65535 if slots is NULL;  ws: det_attn_decode_kv8_workspace_bytes bytes, or

@@ -4,8 +4,12 @@
 //   scores   q of a (row, head) as a fixed-point number of 23 bits relative to its largest element, in three signed digits of base 256; digit
 //            sums are below 2^21 and exact in fp32.
 //   values   the weights w_j = e_j d^V_j of a chunk of 256 tokens as fixed-point numbers of 22 bits relative to the chunk's largest, three
-//            digits; a chunk's digit sums are below 2^22.  What a weight loses is at most 2^-22 of the largest one, whose own value
-//            the cache holds to half a code only.
+//            digits; a chunk's digit sums are below 2^22.  What a weight loses is at most 2^-22 of the chunk's largest, so a result is off by at
+//            most 2^-22 of the largest weight times its column's codes.  That is small beside the row, whose other columns hold that weight times codes up
+//            to 127, but not always beside a column in which the heaviest token's code is 0: relative to such a column the error is 3e-7 where all
+//            weights are of a size, 3e-4 where that token outweighs the others by 2^10, 2e-2 by 2^16 (a host model; bf16 rounds by 4e-3 at most).  The query
+//            likewise: an element of less than 2^-14 of the largest keeps fewer than its eight bits.  A fourth digit would need 16 KB of LDS more
+//            a workgroup of the walk, which then has a compute unit for itself.
 // Softmax: a chunk's reference m_c is an integer (the ceiling of its largest score in units of log2), so the factors by which chunks are
 // brought together are powers of two.  Chunks are folded in ascending order.
 //
@@ -13,6 +17,9 @@
 // calls of DET_KV8_WALK_TILES tiles and more, where the tiles alone fill most of the chip, walk their chunks in one launch.  Chunk by chunk against the
 // walk, rows of one slot, 32/8 heads: 256 rows before 8000 tokens (512 tiles) 215 and 223 us, 512 (1024) 380 and 226, 1000 rows of a prompt (2000) 137
 // and 35; slots of 100 rows at 100 to 2000 tokens (800) 69 and 97, of 64 rows at 100 to 1500 (1024) 73 and 47; 16/4 heads, 1000 rows (1000) 56 and 34.
+// The line knows tiles, not slots: calls of few rows a slot, whose tiles go alone, lose by the walk (slots of 200 to 2000 tokens, 32/8 heads: 128 of 9 rows
+// 225 and 170, 256 of 5 rows 291 and 227, but 300 of 3 rows 287 and 369, 600 of 2 rows 364 and 407, 500 of one row 323 and 632, with slots NULL 259; 16/4
+// heads: 128 of 9 rows 129 and 167, 256 of 5 rows 170 and 224, 300 of 3 rows 186 and 298).
 #include <type_traits>
 
 #include "geometry.h"
@@ -26,7 +33,6 @@ typedef __attribute__((__vector_size__(4 * sizeof(int)))) int v4i;
 constexpr int kChunk = 256;               // tokens of a chunk
 constexpr int kChunkPages = kChunk / kPage;
 constexpr int kPairs = 16;                // (row, head) pairs of a tile
-constexpr int kDigitStride = 80;          // bytes of a pair's 64 digits in LDS: padded, so that neither stores nor reads meet in a bank
 
 struct kv8_attn_args {
     const uint16_t* q;  // [R, Hq, 128]
