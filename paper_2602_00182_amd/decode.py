@@ -335,6 +335,8 @@ def _fill_prompts(model, st, prompts, lens_host, stream):
 def _speculative_decode(model, draft, prompts, prompt_lens, n_new, n_draft, uniforms, rope_cos, rope_sin, stream):
     B, dev, V, N = prompts.shape[0], prompts.device, model.cfg.V, n_draft
     lens_host = prompt_lens.cpu().to(torch.int64)
+    if int(lens_host.min()) < 1 or int(lens_host.max()) > prompts.shape[1]:
+        raise ValueError("a prompt's length outside 1..its row")
     T = int(lens_host.max()) + n_new + N  # the last token is drawn at position length + n_new - 1 at most, drafts behind it
     if rope_cos.shape[0] < T:
         raise ValueError("rope tables shorter than the run")

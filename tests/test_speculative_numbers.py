@@ -102,3 +102,12 @@ def test_one_request_of_numbers_a_round():
     _, counts = decode.speculative_decode(Table(even), Table(even), torch.zeros((2, 1), dtype=torch.int32), torch.ones(2, dtype=torch.int32), 8, 3,
                                           uniforms, cos, cos)
     assert asked == [(-1, (2, 2))] + [(t, (2, 7)) for t in range(len(counts))]
+
+
+@pytest.mark.parametrize("lens", [[0, 2], [2, -1], [3, 1]])
+def test_prompts_without_a_token_and_longer_than_their_rows_are_refused(lens):
+    """An empty prompt has no row whose logits its first token could be drawn from: it drew from a neighbour's."""
+    model, cos = Table([[0.25, 0.5, 0.25]] * V), torch.zeros(20, 1)
+    with pytest.raises(ValueError):
+        decode.speculative_decode(model, model, torch.zeros((2, 2), dtype=torch.int32), torch.tensor(lens, dtype=torch.int32), 3, 1,
+                                  lambda turn, shape: torch.full(shape, 0.5), cos, cos)
