@@ -262,6 +262,47 @@ int det_sample(const float *logits, int B, int V, float temperature, int top_k, 
                void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rules on logits, between the output head and det_argmax, det_sample or det_softmax_f32 (section 6.6: the decode policy is part of what the token is a
+ * function of).  Row b, token t, z = logits[b][t]; every step one rounded fp32 operation:
+ *   t occurs in the row's history:  z = z > 0 ? z / repetition : z * repetition;
+ *   c > 0 of its occurrences are generated ones (index generated_from[b] or behind):  z = (z - frequency * c) - presence;
+ *   t has an entry in the row's biases:  z = z + its value (several entries: the last one);
+ *   the bit of t in the row's mask is 0:  z = -inf.
+ * A token that no rule reaches keeps its bits.  A row whose mask allows nothing is -inf throughout: det_argmax gives 0 there.
+ * det_logits_rules: device pointers; the part whose first pointer is NULL is left out.
+ *   penalties [B, 3] fp32: repetition (> 0), frequency, presence.  history [n_history, ld_history] int32, of which row b has the first history_lens[b] ids
+ *   (0..ld_history) of row history_rows[b] (NULL: b; outside 0..n_history-1: none); ids outside 0..V-1 are ignored; generated_from [B] or NULL (0).
+ *   bias_begin [B + 1]: row b's entries are bias_begin[b] .. bias_begin[b+1]-1 of bias_tokens, bias_values [n_biases].
+ *   masks [n_masks, mask_words]: bit t % 32 of word t / 32; mask_rows [B]: the row's mask (NULL: b; outside 0..n_masks-1: none).
+ * logits, out [B, V] fp32 (DET_F32) or bf16 (DET_BF16: computed in fp32, rounded once) with row strides ld >= V in elements; out may be logits (with
+ * its stride), else the two may not overlap.  16-byte aligned (rows need not be).  B <= 65535, V <= 2^30, 32 mask_words >= V. */
+typedef struct det_logits_rules {
+    const float *penalties;
+    const int32_t *history;
+    const int32_t *history_rows;
+    const int32_t *history_lens;
+    const int32_t *generated_from;
+    const int32_t *bias_begin;
+    const int32_t *bias_tokens;
+    const float *bias_values;
+    const uint32_t *masks;
+    const int32_t *mask_rows;
+    int32_t ld_history, n_history, n_biases, n_masks, mask_words;
+} det_logits_rules;
+int det_logits_process(const void *logits, int64_t ld_logits, void *out, int64_t ld_out, int dtype, int B, int V,
+                       const det_logits_rules *rules /* host */, void *stream);
+
+/* What the rules need of a step, on the device: history[b][lens_in[b]] = tokens[b] and lens_out[b] = lens_in[b] + 1 (a full row stays as it is;
+ * history NULL: neither); states_out[b] = transitions[states_in[b]][class of tokens[b]], the class of a token token_class[token] (NULL: itself), -1 where
+ * the state, the token, its class or the next state is none (transitions NULL: left out).  A state is the mask_rows entry of the next step.
+ *   history [B, ld_history]; lens, states, tokens [B]; transitions [n_states, n_classes]; token_class [V], all int32.  lens_out may be lens_in, states_out
+ *   states_in. */
+int det_logits_advance(const int32_t *tokens, int32_t *history, int ld_history, const int32_t *lens_in,
+                       int32_t *lens_out, const int32_t *transitions, int n_states, int n_classes,
+                       const int32_t *token_class, int V, const int32_t *states_in, int32_t *states_out, int B,
+                       void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Elementwise steps of the decoder layer, exported so each can be checked bit for bit.
  *
  * det_rope: rotary embedding, rotate-half pairing (i, i + D/2), on nh heads of one token per row.
@@ -509,6 +550,41 @@ size_t det_attn_decode_kv8_rows_workspace_bytes(int R, int Hq, int Hkv, int D, i
 int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
                         int max_pages, const int32_t *seqlens, const int32_t *slots, void *out, void *ws, size_t ws_bytes,
                         int R, int Hq, int Hkv, int D, float scale, void *stream);
+
+/* det_attn_decode_kv8 for rows whose first tokens lie in the same pages (continuations of a prompt, a document that all requests begin with): the
+ * shared chunks are read once for a group of rows.  Group g: rows group_rows[g] .. group_rows[g+1]-1 (group_rows ascending; rows in no group are read for
+ * themselves), which hold their first shared[g] tokens in the same pages; of these the whole chunks of 256 tokens are read through the table of the
+ * group's first row, whatever the tables of its other rows name there.  A row may be shorter than what its group shares.
+ * Output bytes are those of det_attn_decode_kv8 (whose arguments, rules and errors hold; slots NULL or not), whatever the groups.
+ *   group_rows [n_groups + 1], shared [n_groups] int32;  0 <= n_groups <= R (n_groups = 0: both may be NULL);  R <= 65535;
+ *   ws: det_attn_decode_kv8_shared_workspace_bytes bytes. */
+size_t det_attn_decode_kv8_shared_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
+int det_attn_decode_kv8_shared(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
+                               int max_pages, const int32_t *seqlens, const int32_t *slots, const int32_t *group_rows,
+                               const int32_t *shared, int n_groups, void *out, void *ws, size_t ws_bytes, int R, int Hq,
+                               int Hkv, int D, float scale, void *stream);
+
+/* The same, and what weight each page of each slot got:
+ *   weights_out[s][i] = weights_in[s][i] + sum over the rows r that name slot s, the heads h and the tokens j of page i (64 i .. 64 i + 63) of p[r][h][j],
+ * p the softmax of row r and head h.  fp32, in a fixed order: for each row (ascending) and each quarter of the heads (ascending) into one of four sums,
+ * these in order, then onto weights_in.  A row whose softmax is not finite adds nothing.  Output bytes as above.
+ *   weights_in, weights_out [n_slots, max_pages] fp32, every entry written; weights_in NULL: zeros; the two may be the same array.  n_slots <= 65535.
+ *   ws: det_attn_decode_kv8_weights_workspace_bytes bytes. */
+size_t det_attn_decode_kv8_weights_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
+int det_attn_decode_kv8_weights(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
+                                int max_pages, const int32_t *seqlens, const int32_t *slots, const int32_t *group_rows,
+                                const int32_t *shared, int n_groups, const float *weights_in, float *weights_out,
+                                void *out, void *ws, size_t ws_bytes, int R, int Hq, int Hkv, int D, float scale,
+                                void *stream);
+
+/* Which pages the slots give up, by the weights that det_attn_decode_kv8_weights added up.  Slot s has ceil(lengths[s] / 64) pages (at most max_pages;
+ * none for a length below 1), of which those that its table names are there.  The first `first` and the last `recent` of them always stay.  Of the others
+ * that are there the max(0, pages there - keep[s]) with the smallest weight go, as far as there are so many; of equal weights the first pages go;
+ * a NaN is the smallest weight.  dropped[s][i] = 1 where page i goes, else 0 (every entry is written; the table is left as it is).
+ *   weights [n_slots, max_pages] fp32; lengths, keep [n_slots] int32 (a negative keep counts 0); dropped [n_slots, max_pages] bytes;  first, recent >= 0. */
+int det_kv8_pick_pages(const float *weights, const int32_t *page_table, int n_pages, int n_slots, int max_pages,
+                       const int32_t *lengths, const int32_t *keep, int first, int recent, uint8_t *dropped,
+                       void *stream);
 
 /* The decoder layers on the 8-bit cache: the steps of det_decoder_layer_rows and det_qdecoder_layer in the same order, with qkv in bf16,
  * det_kv8_rope_append and det_attn_decode_kv8 in place of the fused projection and the attention over a bf16 cache (the quantized layer's attention

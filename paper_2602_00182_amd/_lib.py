@@ -20,6 +20,12 @@ class LayerWeights(C.Structure):
                 ("w_norm2", C.c_void_p), ("wgu", C.c_void_p), ("wdown", C.c_void_p)]
 
 
+class LogitsRules(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("penalties", "history", "history_rows", "history_lens", "generated_from", "bias_begin", "bias_tokens",
+                                          "bias_values", "masks", "mask_rows")]
+    _fields_ += [(n, C.c_int32) for n in ("ld_history", "n_history", "n_biases", "n_masks", "mask_words")]
+
+
 class Sha256Ctx(C.Structure):
     _fields_ = [("h", C.c_uint32 * 8), ("nbytes", C.c_uint64), ("buf", C.c_uint8 * 64), ("fill", C.c_uint32)]
 
@@ -90,6 +96,13 @@ SIGNATURES = {
     "det_attn_decode_kv8_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "det_attn_decode_kv8_rows_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "det_attn_decode_kv8": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _i, _f, _vp]),
+    "det_attn_decode_kv8_shared_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "det_attn_decode_kv8_shared": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _sz, _i, _i, _i, _i, _f, _vp]),
+    "det_attn_decode_kv8_weights_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "det_attn_decode_kv8_weights": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _i, _f, _vp]),
+    "det_kv8_pick_pages": (_i, [_vp, _vp, _i, _i, _i, _vp, _vp, _i, _i, _vp, _vp]),
+    "det_logits_process": (_i, [_vp, _i64, _vp, _i64, _i, _i, _i, C.POINTER(LogitsRules), _vp]),
+    "det_logits_advance": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp]),
     "det_decoder_layer_kv8_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_decoder_layer_kv8_rows_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_decoder_layer_kv8": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,

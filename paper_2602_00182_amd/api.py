@@ -8,7 +8,7 @@ import ctypes as C
 
 import torch
 
-from ._lib import LayerCfg, LayerWeights, Sha256Ctx, lib
+from ._lib import LayerCfg, LayerWeights, LogitsRules, Sha256Ctx, lib
 
 __all__ = [
     "DetError", "det_gemm_bf16", "det_gemm_bf16_fixed_tile", "det_probe_lds_fill", "det_gemm_wide_rows", "det_gemm_tile", "det_qgemm_tile", "det_gemm_packed_b_bytes", "det_gemm_pack_b", "det_gemm_bf16_residual",
@@ -29,6 +29,8 @@ __all__ = [
     "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8_rows_workspace_bytes", "det_attn_decode_kv8",
     "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8_rows_workspace_bytes", "det_decoder_layer_kv8",
     "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8_rows_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts_workspace_bytes", "det_verify_drafts",
+    "det_attn_decode_kv8_shared_workspace_bytes", "det_attn_decode_kv8_shared", "det_attn_decode_kv8_weights_workspace_bytes",
+    "det_attn_decode_kv8_weights", "det_kv8_pick_pages", "logits_rules", "det_logits_process", "det_logits_advance",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -804,6 +806,64 @@ def det_attn_decode_kv8(q, pool, page_table, seqlens, slots, out, ws, scale: flo
         Hkv, D, scale, _stream(stream)))
 
 
+def det_attn_decode_kv8_shared_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_pages: int) -> int:
+    return lib().det_attn_decode_kv8_shared_workspace_bytes(R, Hq, Hkv, D, max_pages)
+
+
+def det_attn_decode_kv8_weights_workspace_bytes(R: int, Hq: int, Hkv: int, D: int, max_pages: int) -> int:
+    return lib().det_attn_decode_kv8_weights_workspace_bytes(R, Hq, Hkv, D, max_pages)
+
+
+def _groups(group_rows, shared):
+    """(group_rows, shared, n_groups) of a call; None and None: no groups."""
+    if group_rows is None and shared is None:
+        return None, None, 0
+    n, = shared.shape
+    if group_rows.shape != (n + 1,):
+        raise ValueError("n_groups + 1 first rows for the shared tokens of n_groups groups")
+    return _contig(group_rows, torch.int32), _contig(shared, torch.int32), n
+
+
+def det_attn_decode_kv8_shared(q, pool, page_table, seqlens, slots, group_rows, shared, out, ws, scale: float, stream=None) -> None:
+    """det_attn_decode_kv8, with the first shared[g] tokens of the rows group_rows[g] .. group_rows[g+1]-1, which lie in the same pages, read once."""
+    shape = R, Hq, D = q.shape
+    cache, Hkv = _kv8(pool, page_table)
+    if out.shape != shape or seqlens.shape != (R,):
+        raise ValueError("bad attention shapes")
+    bf16 = torch.bfloat16
+    _check("det_attn_decode_kv8_shared", lib().det_attn_decode_kv8_shared(
+        _contig(q, bf16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, cache[3]), *_groups(group_rows, shared), _contig(out, bf16),
+        _contig(ws), ws.nbytes, R, Hq, Hkv, D, scale, _stream(stream)))
+
+
+def det_attn_decode_kv8_weights(q, pool, page_table, seqlens, slots, group_rows, shared, weights_in, weights_out, out, ws, scale: float,
+                                stream=None) -> None:
+    """det_attn_decode_kv8_shared (group_rows and shared may be None), and weights_out [n_slots, max_pages] = weights_in (None: zeros) and what
+    weight each page got, summed over the rows that name the slot and their heads."""
+    shape = R, Hq, D = q.shape
+    cache, Hkv = _kv8(pool, page_table)
+    if out.shape != shape or seqlens.shape != (R,):
+        raise ValueError("bad attention shapes")
+    if weights_out.shape != page_table.shape or (weights_in is not None and weights_in.shape != page_table.shape):
+        raise ValueError("a weight for each entry of the page table")
+    bf16 = torch.bfloat16
+    _check("det_attn_decode_kv8_weights", lib().det_attn_decode_kv8_weights(
+        _contig(q, bf16), *cache, _contig(seqlens, torch.int32), _slots(slots, R, cache[3]), *_groups(group_rows, shared),
+        None if weights_in is None else _contig(weights_in, torch.float32), _contig(weights_out, torch.float32), _contig(out, bf16), _contig(ws),
+        ws.nbytes, R, Hq, Hkv, D, scale, _stream(stream)))
+
+
+def det_kv8_pick_pages(weights, page_table, n_pages: int, lengths, keep, first: int, recent: int, dropped, stream=None) -> None:
+    """dropped [n_slots, max_pages] (bytes): 1 for the pages of least weight that bring a slot of lengths[s] tokens back to keep[s] pages; the first
+    `first` and the last `recent` pages stay."""
+    shape = n_slots, max_pages = page_table.shape
+    if weights.shape != shape or dropped.shape != shape or lengths.shape != (n_slots,) or keep.shape != (n_slots,):
+        raise ValueError("bad page shapes")
+    _check("det_kv8_pick_pages", lib().det_kv8_pick_pages(
+        _contig(weights, torch.float32), _contig(page_table, torch.int32), n_pages, n_slots, max_pages, _contig(lengths, torch.int32),
+        _contig(keep, torch.int32), first, recent, _contig(dropped, torch.uint8), _stream(stream)))
+
+
 def det_decoder_layer_kv8_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int) -> int:
     return lib().det_decoder_layer_kv8_workspace_bytes(C.byref(cfg), R, max_pages)
 
@@ -864,3 +924,79 @@ def det_verify_drafts(p, q, drafts, n_drafts, u, accepted, tokens, ws=None, stre
         _contig(p, torch.float32), None if q is None else _contig(q, torch.float32), _contig(drafts, torch.int32),
         None if n_drafts is None else _contig(n_drafts, torch.int32), _contig(u, torch.float32), _contig(accepted, torch.int32),
         _contig(tokens, torch.int32), _contig(ws), ws.nbytes, B, N, V, _stream(stream)))
+
+
+def logits_rules(history=None, history_lens=None, history_rows=None, generated_from=None, penalties=None, bias_begin=None, bias_tokens=None,
+                 bias_values=None, masks=None, mask_rows=None) -> LogitsRules:
+    """The rules of det_logits_process over device tensors, which it keeps: what they hold when a call runs is what counts.
+    penalties [B, 3] fp32 (repetition, frequency, presence) over history [n, most] int32 with history_lens [B] (history_rows [B]: the row of history;
+    generated_from [B]: where a row's generated tokens begin); bias_begin [B + 1], bias_tokens, bias_values [entries]; masks [n, words] int32 (their 32 bits
+    are those of 32 tokens), mask_rows [B]."""
+    r, B = LogitsRules(), None
+
+    def rows(t, what):  # a tensor of one value a row of logits
+        nonlocal B
+        if t is None:
+            return None
+        n = t.shape[0] - (what == "bias_begin")
+        if t.dim() != 1 or (B is not None and n != B):
+            raise ValueError(f"{what}: one value for each row of logits")
+        B = n
+        return _contig(t, torch.int32)
+
+    if penalties is not None:
+        if history is None or history_lens is None or history.dim() != 2 or penalties.dim() != 2 or penalties.shape[1] != 3:
+            raise ValueError("penalties [B, 3] go with a history [n, most] and its lengths")
+        B = penalties.shape[0]
+        r.penalties, r.history = _contig(penalties, torch.float32), _contig(history, torch.int32)
+        r.n_history, r.ld_history = history.shape
+        r.history_lens, r.history_rows = rows(history_lens, "history_lens"), rows(history_rows, "history_rows")
+        r.generated_from = rows(generated_from, "generated_from")
+        if history_rows is None and r.n_history < B:
+            raise ValueError("fewer histories than rows")
+    if bias_begin is not None:
+        if bias_tokens is None or bias_values is None or bias_tokens.dim() != 1 or bias_values.shape != bias_tokens.shape:
+            raise ValueError("as many bias values as tokens")
+        r.bias_begin, r.n_biases = rows(bias_begin, "bias_begin"), bias_tokens.shape[0]
+        if r.n_biases > 0:
+            r.bias_tokens, r.bias_values = _contig(bias_tokens, torch.int32), _contig(bias_values, torch.float32)
+    if masks is not None:
+        if masks.dim() != 2:
+            raise ValueError("masks [n, words]")
+        r.masks, r.mask_rows = _contig(masks, torch.int32), rows(mask_rows, "mask_rows")
+        r.n_masks, r.mask_words = masks.shape
+    r._rows = B
+    r._tensors = (history, history_lens, history_rows, generated_from, penalties, bias_begin, bias_tokens, bias_values, masks, mask_rows)
+    return r
+
+
+def det_logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
+    """out [B, V] = logits with the rules (logits_rules) applied; fp32 or bf16, rows may have a stride; out may be logits."""
+    shape = B, V = logits.shape
+    dtype = logits.dtype
+    if out.shape != shape or out.dtype != dtype or logits.stride(1) != 1 or out.stride(1) != 1 or rules._rows not in (None, B):
+        raise ValueError("bad logits or rules of other rows")
+    _check("det_logits_process", lib().det_logits_process(
+        _ptr(logits), _ld(logits, V), _ptr(out), _ld(out, V), {torch.float32: DET_F32, torch.bfloat16: DET_BF16}[dtype], B, V, C.byref(rules),
+        _stream(stream)))
+
+
+def det_logits_advance(tokens, history, lens_in, lens_out, transitions=None, token_class=None, states_in=None, states_out=None, stream=None) -> None:
+    """tokens [B] go into history [B, most] at lens_in (lens_out: one more), and states_out = transitions[states_in, class of the token] ([n_states,
+    n_classes]; token_class [V], None: a token is its class).  history None or transitions None leaves a part out."""
+    B, = tokens.shape
+    i32 = torch.int32
+    most = V = n_states = n_classes = 0
+    if history is not None:
+        rows, most = history.shape
+        if rows != B or lens_in.shape != (B,) or lens_out.shape != (B,):
+            raise ValueError("bad history")
+    if transitions is not None:
+        n_states, n_classes = transitions.shape
+        V = n_classes if token_class is None else token_class.shape[0]
+        if states_in.shape != (B,) or states_out.shape != (B,) or (token_class is not None and token_class.dim() != 1):
+            raise ValueError("bad states")
+    opt = lambda t: None if t is None else _contig(t, i32)
+    _check("det_logits_advance", lib().det_logits_advance(
+        _contig(tokens, i32), opt(history), most, opt(lens_in), opt(lens_out), opt(transitions), n_states, n_classes, opt(token_class), V,
+        opt(states_in), opt(states_out), B, _stream(stream)))

@@ -63,6 +63,18 @@ int attn_decode_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
 // Workspace for attn_decode_kv8_impl of up to R rows.  named: its rows name slots, and calls of many of them keep nothing there.
 size_t attn_decode_kv8_workspace(int R, int Hq, int Hkv, int max_pages, bool named);
 
+// What a step over the cache is told beside its rows: groups of rows whose first pages are the same, and where the pages' weights go (null: nowhere).
+struct kv8_step {
+    const int32_t* group_rows;  // [n_groups + 1]
+    const int32_t* shared;      // [n_groups]: tokens
+    int n_groups;
+    const float* weights_in;    // [n_slots, max_pages] or null
+    float* weights_out;
+};
+int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset,
+                         const kv8_step& step, void* out, void* ws, size_t ws_bytes, int R, int Hq, int D, float scale, hipStream_t s);
+size_t attn_shared_kv8_workspace(int R, int Hq, int max_pages, bool weights);
+
 inline int kv8_check(const void* pool, const int32_t* table, int n_pages, int n_slots, int max_pages, int Hkv, int D)
 {
     if (!pool || !table || n_pages < 1 || n_slots < 1 || max_pages < 1 || Hkv < 1) return DET_EINVAL;
