@@ -554,7 +554,7 @@ int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_tab
 /* det_attn_decode_kv8 for rows whose first tokens lie in the same pages (continuations of a prompt, a document that all requests begin with): the
  * shared chunks are read once for a group of rows.  Group g: rows group_rows[g] .. group_rows[g+1]-1 (group_rows ascending; rows in no group are read for
  * themselves), which hold their first shared[g] tokens in the same pages; of these the whole chunks of 256 tokens are read through the table of the
- * group's first row, whatever the tables of its other rows name there.  A row may be shorter than what its group shares.
+ * group's first row, whatever the tables of its other rows of more than 256 tokens name there.  A row may be shorter than what its group shares.
  * Output bytes are those of det_attn_decode_kv8 (whose arguments, rules and errors hold; slots NULL or not), whatever the groups.
  *   group_rows [n_groups + 1], shared [n_groups] int32;  0 <= n_groups <= R (n_groups = 0: both may be NULL);  R <= 65535;
  *   ws: det_attn_decode_kv8_shared_workspace_bytes bytes. */
@@ -566,8 +566,7 @@ int det_attn_decode_kv8_shared(const void *q, const void *pool, const int32_t *p
 
 /* The same, and what weight each page of each slot got:
  *   weights_out[s][i] = weights_in[s][i] + sum over the rows r that name slot s, the heads h and the tokens j of page i (64 i .. 64 i + 63) of p[r][h][j],
- * p the softmax of row r and head h.  fp32, in a fixed order: for each row (ascending) and each quarter of the heads (ascending) into one of four sums,
- * these in order, then onto weights_in.  A row whose softmax is not finite adds nothing.  Output bytes as above.
+ * p the softmax of row r and head h.  fp32, in a fixed order: of each row (ascending) the heads (ascending) into the sum h mod 8, these eight in order, then onto weights_in.  A row whose softmax is not finite adds nothing.  Output bytes as above.
  *   weights_in, weights_out [n_slots, max_pages] fp32, every entry written; weights_in NULL: zeros; the two may be the same array.  n_slots <= 65535.
  *   ws: det_attn_decode_kv8_weights_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_weights_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);

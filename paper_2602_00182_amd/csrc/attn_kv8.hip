@@ -298,64 +298,6 @@ __global__ __launch_bounds__(128) void kv8_attn_combine_kernel(kv8_attn_args a)
     __builtin_nontemporal_store(to_bf16(o * row_factor(l)), &a.out[at * kHeadDim + threadIdx.x]);
 }
 
-// Scores to weights e d^V, in place, and what the fold needs of the chunk.  scales(p, dk, dv): those of this lane's tokens of page p.
-template <class Scales>
-__device__ __forceinline__ void softmax_weights(float (&s)[kChunkPages][4][4], const float (&factors)[4], Scales scales, float (&mc)[4],
-                                                float (&lc)[4], float (&up)[4], float (&unit)[4])
-{
-    float safe[4], sum[kChunkPages][4], top[4], f[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float x = -__builtin_inff();
-#pragma unroll
-        for (int p = 0; p < kChunkPages; ++p)
-#pragma unroll
-            for (int t = 0; t < 4; t += 2) x = max3(x, s[p][t][r], s[p][t + 1][r]);
-        x = row_max(x);
-        f[r] = seen_factor(x, factors[r]);
-        mc[r] = __builtin_ceilf(x * f[r]);
-        safe[r] = mc[r] == -__builtin_inff() ? 0.0f : mc[r];
-        top[r] = 0.0f;
-    }
-    if (__builtin_expect(__ballot(max3(max2(fabsf(safe[0]), fabsf(safe[1])), fabsf(safe[2]), fabsf(safe[3])) >= kFarScore) != 0, 0)) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-#pragma unroll
-            for (int p = 0; p < kChunkPages; ++p) {
-                float x[4] = {s[p][0][r], s[p][1][r], s[p][2][r], s[p][3][r]};
-                far_scores(x, f[r], safe[r]);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) s[p][t][r] = x[t];
-            }
-            if (fabsf(safe[r]) >= kFarScore) f[r] = 1.0f, safe[r] = 0.0f;
-        }
-    }
-#pragma unroll
-    for (int p = 0; p < kChunkPages; ++p) {
-        float dk[4], dv[4];
-        scales(p, dk, dv);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float e[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                e[t] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][t][r], f[r], -safe[r]));
-                s[p][t][r] = e[t] * dv[t];
-            }
-            top[r] = max3(max3(top[r], s[p][0][r], s[p][1][r]), s[p][2][r], s[p][3][r]);
-            sum[p][r] = (e[0] + e[1]) + (e[2] + e[3]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        lc[r] = row_sum((sum[0][r] + sum[1][r]) + (sum[2][r] + sum[3][r]));
-        const int e = exponent_above(row_max(top[r]));
-        up[r] = pow2i(22 - e);
-        unit[r] = pow2i(e - 22);
-    }
-}
-
 __device__ __forceinline__ void store_rows(const kv8_attn_args& a, int row0, int kvh, unsigned members, const float (&l)[4], const float (&o)[8][4])
 {
     const int lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
@@ -487,12 +429,6 @@ constexpr int walk_wait(int j)
     for (int k = 1; k < kRingAhead; ++k) n += (j + k) % kSteps < kChunkPages ? 3 : 2;
     return n;
 }
-template <int N>
-__device__ __forceinline__ void wait_loads_barrier()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
 __global__ __launch_bounds__(256, 2) void kv8_attn_walk_kernel(kv8_attn_args a)
 {
     __shared__ __attribute__((aligned(1024))) uint8_t ring[kRing * kStepBytes];

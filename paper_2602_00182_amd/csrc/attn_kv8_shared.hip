@@ -6,8 +6,11 @@
 //
 // The weight of a page: what the chunk's softmax sums to over its 64 tokens is kept beside the chunk's sums, and a last launch adds it up over the heads
 // once the row's largest score and sum are known.
+#include <type_traits>
+
 #include "attn_kv8.h"
 #include "geometry.h"
+#include "stream.h"
 
 namespace det {
 
@@ -16,7 +19,10 @@ struct kv8_shared_args : kv8_attn_args {
     const int32_t* shared;      // [n_groups]
     int n_groups;
     float4* page_sums;          // [R, Hq, chunks]: of each page of a chunk the sum of its e, or null
-    float2* row_stats;          // [R, Hq]: m and 1 / l
+    const float* weights_in;    // [n_slots, max_pages] or null
+    float* weights_out;
+    int group_wgs, group_steps; // workgroups of a KV head that take shared chunks; of them to a tile
+    int row_steps;              // workgroups of a KV head to a row
 };
 
 // ---------------------------------------------------------------- groups
@@ -77,21 +83,75 @@ __device__ __forceinline__ kv8_group tile_of_groups(const kv8_shared_args& a, in
     return kv8_group{0, 0, 0, 0};
 }
 
+// The groups' shared chunks times the sets of four tiles that read them, in all (below 2^30), and the place of number `at` among them: chunk c of
+// rows row0 .. row0 + rows - 1 of a group.
+__device__ __forceinline__ int sets_of(const kv8_shared_args& a, const kv8_group& g) { return (g.rows + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile); }
+__device__ __forceinline__ int chunks_of_groups(const kv8_shared_args& a)
+{
+    int all = 0;
+    for (int base = 0; base < a.n_groups; base += kWave) {
+        const kv8_group mine = group_at(a, base + (threadIdx.x & 63));
+        all += sets_of(a, mine) * mine.chunks;
+    }
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) all += __shfl_xor(all, off, kWave);
+    return __builtin_amdgcn_readfirstlane(all);
+}
+__device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, int at, int& chunk)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int base = 0; base < a.n_groups; base += kWave) {
+        const kv8_group mine = group_at(a, base + lane);
+        const int count = sets_of(a, mine) * mine.chunks;
+        int sum = count;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const int x = __shfl_up(sum, off, kWave);
+            sum += lane >= off ? x : 0;
+        }
+        const unsigned long long past = __ballot(before + sum > at);
+        if (past != 0) {
+            const int g = __builtin_ctzll(past);
+            kv8_group o{__builtin_amdgcn_readlane(mine.first, g), 0, __builtin_amdgcn_readlane(mine.rows, g), __builtin_amdgcn_readlane(mine.chunks, g)};
+            const int in = at - before - (__builtin_amdgcn_readlane(sum, g) - __builtin_amdgcn_readlane(count, g)), set = in / o.chunks;
+            chunk = in - set * o.chunks;
+            o.row0 = o.first + 4 * a.rows_per_tile * set;
+            o.rows = min(o.rows - 4 * a.rows_per_tile * set, 4 * a.rows_per_tile);
+            return o;
+        }
+        before += __builtin_amdgcn_readlane(sum, kWave - 1);
+    }
+    chunk = 0;
+    return kv8_group{0, 0, 0, 0};
+}
+
 // ---------------------------------------------------------------- chunks of a tile
 
 // Every step-th chunk from first_chunk on, below end_chunk, for `rows` rows from row0 on, all of which read the pages of slot `now`.  As
 // kv8_attn_chunk_kernel takes one (attn_kv8.hip): a page a wave for the scores, 32 columns a wave for the weighted sums.
-template <bool PACK, bool WEIGHTS>
-__device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, int kvh, int row0, int rows, int now, int first_chunk, int end_chunk, int step)
+template <bool PACK>
+struct tile_lds {
+    static constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
+    __attribute__((aligned(1024))) uint8_t digits[DIGITS * kPairs * kChunk];
+    float top[2][4][PAIRS];  // largest score, largest weight of each wave
+    float lsum[4][PAIRS][16];
+};
+
+template <bool PACK, bool WEIGHTS, bool GROUP>
+__device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int now, int first_chunk,
+                                               int end_chunk, int step)
 {
-    constexpr int NP = PACK ? 1 : 4;                 // pairs of a lane
-    constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
-    __shared__ __attribute__((aligned(1024))) uint8_t digits[DIGITS * kPairs * kChunk];
-    __shared__ float top[2][4][PAIRS];               // largest score, largest weight of each wave
-    __shared__ float lsum[4][PAIRS][16];
+    constexpr int NP = PACK ? 1 : 4;  // pairs of a lane
+    constexpr int DIGITS = tile_lds<PACK>::DIGITS;
+    tile_lds<PACK>& shared = *reinterpret_cast<tile_lds<PACK>*>(lds);
+    auto& digits = shared.digits;
+    auto& top = shared.top;
+    auto& lsum = shared.lsum;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
     int slot, len = 0;
     if (col < rows * a.G) len = row_length(a, row0 + pair_row(a, col), slot);
+    if (GROUP && len <= kChunk) len = 0;  // such a row is read for itself
     int longest = len;
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
@@ -265,14 +325,11 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, int kvh
             float o[2];
 #pragma unroll
             for (int n = 0; n < 2; ++n) o[n] = PACK ? digits_value(acc[0][n][0], acc[0][n][1], acc[0][n][2]) : digits_value(acc[0][n][r], acc[PACK ? 0 : 1][n][r], acc[PACK ? 0 : 2][n][r]);
-            if (lens[r] <= kChunk) {  // the row's only chunk
+            if (!GROUP && lens[r] <= kChunk) {  // the row's only chunk
                 float fm = -__builtin_inff(), l = 0.0f, fa, fb;
                 fold_step(fm, l, mc[r], lc, unit[r], fa, fb);
                 const float by = row_factor(l);
-                if (WEIGHTS && wave == 0 && col == 0) {
-                    a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
-                    a.row_stats[head] = make_float2(fm, by);
-                }
+                if (WEIGHTS && wave == 0 && col == 0) a.part[at] = make_float4(mc[r], lc, unit[r], 0.0f);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) __builtin_nontemporal_store(to_bf16(fold_value(0.0f, o[n], fa, fb) * by), &a.out[head * kHeadDim + 32 * wave + 16 * n + col]);
             } else {
@@ -284,41 +341,293 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, int kvh
     }
 }
 
-// The chunks that a group's rows share.  Grid (KV heads x chunk_step, tiles of all groups).
-template <bool WEIGHTS>
-__global__ __launch_bounds__(256, 2) void kv8_shared_tile_kernel(kv8_shared_args a)
+// ---------------------------------------------------------------- chunks of four tiles
+
+// As kv8_attn_walk_kernel (attn_kv8.hip) brings chunks through a ring of LDS slots, a tile a wave; but a chunk's sums go to memory, so nothing is kept
+// from chunk to chunk and any run of chunks can be a workgroup's.  Stores are held back until the next step's barrier and stand in front of its loads: a
+// step's wait, which counts the loads behind it, then waits for no load that was asked for later.
+constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = kRecordV;  // slots, steps in flight, bytes of a slot
+constexpr int kSteps = 2 * kChunkPages;                                  // of a chunk: its pages' K codes, then quarters of its V codes
+constexpr int kRingScales = 2 * kChunkPages * 512 + 512;                 // two chunks' (K, V of each page); what no one reads
+constexpr int kRingLds = kRing * kStepBytes + 4 * kChunkDigits + kRingScales;
+
+constexpr int ring_wait(int j)  // loads of the steps behind step j (3 for K codes, 2 for V codes)
 {
-    const int kvh = blockIdx.x % a.c.Hkv, first = blockIdx.x / a.c.Hkv;
-    const kv8_group tile = tile_of_groups(a, blockIdx.y);
-    if (first >= tile.chunks) return;
-    // the pages are those of the group's first row
-    const int now = a.slots ? a.slots[tile.first] : tile.first;
-    chunks_of_tile<false, WEIGHTS>(a, kvh, tile.row0, tile.rows, now, first, tile.chunks, a.chunk_step);
+    int n = 0;
+    for (int k = 1; k < kRingAhead; ++k) n += (j + k) % kSteps < kChunkPages ? 3 : 2;
+    return n;
 }
 
-// What a row has behind them.  Grid (KV heads x chunk_step, rows).
-template <bool PACK, bool WEIGHTS>
-__global__ __launch_bounds__(256, PACK ? 3 : 2) void kv8_shared_row_kernel(kv8_shared_args a)
+// Chunks c0 .. c1 - 1 of slot `now` for `rows` rows from row0 on, at most four tiles.
+template <bool WEIGHTS>
+__device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int now, int c0, int c1)
 {
-    const int kvh = blockIdx.x % a.c.Hkv, nth = blockIdx.x / a.c.Hkv, row = blockIdx.y;
+    uint8_t* const ring = lds;
+    uint8_t* const scales = lds + kRing * kStepBytes + 4 * kChunkDigits;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
+    uint8_t* const digits = lds + kRing * kStepBytes + wave * kChunkDigits;
+    const int my_row0 = row0 + wave * a.rows_per_tile, my_rows = min(max(rows - wave * a.rows_per_tile, 0), a.rows_per_tile);
+    const int in_tile = pair_row(a, col);
+    const bool live = col < my_rows * a.G;
+    int slot, len = 0;
+    if (live) len = row_length(a, my_row0 + in_tile, slot);
+    if (len <= kChunk) len = 0;  // such a row is read for itself
+    uint32_t words[16];
+    ask_query(live ? a.q + ((size_t)(my_row0 + in_tile) * a.Hq + kvh * a.G + col - in_tile * a.G) * kHeadDim : nullptr, words);
+    int mine = len, least = len > 0 ? len : 0x7FFFFFFF;
+    int lens[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) lens[r] = __shfl(len, 4 * group + r, kWave);
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+        mine = max(mine, __shfl_xor(mine, off, kWave));
+        least = min(least, __shfl_xor(least, off, kWave));
+    }
+    const int my_longest = __builtin_amdgcn_readfirstlane(mine), my_shortest = __builtin_amdgcn_readfirstlane(least);
+
+    // what this wave brings of a step: two blocks of 1 KB, of V codes those of one page; and with K codes one of the page's rows of scales
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_char_t*)ring, scales_at = (uint32_t)(uintptr_t)(lds_char_t*)scales;
+    uint32_t key_from[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int c = 8 * b + (lane >> 3);  // LDS row 16 wave + c: token 4 c + wave
+        key_from[b] = 512 * c + 128 * wave + 16 * ((lane & 7) ^ (c >> 1));
+    }
+    // of sixteen tokens 32 columns, of the next sixteen too: the even columns in front of the odd ones, so that a lane's two are neighbours in memory
+    const uint32_t value_from = kRecordV + 2048 * (lane >> 5) + 32 * (lane & 15) + 16 * ((lane >> 4) & 1);
+    const uint32_t scale_from = kRecordKs + 256 * (wave & 1) + 4 * lane;
+    // where it reads: a K row's piece, a V operand
+    const uint32_t key_at = 128 * col + 16 * (group ^ (col >> 1)), value_at = 512 * group + 16 * col;
+
+    // records of a chunk; where a page is missing, any (its tokens are masked)
+    auto look_up = [&](int chunk, const uint8_t* (&rec)[kChunkPages + 1]) {
+        unsigned gone = 0;
+        rec[kChunkPages] = a.c.pool;
+#pragma unroll
+        for (int p = 0; p < kChunkPages; ++p) {
+            const uint8_t* at = chunk < c1 ? kv8_record_uniform(a.c, now, chunk * kChunkPages + p, kvh) : nullptr;
+            gone |= at ? 0u : 1u << p;
+            rec[p] = at ? at : a.c.pool;
+            rec[kChunkPages] = p == wave ? rec[p] : rec[kChunkPages];  // the page whose V codes this wave brings
+        }
+        return gone;
+    };
+    // step j of a chunk with the records rec, into ring slot `to`
+    auto bring = [&](int j, const uint8_t* const (&rec)[kChunkPages + 1], int chunk, int to) {
+        const uint8_t* from = rec[j < kChunkPages ? j : kChunkPages];
+        const uint32_t at = ring_at + to * kStepBytes + 2048 * wave;
+        if (j < kChunkPages) {
+            dma_block(from, key_from[0], at);
+            dma_block(from, key_from[1], at + 1024);
+            dma_words(from, scale_from, wave < 2 ? scales_at + ((chunk & 1) * kChunkPages + j) * 512 + 256 * wave
+                                                 : scales_at + 2 * kChunkPages * 512 + 256 * (wave - 2));
+        } else {
+            dma_block(from + 512 * (j - kChunkPages), value_from, at);
+            dma_block(from + 512 * (j - kChunkPages) + 4096, value_from, at + 1024);
+        }
+    };
+    const uint8_t *rec[kChunkPages + 1], *next[kChunkPages + 1];
+    unsigned gone = look_up(c0, rec);
+    int place = 0;  // ring slot of the step at hand
+#pragma unroll
+    for (int j = 0; j < kRingAhead; ++j) bring(j, rec, c0, j);
+    q_digits qd[2];  // while they are on their way
+    float factor, factors[4];
+    cut_query(words, a.scale_log2, qd, factor);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
+    const v4i zero = {0, 0, 0, 0};
+    size_t heads[4];  // of the chunks' sums of each pair, from chunk 0 on
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int p = 4 * group + r, row = pair_row(a, p);
+        heads[r] = ((size_t)(my_row0 + row) * a.Hq + kvh * a.G + p - row * a.G) * a.chunks;
+    }
+    float o[2][4];       // held back: two columns of each pair
+    int o_chunk = -1;    // their chunk
+    auto flush = [&](int j) {  // those of step j
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (lens[r] > o_chunk * kChunk)
+                *reinterpret_cast<float2*>(a.part_o + (heads[r] + o_chunk) * kHeadDim + 32 * (j - kChunkPages) + 2 * col) = make_float2(o[0][r], o[1][r]);
+    };
+    for (int chunk = c0; chunk < c1; ++chunk) {
+        const unsigned next_gone = look_up(chunk + 1, next);
+        int here = lane;  // unknown to the compiler: what follows from it is not kept in registers over the loop
+        asm volatile("" : "+v"(here));
+        const bool busy = chunk * kChunk < my_longest;
+        const int pages = min(kChunkPages, (my_longest - chunk * kChunk + kPage - 1) / kPage);  // of this wave's rows
+        float mc[4], lc[4], up[4], unit[4], sums[kChunkPages][4];
+        auto arrive = [&](auto step) {
+            constexpr int j = decltype(step)::value;
+            wait_loads_barrier<ring_wait(j)>();
+            if (j == 0) {
+                if (o_chunk >= 0) flush(kSteps - 1);
+                o_chunk = -1;
+            } else if (j == kChunkPages) {
+                if (busy && (here & 15) < 4) {
+                    const int r = here & 3;
+                    auto of = [&](const float (&x)[4]) { return r < 2 ? (r == 0 ? x[0] : x[1]) : (r == 2 ? x[2] : x[3]); };
+                    const size_t at = (r < 2 ? (r == 0 ? heads[0] : heads[1]) : (r == 2 ? heads[2] : heads[3])) + chunk;
+                    const int its = r < 2 ? (r == 0 ? lens[0] : lens[1]) : (r == 2 ? lens[2] : lens[3]);
+                    if (its > chunk * kChunk) {
+                        a.part[at] = make_float4(of(mc), of(lc), of(unit), 0.0f);
+                        if (WEIGHTS) a.page_sums[at] = make_float4(of(sums[0]), of(sums[1]), of(sums[2]), of(sums[3]));
+                    }
+                }
+            } else if (j > kChunkPages) {
+                if (busy) flush(j - 1);
+            }
+            const int to = place == 0 ? kRing - 1 : place - 1;
+            if (j + kRingAhead < kSteps) bring((j + kRingAhead) % kSteps, rec, chunk, to);
+            else bring((j + kRingAhead) % kSteps, next, chunk + 1, to);
+            const uint8_t* codes = ring + place * kStepBytes;
+            place = place + 1 == kRing ? 0 : place + 1;
+            return codes;
+        };
+        const uint8_t* chunk_scales = scales + (chunk & 1) * kChunkPages * 512;
+        float s[kChunkPages][4][4];  // page, token 4 col + t, pair
+        auto keys = [&](auto step) {
+            constexpr int p = decltype(step)::value;
+            const uint8_t* codes = arrive(step);
+            if (!busy || p >= pages) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[p][t][r] = 0.0f;
+                return;
+            }
+            float dk[4], dv[4];
+            clean_scales(chunk_scales + 512 * p, col, dk, dv);
+            v4i d[4][3];
+#pragma unroll
+            for (int two = 0; two < 4; two += 2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = two; t < two + 2; ++t) {
+                        const v4i k = *reinterpret_cast<const v4i*>(codes + (h ? key_at ^ 64u : key_at) + 2048 * t);
+#pragma unroll
+                        for (int g = 0; g < 3; ++g) d[t][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[h].d[g], k, h ? d[t][g] : zero, 0, 0, 0);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[p][t][r] = score_of(d[t][0][r], d[t][1][r], d[t][2][r], dk[t]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        keys(std::integral_constant<int, 0>{});
+        keys(std::integral_constant<int, 1>{});
+        keys(std::integral_constant<int, 2>{});
+        keys(std::integral_constant<int, 3>{});
+        if (busy) {
+            if ((chunk + 1) * kChunk > my_shortest || gone != 0) {
+#pragma unroll
+                for (int p = 0; p < kChunkPages; ++p)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const int token = (gone >> p) & 1u ? 0x7FFFFFFF : chunk * kChunk + p * kPage + 4 * (here & 15) + t;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? s[p][t][r] : -__builtin_inff();
+                    }
+            }
+            softmax_weights<WEIGHTS>(s, factors, [&](int p, float (&dk)[4], float (&dv)[4]) { clean_scales(chunk_scales + 512 * p, col, dk, dv); }, mc, lc, up,
+                                     unit, sums);
+            store_digits(s, up, digits, here);
+        }
+        auto values = [&](auto step) {
+            const uint8_t* codes = arrive(step);
+            if (!busy) return;
+            v4i acc[3][2];
+#pragma unroll
+            for (int p = 0; p < kChunkPages; ++p) {
+                if (p < pages) {
+                    v4i w[3];
+#pragma unroll
+                    for (int g = 0; g < 3; ++g) w[g] = load_digits(digits, g, p, here);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const v4i v = *reinterpret_cast<const v4i*>(codes + value_at + 2048 * p + 256 * n);
+#pragma unroll
+                        for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, p == 0 ? zero : acc[g][n], 0, 0, 0);
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[n][r] = digits_value(acc[0][n][r], acc[1][n][r], acc[2][n][r]);
+            o_chunk = chunk;
+        };
+        values(std::integral_constant<int, 4>{});
+        values(std::integral_constant<int, 5>{});
+        values(std::integral_constant<int, 6>{});
+        values(std::integral_constant<int, 7>{});
+        gone = next_gone;
+#pragma unroll
+        for (int p = 0; p <= kChunkPages; ++p) rec[p] = next[p];
+    }
+    if (o_chunk >= 0) flush(kSteps - 1);
+    // the steps asked for past the last chunk have to land before the ring begins anew
+    wait_loads_barrier<0>();
+}
+
+// ---------------------------------------------------------------- the launches
+
+// Grid: workgroups of shared chunks, then row_steps of every row; neighbours take the KV heads of one page, whose records lie side by side.
+// kRuns: four tiles go through a run of chunks together.  All chunks of all groups, one behind the other, are cut into group_wgs equal runs.
+// kTiles: a workgroup takes every group_steps-th chunk of a tile.  PACK: a row's up to four heads a KV head.
+enum { kNoGroups, kTiles, kRuns };
+template <int FORM, bool PACK, bool WEIGHTS>
+__global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_shared_kernel(kv8_shared_args a)
+{
+    constexpr int kTileLds = FORM == kNoGroups ? sizeof(tile_lds<PACK>) : sizeof(tile_lds<false>);
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[FORM == kRuns && kRingLds > kTileLds ? kRingLds : kTileLds];
+    const int kvh = blockIdx.x % a.c.Hkv;
+    int nth = blockIdx.x / a.c.Hkv;
+    if (FORM != kNoGroups && nth < a.group_wgs) {
+        if constexpr (FORM == kRuns) {
+            const long long all = chunks_of_groups(a);
+            int at = (int)(all * nth / a.group_wgs);
+            const int to = (int)(all * (nth + 1) / a.group_wgs);
+            while (at < to) {
+                int c0;
+                const kv8_group tiles = place_in_groups(a, at, c0);
+                if (tiles.chunks == 0) return;
+                const int c1 = min(tiles.chunks, c0 + to - at);
+                chunks_of_tiles<WEIGHTS>(a, lds, kvh, tiles.row0, tiles.rows, a.slots ? a.slots[tiles.first] : tiles.first, c0, c1);
+                at += c1 - c0;
+            }
+        } else {
+            const kv8_group tile = tile_of_groups(a, nth / a.group_steps);
+            const int first = nth % a.group_steps;
+            if (first >= tile.chunks) return;
+            // the pages are those of the group's first row
+            chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks, a.group_steps);
+        }
+        return;
+    }
+    if (FORM != kNoGroups) nth -= a.group_wgs;
+    const int row = nth / a.row_steps, first = nth % a.row_steps;
     int slot;
     const int len = row_length(a, row, slot);
     if (len == 0) {
-        if (nth == 0)
+        if (first == 0)
             for (int i = threadIdx.x; i < a.G * kHeadDim / 2; i += kBlock)
                 reinterpret_cast<uint32_t*>(a.out + ((size_t)row * a.Hq + kvh * a.G) * kHeadDim)[i] = 0u;
         return;
     }
-    const int behind = a.group_rows ? group_of_row(a, row).chunks : 0;
-    chunks_of_tile<PACK, WEIGHTS>(a, kvh, row, 1, slot, behind + nth, a.chunks, a.chunk_step);
+    const int behind = FORM != kNoGroups && len > kChunk ? group_of_row(a, row).chunks : 0;
+    chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, row, 1, slot, behind + first, a.chunks, a.row_steps);
 }
 
-// The chunks of one (row, head) of more than one chunk, folded in ascending order: kv8_attn_combine_kernel (attn_kv8.hip) and what the weights need.
-template <bool WEIGHTS>
-__global__ __launch_bounds__(128) void kv8_shared_combine_kernel(kv8_shared_args a)
+// The chunks of one (row, head) of more than one chunk, folded in ascending order, one column a thread.  As kv8_attn_combine_kernel (attn_kv8.hip).
+__device__ __forceinline__ void combine_head(const kv8_shared_args& a, size_t at)
 {
     constexpr int kBlockChunks = 16;
-    const size_t at = blockIdx.x;
     int slot;
     const int len = row_length(a, (int)(at / a.Hq), slot);
     if (len <= kChunk) return;
@@ -351,50 +660,73 @@ __global__ __launch_bounds__(128) void kv8_shared_combine_kernel(kv8_shared_args
         if (c0 + 2 * kBlockChunks < chunks) ask(x[0], c0 + 2 * kBlockChunks);
         fold(x[1], c0 + kBlockChunks);
     }
-    const float by = row_factor(l);
-    if (WEIGHTS && threadIdx.x == 0) a.row_stats[at] = make_float2(m, by);
-    __builtin_nontemporal_store(to_bf16(o * by), &a.out[at * kHeadDim + threadIdx.x]);
+    __builtin_nontemporal_store(to_bf16(o * row_factor(l)), &a.out[at * kHeadDim + threadIdx.x]);
 }
 
 // ---------------------------------------------------------------- the pages' weights
 
-// weights_out[slot] = weights_in[slot] + what the pages get from the rows that name the slot.  Grid (blocks of 64 chunks, slots); a lane has a chunk, a
-// wave a quarter of the heads.  Sums in a fixed order: rows ascending, of a row each quarter's heads ascending, then the four quarters.  A
-// row whose softmax is not finite adds nothing.
-__global__ __launch_bounds__(256) void kv8_page_weights_kernel(kv8_shared_args a, const float* weights_in, float* weights_out)
+// weights_out[slot] = weights_in[slot] + what sixteen chunks' pages get from the rows that name the slot.  A thread has one chunk and every eighth
+// head; the rows' largest scores and sums are folded here again, beside the heads' own workgroups instead of behind them.  Sums in a fixed order:
+// of each eighth the rows ascending and in a row its heads, then the eighths.  A row whose softmax is not finite adds nothing.
+constexpr int kWeightChunks = 16, kWeightParts = 8, kCombineThreads = kWeightChunks * kWeightParts;
+struct weights_lds {
+    float2 stats[kCombineThreads];
+    float4 parts[kWeightParts - 1][kWeightChunks];
+};
+__device__ __forceinline__ void page_weights(const kv8_shared_args& a, weights_lds& lds, int slot, int block)
 {
-    __shared__ float4 quarter[3][kWave];
-    const int slot = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, chunk = blockIdx.x * kWave + lane;
-    const int each = (a.Hq + 3) / 4, h0 = wave * each, h1 = min(a.Hq, h0 + each);
+    const int tid = threadIdx.x, part = tid / kWeightChunks, chunk = block * kWeightChunks + tid % kWeightChunks;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     auto add_row = [&](int row) {
         int its;
-        const int len = row_length(a, row, its);
-        if (its != slot || chunk * kChunk >= len) return;
-#pragma unroll 8
-        for (int h = h0; h < h1; ++h) {
-            const size_t head = (size_t)row * a.Hq + h, at = head * a.chunks + chunk;
-            const float2 st = a.row_stats[head];
-            const float by = pow2_step(a.part[at].x, st.x) * st.y;
-            if (!(by < __builtin_inff())) continue;
-            const float4 e = a.page_sums[at];
-            sum.x = __builtin_fmaf(e.x, by, sum.x);
-            sum.y = __builtin_fmaf(e.y, by, sum.y);
-            sum.z = __builtin_fmaf(e.z, by, sum.z);
-            sum.w = __builtin_fmaf(e.w, by, sum.w);
+        const int len = row_length(a, row, its), chunks = (len + kChunk - 1) / kChunk;
+        if (its != slot || block * kWeightChunks >= chunks) return;
+        for (int h0 = 0; h0 < a.Hq; h0 += kCombineThreads) {
+            __syncthreads();
+            if (h0 + tid < a.Hq) {
+                const float4* ps = a.part + ((size_t)row * a.Hq + h0 + tid) * a.chunks;
+                float m = -__builtin_inff(), l = 0.0f, fa, fb;
+                for (int c0 = 0; c0 < chunks; c0 += 8) {
+                    float4 st[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) st[k] = ps[min(c0 + k, chunks - 1)];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (c0 + k < chunks) fold_step(m, l, st[k].x, st[k].y, st[k].z, fa, fb);
+                }
+                lds.stats[tid] = make_float2(m, row_factor(l));
+            }
+            __syncthreads();
+            if (chunk >= chunks) continue;
+            const int count = min(a.Hq - h0, kCombineThreads);
+#pragma unroll 4
+            for (int h = part; h < count; h += kWeightParts) {
+                const size_t at = ((size_t)row * a.Hq + h0 + h) * a.chunks + chunk;
+                const float2 st = lds.stats[h];
+                const float4 e = a.page_sums[at];
+                float by = pow2_step(a.part[at].x, st.x) * st.y;
+                const bool fine = by < __builtin_inff();
+                sum.x = fine ? __builtin_fmaf(e.x, by, sum.x) : sum.x;
+                sum.y = fine ? __builtin_fmaf(e.y, by, sum.y) : sum.y;
+                sum.z = fine ? __builtin_fmaf(e.z, by, sum.z) : sum.z;
+                sum.w = fine ? __builtin_fmaf(e.w, by, sum.w) : sum.w;
+            }
         }
     };
     if (!a.slots) {
         if (slot < a.R) add_row(slot);
     } else {
-        for (int row = 0; row < a.R; ++row) add_row(row);
+        for (int r0 = 0; r0 < a.R; r0 += kWave) {
+            const int r = r0 + (tid & 63);
+            for (unsigned long long some = __ballot(r < a.R && a.slots[r] == slot); some != 0; some &= some - 1) add_row(r0 + __builtin_ctzll(some));
+        }
     }
-    if (wave > 0) quarter[wave - 1][lane] = sum;
+    if (part > 0) lds.parts[part - 1][tid % kWeightChunks] = sum;
     __syncthreads();
-    if (wave > 0) return;
+    if (part > 0) return;
 #pragma unroll
-    for (int w = 0; w < 3; ++w) {
-        const float4 x = quarter[w][lane];
+    for (int w = 0; w < kWeightParts - 1; ++w) {
+        const float4 x = lds.parts[w][tid];
         sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
     }
     const float of[4] = {sum.x, sum.y, sum.z, sum.w};
@@ -403,28 +735,42 @@ __global__ __launch_bounds__(256) void kv8_page_weights_kernel(kv8_shared_args a
         const int page = chunk * kChunkPages + p;
         if (page >= a.c.max_pages) continue;
         const size_t at = (size_t)slot * a.c.max_pages + page;
-        weights_out[at] = (weights_in ? weights_in[at] : 0.0f) + of[p];
+        a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.0f) + of[p];
+    }
+}
+
+// Grid (R * Hq) of a column a thread; before them, if the pages are weighed, (blocks of chunks, slots).
+template <bool WEIGHTS>
+__global__ __launch_bounds__(kCombineThreads) void kv8_shared_combine_kernel(kv8_shared_args a, int weight_blocks)
+{
+    static_assert(kCombineThreads == kHeadDim);
+    if constexpr (WEIGHTS) {
+        __shared__ weights_lds lds;
+        if ((int)blockIdx.x < weight_blocks * a.c.n_slots) {
+            page_weights(a, lds, blockIdx.x / weight_blocks, blockIdx.x % weight_blocks);
+            return;
+        }
+        combine_head(a, blockIdx.x - (size_t)weight_blocks * a.c.n_slots);
+    } else {
+        combine_head(a, blockIdx.x);
     }
 }
 
 // ---------------------------------------------------------------- host
 
-struct kv8_shared_ws {
-    size_t part, page_sums, row_stats, total;
-};
+static size_t shared_chunks(int R, int Hq, int max_pages) { return (size_t)R * Hq * (((size_t)max_pages + kChunkPages - 1) / kChunkPages); }
 
-static kv8_shared_ws shared_ws(int R, int Hq, int max_pages, bool weights)
+size_t attn_shared_kv8_workspace(int R, int Hq, int max_pages, bool weights)
 {
-    kv8_shared_ws w{};
-    const size_t heads = (size_t)R * Hq, all = heads * (((size_t)max_pages + kChunkPages - 1) / kChunkPages);
-    w.part = all * kHeadDim * sizeof(float);
-    w.page_sums = w.part + all * sizeof(float4);
-    w.row_stats = w.page_sums + (weights ? all * sizeof(float4) : 0);
-    w.total = w.row_stats + (weights ? heads * sizeof(float2) : 0);
-    return w;
+    return shared_chunks(R, Hq, max_pages) * (kHeadDim * sizeof(float) + (weights ? 2 : 1) * sizeof(float4));
 }
 
-size_t attn_shared_kv8_workspace(int R, int Hq, int max_pages, bool weights) { return shared_ws(R, Hq, max_pages, weights).total; }
+template <int FORM, bool PACK>
+static void launch_shared(const kv8_shared_args& a, bool weights, unsigned grid, hipStream_t s)
+{
+    if (weights) hipLaunchKernelGGL((kv8_shared_kernel<FORM, PACK, true>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv8_shared_kernel<FORM, PACK, false>), dim3(grid), dim3(256), 0, s, a);
+}
 
 int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* seqlens, const int32_t* slots, int len_offset,
                          const kv8_step& step, void* out, void* ws, size_t ws_bytes, int R, int Hq, int D, float scale, hipStream_t s)
@@ -438,19 +784,17 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     const bool weights = step.weights_out != nullptr;
     if (weights && cache.n_slots > 65535) return DET_ESHAPE;
     if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return DET_EALIGN;
-    const kv8_shared_ws w = shared_ws(R, Hq, cache.max_pages, weights);
-    if (ws_bytes < w.total) return DET_EWORKSPACE;
-    char* base = static_cast<char*>(ws);
+    if (ws_bytes < attn_shared_kv8_workspace(R, Hq, cache.max_pages, weights)) return DET_EWORKSPACE;
+    const size_t all = shared_chunks(R, Hq, cache.max_pages);
     kv8_shared_args a{};
     a.q = static_cast<const uint16_t*>(q);
     a.c = cache;
     a.seqlens = seqlens;
     a.slots = slots;
     a.out = static_cast<uint16_t*>(out);
-    a.part_o = reinterpret_cast<float*>(base);
-    a.part = reinterpret_cast<float4*>(base + w.part);
-    a.page_sums = weights ? reinterpret_cast<float4*>(base + w.page_sums) : nullptr;
-    a.row_stats = weights ? reinterpret_cast<float2*>(base + w.row_stats) : nullptr;
+    a.part_o = static_cast<float*>(ws);
+    a.part = reinterpret_cast<float4*>(a.part_o + all * kHeadDim);
+    a.page_sums = a.part + all;
     a.R = R;
     a.Hq = Hq;
     a.G = Hq / cache.Hkv;
@@ -459,37 +803,42 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     a.len_offset = len_offset;
     a.chunks = (cache.max_pages + kChunkPages - 1) / kChunkPages;
     a.scale_log2 = scale * 1.44269504f;
-    a.group_rows = step.n_groups > 0 ? step.group_rows : nullptr;
+    a.group_rows = step.group_rows;
     a.shared = step.shared;
     a.n_groups = step.n_groups;
-    if ((long long)R * Hq > 0x7FFFFFFFll / 128) return DET_ESHAPE;
-    auto share_out = [&](long long tiles) {
-        const long long room = DET_KV8_CHUNK_WGS / (tiles * cache.Hkv);
-        a.chunk_step = room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
-        return dim3((unsigned)(a.chunk_step * cache.Hkv), (unsigned)tiles);
+    a.weights_in = step.weights_in;
+    a.weights_out = step.weights_out;
+    // workgroups between which a row's, or a tile's, chunks are shared out
+    auto steps = [&](long long rows, long long wgs) {
+        const long long room = wgs / (rows * cache.Hkv);
+        return room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
     };
+    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_TAIL_WGS : DET_KV8_CHUNK_WGS);
+    bool ring = false;
     if (step.n_groups > 0) {
-        // a group of n rows has at most n / rows_per_tile + 1 tiles, and at most n
-        const long long tiles = R / a.rows_per_tile + step.n_groups < R ? R / a.rows_per_tile + step.n_groups : R;
-        const dim3 grid = share_out(tiles);
-        if (weights) hipLaunchKernelGGL(kv8_shared_tile_kernel<true>, grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(kv8_shared_tile_kernel<false>, grid, dim3(256), 0, s, a);
+        ring = (long long)R * a.G > (long long)DET_KV8_RING_PAIRS * step.n_groups;
+        if (ring) {
+            a.group_wgs = DET_KV8_RING_WGS / cache.Hkv < 1 ? 1 : DET_KV8_RING_WGS / cache.Hkv;
+        } else {
+            // a group of n rows has at most n / rows_per_tile + 1 tiles, and at most n
+            const long long tiles = R / a.rows_per_tile + step.n_groups < R ? R / a.rows_per_tile + step.n_groups : R;
+            a.group_steps = steps(tiles, DET_KV8_CHUNK_WGS);
+            if (tiles * a.group_steps > 0x3FFFFFFFll) return DET_ESHAPE;
+            a.group_wgs = (int)(tiles * a.group_steps);
+        }
     }
-    const dim3 grid = share_out(R);
-    if (a.G <= 4) {
-        if (weights) hipLaunchKernelGGL((kv8_shared_row_kernel<true, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((kv8_shared_row_kernel<true, false>), grid, dim3(256), 0, s, a);
-    } else {
-        if (weights) hipLaunchKernelGGL((kv8_shared_row_kernel<false, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((kv8_shared_row_kernel<false, false>), grid, dim3(256), 0, s, a);
-    }
-    if (a.chunks > 1) {
-        if (weights) hipLaunchKernelGGL(kv8_shared_combine_kernel<true>, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);
-        else hipLaunchKernelGGL(kv8_shared_combine_kernel<false>, dim3((unsigned)(R * Hq)), dim3(128), 0, s, a);
-    }
-    if (weights)
-        hipLaunchKernelGGL(kv8_page_weights_kernel, dim3((unsigned)((a.chunks + kWave - 1) / kWave), (unsigned)cache.n_slots), dim3(256), 0, s, a,
-                           step.weights_in, step.weights_out);
+    const long long grid = (a.group_wgs + (long long)R * a.row_steps) * cache.Hkv, blocks = weights ? (a.chunks + kWeightChunks - 1) / kWeightChunks : 0,
+                    second = blocks * cache.n_slots + (long long)R * Hq;
+    if (grid > 0x7FFFFFFFll / 256 || second > 0x7FFFFFFFll / kCombineThreads) return DET_ESHAPE;
+    auto launch = [&](auto form) {
+        if (a.G <= 4) launch_shared<decltype(form)::value, true>(a, weights, (unsigned)grid, s);
+        else launch_shared<decltype(form)::value, false>(a, weights, (unsigned)grid, s);
+    };
+    if (ring) launch(std::integral_constant<int, kRuns>{});
+    else if (step.n_groups > 0) launch(std::integral_constant<int, kTiles>{});
+    else launch(std::integral_constant<int, kNoGroups>{});
+    if (weights) hipLaunchKernelGGL(kv8_shared_combine_kernel<true>, dim3((unsigned)second), dim3(kCombineThreads), 0, s, a, (int)blocks);
+    else if (a.chunks > 1) hipLaunchKernelGGL(kv8_shared_combine_kernel<false>, dim3((unsigned)second), dim3(kCombineThreads), 0, s, a, 0);
     return check_launch();
 }
 

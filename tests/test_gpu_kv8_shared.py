@@ -162,6 +162,46 @@ def test_what_the_first_rows_table_names_counts(d):
     assert same_bytes(grouped(d, q, pool, table, lens, up(c.group_rows), up(c.shared)), plain(d, q, pool, table, lens))
 
 
+RAGGED = [
+    ("two groups", [1024, 512], [[1025 + 3 * i for i in range(33)], [513 + i for i in range(41)]]),
+    ("groups of all sizes", [768, 0, 512, 256, 1536], [[770] * 35, [300, 20], [513 + i for i in range(70)], [900, 257, 300], [1537 + 5 * i for i in range(64)]]),
+    ("rows that end inside", [1280], [[1280] + [1 + 31 * i for i in range(60)]]),
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 2), (9, 3), (8, 2), (5, 1), (16, 2), (16, 1)])
+@pytest.mark.parametrize("what,common,lengths", RAGGED, ids=[s[0] for s in RAGGED])
+def test_groups_of_many_rows(d, what, common, lengths, Hq, Hkv):
+    """Runs of chunks that begin and end anywhere in a group; pages given up in some of them, tokens that are not finite in others."""
+    c = SharedCache(720 + Hq, Hkv, common, lengths)
+    rng = np.random.default_rng(Hq)
+    for g, n in enumerate(common):
+        b, e = c.group_rows[g], c.group_rows[g + 1]
+        away = rng.choice(n // PAGE, n // PAGE // 4, replace=False) if n else []
+        c.table[b:e, away] = -1
+    c.table[c.group_rows[0]:c.group_rows[1], 4:8] = -1
+    last = c.group_rows[-2]
+    if common[-1] >= 512 and len(common) > 2:
+        parts(c.pool)[3][c.table[last][c.table[last] >= 0][3], 0, 9] = np.inf  # all rows of the last group see it
+    bits = ds.normal_bf16(721 + Hq, (len(c.lengths), Hq, D), 1.5)
+    bits[7, Hq - 1, 3] = 0xFF80
+    bits[11] = ds.f32_to_bf16_bits(ds.bf16_bits_to_f32(bits[11]) * np.float32(2.0 ** 36))
+    q, pool, table, lens = up_bf16(bits), up(c.pool), up(c.table), up(np.asarray(c.lengths, np.int32))
+    rows, shared = up(c.group_rows), up(c.shared)
+    step(f"{what}, {Hq}/{Hkv} heads")
+    want = plain(d, q, pool, table, lens)
+    assert same_bytes(grouped(d, q, pool, table, lens, rows, shared), want)
+    out, weights = weighed(d, q, pool, table, lens, None, rows, shared)
+    alone, others = weighed(d, q, pool, table, lens, None)
+    assert same_bytes(out, want) and same_bytes(alone, want) and torch.equal(weights, others)
+    assert torch.isfinite(weights).all() and not weights[table < 0].any()
+    perm = torch.randperm(len(c.lengths), device=DEV)  # the slots in another order, named by the rows
+    inverse = torch.argsort(perm)
+    slots = inverse.to(torch.int32)
+    out, weights = weighed(d, q, pool, table[perm].contiguous(), lens, None, rows, shared, slots)
+    assert same_bytes(out, want) and torch.equal(weights, others[perm])
+
+
 def test_missing_pages_and_slots_that_are_none(d):
     """Pages given up weigh nothing, whole chunks of them too; rows without any page, slot or token give zeros and add nothing."""
     c = SharedCache(800, 2, [1024], [[1100, 1200, 1300, 1024]])

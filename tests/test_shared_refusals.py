@@ -74,7 +74,7 @@ def test_rules_that_are_refused(change, rules, code):
 
 def test_sizes():
     assert d.det_attn_decode_kv8_shared_workspace_bytes(3, 32, 8, 128, 9) == d.det_attn_decode_kv8_workspace_bytes(3, 32, 8, 128, 9)
-    assert d.det_attn_decode_kv8_weights_workspace_bytes(3, 32, 8, 128, 9) == 3 * 32 * (3 * (132 + 4) + 2) * 4
+    assert d.det_attn_decode_kv8_weights_workspace_bytes(3, 32, 8, 128, 9) == 3 * 32 * 3 * (132 + 4) * 4
     for of in (d.det_attn_decode_kv8_shared_workspace_bytes, d.det_attn_decode_kv8_weights_workspace_bytes):
         assert of(1, 32, 8, 64, 4) == 0 and of(1, 32, 7, 128, 4) == 0 and of(1, 34, 2, 128, 4) == 0 and of(1, 32, 8, 128, 131073) == 0 and of(0, 32, 8, 128, 4) == 0
         assert of(65535, 128, 8, 128, 131072) > 1 << 40  # no 32-bit product
