@@ -343,29 +343,39 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
 
 // ---------------------------------------------------------------- chunks of four tiles
 
-// As kv8_attn_walk_kernel (attn_kv8.hip) brings chunks through a ring of LDS slots, a tile a wave; but a chunk's sums go to memory, so nothing is kept
-// from chunk to chunk and any run of chunks can be a workgroup's.  Stores are held back until the next step's barrier and stand in front of its loads: a
-// step's wait, which counts the loads behind it, then waits for no load that was asked for later.
-constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = kRecordV;  // slots, steps in flight, bytes of a slot
-constexpr int kSteps = 2 * kChunkPages;                                  // of a chunk: its pages' K codes, then quarters of its V codes
+// A wave has a tile, and the four go through a run of chunks together: a chunk's eight pages of codes, of K and then of V, 8 KB each, come by LDS-DMA
+// through a ring of six slots, five in flight, one barrier a page.  A chunk's sums go to memory, so nothing is kept from chunk to chunk and any run of
+// chunks can be a workgroup's.  All 128 columns are summed at once (96 sums a lane), page by page: a page's digits are cut while the page in front of it is
+// multiplied, and two pages' of them are all that LDS holds.
+//
+// K rows and their scales lie in LDS as in kv8_attn_walk_kernel (attn_kv8.hip).  V: column 64 h + 4 c + i of sixteen tokens at [h][i][c], so that a lane
+// ends with four neighbouring columns of a pair, twice.  Digits: the 64 bytes of pair p at row 4 (p % 4) + p / 4, their sixteen-byte pieces swizzled by
+// p % 4: neither writes nor reads meet in a bank.
+//
+// A chunk's results are stored during the next one's K pages, in front of a page's loads: a wait, which counts the loads behind the page it waits for, then
+// waits for no load that was asked for later.
+constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = 2 * kRecordV;  // slots, steps in flight, bytes of a slot
+constexpr int kSteps = kChunkPages;                                          // of a chunk: two pages each, K codes and then V codes
+constexpr int kPageDigits = 3 * kPairs * kPage;                          // bytes
 constexpr int kRingScales = 2 * kChunkPages * 512 + 512;                 // two chunks' (K, V of each page); what no one reads
-constexpr int kRingLds = kRing * kStepBytes + 4 * kChunkDigits + kRingScales;
+struct pair_notes {  // of a wave's sixteen pairs, kept out of the registers
+    float factor[kPairs];
+    int len[kPairs], head[kPairs];
+};
+constexpr int kRingLds = kRing * kStepBytes + 8 * kPageDigits + kRingScales + 4 * sizeof(pair_notes);
 
-constexpr int ring_wait(int j)  // loads of the steps behind step j (3 for K codes, 2 for V codes)
-{
-    int n = 0;
-    for (int k = 1; k < kRingAhead; ++k) n += (j + k) % kSteps < kChunkPages ? 3 : 2;
-    return n;
-}
+// Loads of the step behind step j (three a page for K codes, two for V codes).
+constexpr int ring_wait(int j) { return (j + 1) % kSteps < kSteps / 2 ? 6 : 4; }
 
 // Chunks c0 .. c1 - 1 of slot `now` for `rows` rows from row0 on, at most four tiles.
 template <bool WEIGHTS>
 __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int now, int c0, int c1)
 {
     uint8_t* const ring = lds;
-    uint8_t* const scales = lds + kRing * kStepBytes + 4 * kChunkDigits;
+    uint8_t* const scales = lds + kRing * kStepBytes + 8 * kPageDigits;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
-    uint8_t* const digits = lds + kRing * kStepBytes + wave * kChunkDigits;
+    uint8_t* const digits = lds + kRing * kStepBytes + 2 * kPageDigits * wave;
+    pair_notes& notes = reinterpret_cast<pair_notes*>(scales + kRingScales)[wave];
     const int my_row0 = row0 + wave * a.rows_per_tile, my_rows = min(max(rows - wave * a.rows_per_tile, 0), a.rows_per_tile);
     const int in_tile = pair_row(a, col);
     const bool live = col < my_rows * a.G;
@@ -375,9 +385,6 @@ __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_
     uint32_t words[16];
     ask_query(live ? a.q + ((size_t)(my_row0 + in_tile) * a.Hq + kvh * a.G + col - in_tile * a.G) * kHeadDim : nullptr, words);
     int mine = len, least = len > 0 ? len : 0x7FFFFFFF;
-    int lens[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) lens[r] = __shfl(len, 4 * group + r, kWave);
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) {
         mine = max(mine, __shfl_xor(mine, off, kWave));
@@ -385,7 +392,7 @@ __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_
     }
     const int my_longest = __builtin_amdgcn_readfirstlane(mine), my_shortest = __builtin_amdgcn_readfirstlane(least);
 
-    // what this wave brings of a step: two blocks of 1 KB, of V codes those of one page; and with K codes one of the page's rows of scales
+    // what this wave brings of a step: two blocks of 1 KB; and with K codes one of the page's rows of scales
     const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_char_t*)ring, scales_at = (uint32_t)(uintptr_t)(lds_char_t*)scales;
     uint32_t key_from[2];
 #pragma unroll
@@ -393,138 +400,178 @@ __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_
         const int c = 8 * b + (lane >> 3);  // LDS row 16 wave + c: token 4 c + wave
         key_from[b] = 512 * c + 128 * wave + 16 * ((lane & 7) ^ (c >> 1));
     }
-    // of sixteen tokens 32 columns, of the next sixteen too: the even columns in front of the odd ones, so that a lane's two are neighbours in memory
-    const uint32_t value_from = kRecordV + 2048 * (lane >> 5) + 32 * (lane & 15) + 16 * ((lane >> 4) & 1);
+    const uint32_t value_from = kRecordV + 2048 * wave + 64 * (lane & 15) + 16 * (lane >> 4);  // sixteen tokens of 64 columns, of the other 64 too
     const uint32_t scale_from = kRecordKs + 256 * (wave & 1) + 4 * lane;
     // where it reads: a K row's piece, a V operand
-    const uint32_t key_at = 128 * col + 16 * (group ^ (col >> 1)), value_at = 512 * group + 16 * col;
+    const uint32_t key_at = 128 * col + 16 * (group ^ (col >> 1)), value_at = 2048 * group + 16 * col;
 
-    // records of a chunk; where a page is missing, any (its tokens are masked)
-    auto look_up = [&](int chunk, const uint8_t* (&rec)[kChunkPages + 1]) {
+    // records of a chunk; where a page is missing, any (its tokens are masked).  The table's entries of sixteen chunks are asked for at once, one a lane.
+    int entries = -1;
+    auto look_up = [&](int chunk, const uint8_t* (&rec)[kChunkPages]) {
+        if ((chunk - c0) % 16 == 0) {
+            const int page = chunk * kChunkPages + lane;
+            entries = (unsigned)now < (unsigned)a.c.n_slots && page < min(c1 * kChunkPages, a.c.max_pages) ? a.c.table[(size_t)now * a.c.max_pages + page] : -1;
+        }
         unsigned gone = 0;
-        rec[kChunkPages] = a.c.pool;
 #pragma unroll
         for (int p = 0; p < kChunkPages; ++p) {
-            const uint8_t* at = chunk < c1 ? kv8_record_uniform(a.c, now, chunk * kChunkPages + p, kvh) : nullptr;
-            gone |= at ? 0u : 1u << p;
-            rec[p] = at ? at : a.c.pool;
-            rec[kChunkPages] = p == wave ? rec[p] : rec[kChunkPages];  // the page whose V codes this wave brings
+            const int page = __builtin_amdgcn_readlane(entries, (chunk - c0) % 16 * kChunkPages + p);
+            const bool there = chunk < c1 && (unsigned)page < (unsigned)a.c.n_pages;
+            gone |= there ? 0u : 1u << p;
+            rec[p] = a.c.pool + (there ? ((size_t)page * a.c.Hkv + kvh) * kRecord : 0);
         }
         return gone;
     };
     // step j of a chunk with the records rec, into ring slot `to`
-    auto bring = [&](int j, const uint8_t* const (&rec)[kChunkPages + 1], int chunk, int to) {
-        const uint8_t* from = rec[j < kChunkPages ? j : kChunkPages];
-        const uint32_t at = ring_at + to * kStepBytes + 2048 * wave;
-        if (j < kChunkPages) {
-            dma_block(from, key_from[0], at);
-            dma_block(from, key_from[1], at + 1024);
-            dma_words(from, scale_from, wave < 2 ? scales_at + ((chunk & 1) * kChunkPages + j) * 512 + 256 * wave
-                                                 : scales_at + 2 * kChunkPages * 512 + 256 * (wave - 2));
-        } else {
-            dma_block(from + 512 * (j - kChunkPages), value_from, at);
-            dma_block(from + 512 * (j - kChunkPages) + 4096, value_from, at + 1024);
+    auto bring = [&](int j, const uint8_t* const (&rec)[kChunkPages], int chunk, int to) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int p = 2 * (j % 2) + i;
+            const uint8_t* from = rec[p];
+            const uint32_t at = ring_at + to * kStepBytes + kRecordV * i + 2048 * wave;
+            if (j < kSteps / 2) {
+                dma_block(from, key_from[0], at);
+                dma_block(from, key_from[1], at + 1024);
+                dma_words(from, scale_from, wave < 2 ? scales_at + ((chunk & 1) * kChunkPages + p) * 512 + 256 * wave
+                                                     : scales_at + 2 * kChunkPages * 512 + 256 * (wave - 2));
+            } else {
+                dma_block(from, value_from, at);
+                dma_block(from + 1024, value_from, at + 1024);
+            }
         }
     };
-    const uint8_t *rec[kChunkPages + 1], *next[kChunkPages + 1];
+    const uint8_t *rec[kChunkPages], *next[kChunkPages];
     unsigned gone = look_up(c0, rec);
     int place = 0;  // ring slot of the step at hand
 #pragma unroll
     for (int j = 0; j < kRingAhead; ++j) bring(j, rec, c0, j);
     q_digits qd[2];  // while they are on their way
-    float factor, factors[4];
+    float factor;
     cut_query(words, a.scale_log2, qd, factor);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) factors[r] = __shfl(factor, 4 * group + r, kWave);
-    const v4i zero = {0, 0, 0, 0};
-    size_t heads[4];  // of the chunks' sums of each pair, from chunk 0 on
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int p = 4 * group + r, row = pair_row(a, p);
-        heads[r] = ((size_t)(my_row0 + row) * a.Hq + kvh * a.G + p - row * a.G) * a.chunks;
+    if (lane < kPairs) {
+        notes.factor[lane] = factor;
+        notes.len[lane] = len;
+        notes.head[lane] = (my_row0 + in_tile) * a.Hq + kvh * a.G + lane - in_tile * a.G;
     }
-    float o[2][4];       // held back: two columns of each pair
-    int o_chunk = -1;    // their chunk
-    auto flush = [&](int j) {  // those of step j
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (lens[r] > o_chunk * kChunk)
-                *reinterpret_cast<float2*>(a.part_o + (heads[r] + o_chunk) * kHeadDim + 32 * (j - kChunkPages) + 2 * col) = make_float2(o[0][r], o[1][r]);
+    wave_lds_order();
+    const v4i zero = {0, 0, 0, 0};
+    float o[4][8];     // held back: two times four columns of each pair
+    int o_chunk = -1;  // their chunk
+    auto flush = [&](int r) {
+        if (o_chunk < 0 || notes.len[4 * group + r] <= o_chunk * kChunk) return;
+        float* to = a.part_o + ((size_t)notes.head[4 * group + r] * a.chunks + o_chunk) * kHeadDim + 4 * col;
+        *reinterpret_cast<float4*>(to) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+        *reinterpret_cast<float4*>(to + 64) = make_float4(o[r][4], o[r][5], o[r][6], o[r][7]);
     };
-    for (int chunk = c0; chunk < c1; ++chunk) {
+    // BUSY: the chunk lies in front of the end of this wave's longest row; else the wave only brings what the others need
+    auto pass = [&](int chunk, auto is_busy) {
+        constexpr bool busy = decltype(is_busy)::value;
         const unsigned next_gone = look_up(chunk + 1, next);
         int here = lane;  // unknown to the compiler: what follows from it is not kept in registers over the loop
         asm volatile("" : "+v"(here));
-        const bool busy = chunk * kChunk < my_longest;
-        const int pages = min(kChunkPages, (my_longest - chunk * kChunk + kPage - 1) / kPage);  // of this wave's rows
         float mc[4], lc[4], up[4], unit[4], sums[kChunkPages][4];
-        auto arrive = [&](auto step) {
+        const uint8_t* codes = ring;
+        auto arrive = [&](auto step) {  // the step's codes
             constexpr int j = decltype(step)::value;
             wait_loads_barrier<ring_wait(j)>();
-            if (j == 0) {
-                if (o_chunk >= 0) flush(kSteps - 1);
+            if constexpr (j == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) flush(r);
                 o_chunk = -1;
-            } else if (j == kChunkPages) {
+            } else if constexpr (j == 2) {
                 if (busy && (here & 15) < 4) {
                     const int r = here & 3;
                     auto of = [&](const float (&x)[4]) { return r < 2 ? (r == 0 ? x[0] : x[1]) : (r == 2 ? x[2] : x[3]); };
-                    const size_t at = (r < 2 ? (r == 0 ? heads[0] : heads[1]) : (r == 2 ? heads[2] : heads[3])) + chunk;
-                    const int its = r < 2 ? (r == 0 ? lens[0] : lens[1]) : (r == 2 ? lens[2] : lens[3]);
-                    if (its > chunk * kChunk) {
+                    const int p = 4 * (here >> 4) + r;
+                    if (notes.len[p] > chunk * kChunk) {
+                        const size_t at = (size_t)notes.head[p] * a.chunks + chunk;
                         a.part[at] = make_float4(of(mc), of(lc), of(unit), 0.0f);
                         if (WEIGHTS) a.page_sums[at] = make_float4(of(sums[0]), of(sums[1]), of(sums[2]), of(sums[3]));
                     }
                 }
-            } else if (j > kChunkPages) {
-                if (busy) flush(j - 1);
             }
             const int to = place == 0 ? kRing - 1 : place - 1;
-            if (j + kRingAhead < kSteps) bring((j + kRingAhead) % kSteps, rec, chunk, to);
-            else bring((j + kRingAhead) % kSteps, next, chunk + 1, to);
-            const uint8_t* codes = ring + place * kStepBytes;
+            if constexpr (j + kRingAhead < kSteps) bring(j + kRingAhead, rec, chunk, to);
+            else bring(j + kRingAhead - kSteps, next, chunk + 1, to);
+            codes = ring + place * kStepBytes;
             place = place + 1 == kRing ? 0 : place + 1;
-            return codes;
         };
         const uint8_t* chunk_scales = scales + (chunk & 1) * kChunkPages * 512;
         float s[kChunkPages][4][4];  // page, token 4 col + t, pair
-        auto keys = [&](auto step) {
-            constexpr int p = decltype(step)::value;
-            const uint8_t* codes = arrive(step);
-            if (!busy || p >= pages) {
+        // K codes half a page at a time: while one half is multiplied the one before it becomes scores
+        v4i k[2][4], d[2][2][3];
+        float dk[2][4];
+        auto ask_keys = [&](auto half) {
+            constexpr int i = decltype(half)::value, p = i / 2;
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[p][t][r] = 0.0f;
-                return;
+                for (int h = 0; h < 2; ++h)
+                    k[i & 1][2 * t + h] = *reinterpret_cast<const v4i*>(codes + p % 2 * kRecordV + (h ? key_at ^ 64u : key_at) + 2048 * (2 * (i & 1) + t));
+        };
+        auto ask_page_scales = [&](int p) {
+            const float4 ks = *reinterpret_cast<const float4*>(chunk_scales + 512 * p + 16 * col);
+            const float4 vs = *reinterpret_cast<const float4*>(chunk_scales + 512 * p + 16 * col + (kRecordVs - kRecordKs));
+            // poisoned where the token's V row is not finite, as clean_scales does it
+            dk[p & 1][0] = __builtin_fmaf(vs.x, 0.0f, ks.x), dk[p & 1][1] = __builtin_fmaf(vs.y, 0.0f, ks.y);
+            dk[p & 1][2] = __builtin_fmaf(vs.z, 0.0f, ks.z), dk[p & 1][3] = __builtin_fmaf(vs.w, 0.0f, ks.w);
+        };
+        auto scores = [&](auto half) {
+            constexpr int i = decltype(half)::value, p = i / 2, two = 2 * (i & 1);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[p][two + t][r] = score_of(d[i & 1][t][0][r], d[i & 1][t][1][r], d[i & 1][t][2][r], dk[p & 1][two + t]);
+        };
+        auto keys = [&](auto half) {
+            constexpr int i = decltype(half)::value, p = i / 2;
+            if constexpr (i % 4 == 0) {
+                arrive(std::integral_constant<int, i / 4>{});
+                if constexpr (busy) ask_keys(half);
             }
-            float dk[4], dv[4];
-            clean_scales(chunk_scales + 512 * p, col, dk, dv);
-            v4i d[4][3];
-#pragma unroll
-            for (int two = 0; two < 4; two += 2) {
+            if constexpr (busy) {
+                if constexpr (i % 2 == 0) ask_page_scales(p);
+                if constexpr (i % 4 != 3) ask_keys(std::integral_constant<int, i + 1>{});
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int t = two; t < two + 2; ++t) {
-                        const v4i k = *reinterpret_cast<const v4i*>(codes + (h ? key_at ^ 64u : key_at) + 2048 * t);
+                    for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int g = 0; g < 3; ++g) d[t][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[h].d[g], k, h ? d[t][g] : zero, 0, 0, 0);
+                        for (int g = 0; g < 3; ++g)
+                            d[i & 1][t][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qd[h].d[g], k[i & 1][2 * t + h], h ? d[i & 1][t][g] : zero, 0, 0, 0);
+                if constexpr (i > 0) {
+                    scores(std::integral_constant<int, i - 1>{});
+#pragma unroll
+                    for (int n = 0; n < 12; ++n) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
                     }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[p][t][r] = score_of(d[t][0][r], d[t][1][r], d[t][2][r], dk[t]);
-                __builtin_amdgcn_sched_barrier(0);
+                }
             }
         };
         keys(std::integral_constant<int, 0>{});
         keys(std::integral_constant<int, 1>{});
         keys(std::integral_constant<int, 2>{});
         keys(std::integral_constant<int, 3>{});
-        if (busy) {
+        keys(std::integral_constant<int, 4>{});
+        keys(std::integral_constant<int, 5>{});
+        keys(std::integral_constant<int, 6>{});
+        keys(std::integral_constant<int, 7>{});
+        if constexpr (busy) scores(std::integral_constant<int, 7>{});
+        auto cut_page = [&](int p) {
+            uint8_t* at = digits + (p & 1) * kPageDigits + 64 * (here >> 4) + 4 * (here & 3);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t b[3];
+                cut_weights(s[p], r, up[r], b);
+#pragma unroll
+                for (int g = 0; g < 3; ++g) *reinterpret_cast<uint32_t*>(at + g * kPairs * kPage + 256 * r + 16 * (((here & 15) >> 2) ^ r)) = b[g];
+            }
+        };
+        if constexpr (busy) {
             if ((chunk + 1) * kChunk > my_shortest || gone != 0) {
+                const int4 of = *reinterpret_cast<const int4*>(&notes.len[4 * (here >> 4)]);
+                const int lens[4] = {of.x, of.y, of.z, of.w};
 #pragma unroll
                 for (int p = 0; p < kChunkPages; ++p)
 #pragma unroll
@@ -534,43 +581,66 @@ __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_
                         for (int r = 0; r < 4; ++r) s[p][t][r] = token < lens[r] ? s[p][t][r] : -__builtin_inff();
                     }
             }
-            softmax_weights<WEIGHTS>(s, factors, [&](int p, float (&dk)[4], float (&dv)[4]) { clean_scales(chunk_scales + 512 * p, col, dk, dv); }, mc, lc, up,
-                                     unit, sums);
-            store_digits(s, up, digits, here);
+            const float4 of_pairs = *reinterpret_cast<const float4*>(&notes.factor[4 * (here >> 4)]);
+            const float factors[4] = {of_pairs.x, of_pairs.y, of_pairs.z, of_pairs.w};
+            auto value_scales = [&](int p, float (&)[4], float (&dv)[4]) {
+                const float4 vs = *reinterpret_cast<const float4*>(chunk_scales + 512 * p + 16 * col + (kRecordVs - kRecordKs));
+                const float of[4] = {vs.x, vs.y, vs.z, vs.w};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) dv[t] = fabsf(of[t]) < __builtin_inff() ? of[t] : 0.0f;
+            };
+            softmax_weights<WEIGHTS>(s, factors, value_scales, mc, lc, up, unit, sums);
+            wave_lds_order();
+            cut_page(0);
+            wave_lds_order();
         }
-        auto values = [&](auto step) {
-            const uint8_t* codes = arrive(step);
-            if (!busy) return;
-            v4i acc[3][2];
+        v4i acc[3][8];
+        auto values = [&](auto page) {
+            constexpr int p = decltype(page)::value;
+            if constexpr (p % 2 == 0) arrive(std::integral_constant<int, 2 + p / 2>{});
+            if constexpr (!busy) return;
+            v4i w[3];
 #pragma unroll
-            for (int p = 0; p < kChunkPages; ++p) {
-                if (p < pages) {
-                    v4i w[3];
+            for (int g = 0; g < 3; ++g)
+                w[g] = *reinterpret_cast<const v4i*>(digits + (p & 1) * kPageDigits + g * kPairs * kPage + 256 * (here & 3) + 64 * ((here & 15) >> 2) +
+                                                     16 * ((here >> 4) ^ (here & 3)));
+            v4i v[8];
 #pragma unroll
-                    for (int g = 0; g < 3; ++g) w[g] = load_digits(digits, g, p, here);
+            for (int n = 0; n < 8; ++n) v[n] = *reinterpret_cast<const v4i*>(codes + p % 2 * kRecordV + value_at + 1024 * (n >> 2) + 256 * (n & 3));
+            if constexpr (p + 1 < kChunkPages) cut_page(p + 1);
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const v4i v = *reinterpret_cast<const v4i*>(codes + value_at + 2048 * p + 256 * n);
+            for (int n = 0; n < 8; ++n)
 #pragma unroll
-                        for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v, p == 0 ? zero : acc[g][n], 0, 0, 0);
-                    }
-                }
+                for (int g = 0; g < 3; ++g) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[g], v[n], p == 0 ? zero : acc[g][n], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 7, 0);
+#pragma unroll
+            for (int n = 0; n < 24; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                if (n % 3 == 2 && n < 12) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[n][r] = digits_value(acc[0][n][r], acc[1][n][r], acc[2][n][r]);
-            o_chunk = chunk;
+            wave_lds_order();
         };
-        values(std::integral_constant<int, 4>{});
-        values(std::integral_constant<int, 5>{});
-        values(std::integral_constant<int, 6>{});
-        values(std::integral_constant<int, 7>{});
+        values(std::integral_constant<int, 0>{});
+        values(std::integral_constant<int, 1>{});
+        values(std::integral_constant<int, 2>{});
+        values(std::integral_constant<int, 3>{});
+        if constexpr (busy) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r][n] = digits_value(acc[0][n][r], acc[1][n][r], acc[2][n][r]);
+            o_chunk = chunk;
+        }
         gone = next_gone;
 #pragma unroll
-        for (int p = 0; p <= kChunkPages; ++p) rec[p] = next[p];
-    }
-    if (o_chunk >= 0) flush(kSteps - 1);
+        for (int p = 0; p < kChunkPages; ++p) rec[p] = next[p];
+    };
+    int chunk = c0;
+    for (; chunk < c1 && chunk * kChunk < my_longest; ++chunk) pass(chunk, std::true_type{});
+    for (; chunk < c1; ++chunk) pass(chunk, std::false_type{});
+#pragma unroll
+    for (int r = 0; r < 4; ++r) flush(r);
     // the steps asked for past the last chunk have to land before the ring begins anew
     wait_loads_barrier<0>();
 }
