@@ -34,77 +34,55 @@ struct kv8_group {
 // A group of one row is read like a row without a group.
 __device__ __forceinline__ kv8_group group_at(const kv8_shared_args& a, int g)
 {
-    kv8_group o{0, 0, 0, 0};
-    if (g < 0 || g >= a.n_groups) return o;
-    o.first = o.row0 = min(max(a.group_rows[g], 0), a.R);
-    o.rows = min(a.group_rows[g + 1], a.R) - o.row0;
-    if (o.rows >= 2) o.chunks = min(max(a.shared[g], 0) / kChunk, a.chunks);
+    const bool is = g < a.n_groups;
+    const int begin = a.group_rows[is ? g : 0], end = a.group_rows[is ? g + 1 : 0], shared = a.shared[is ? g : 0];
+    kv8_group o;
+    o.first = o.row0 = min(max(begin, 0), a.R);
+    o.rows = is ? min(end, a.R) - o.row0 : 0;
+    o.chunks = o.rows >= 2 ? min(max(shared, 0) / kChunk, a.chunks) : 0;
     return o;
 }
 
-// The group of a row: the last one that begins at or in front of it.
-__device__ __forceinline__ kv8_group group_of_row(const kv8_shared_args& a, int row)
+// The groups are looked at a wave's width at a time; `mine` is this lane's group of the first 64, which a caller loads once.
+__device__ __forceinline__ kv8_group group_of_lane(const kv8_group& from, int lane)
 {
-    int begins = 0;
-    for (int base = 0; base <= a.n_groups; base += kWave) {
-        const int i = base + (threadIdx.x & 63);
-        const int n = __popcll(__ballot(i <= a.n_groups && a.group_rows[min(i, a.n_groups)] <= row));
-        begins += n;
-        if (n < kWave) break;
-    }
-    return group_at(a, __builtin_amdgcn_readfirstlane(begins - 1));
+    return kv8_group{__builtin_amdgcn_readlane(from.first, lane), __builtin_amdgcn_readlane(from.row0, lane), __builtin_amdgcn_readlane(from.rows, lane),
+                     __builtin_amdgcn_readlane(from.chunks, lane)};
 }
 
-// Tile number `tile` of all groups' tiles of rows_per_tile rows: its group, and row0 / rows of the tile itself; rows = 0 where there is none.
-__device__ __forceinline__ kv8_group tile_of_groups(const kv8_shared_args& a, int tile)
+// Chunks that a row's group reads for it.
+__device__ __forceinline__ int chunks_before(const kv8_shared_args& a, kv8_group mine, int row)
 {
-    const int lane = threadIdx.x & 63;
-    int before = 0;
     for (int base = 0; base < a.n_groups; base += kWave) {
-        const kv8_group mine = group_at(a, base + lane);
-        const int tiles = mine.chunks > 0 ? (mine.rows + a.rows_per_tile - 1) / a.rows_per_tile : 0;
-        int sum = tiles;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const int x = __shfl_up(sum, off, kWave);
-            sum += lane >= off ? x : 0;
-        }
-        const unsigned long long past = __ballot(before + sum > tile);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            kv8_group o{__builtin_amdgcn_readlane(mine.first, at), 0, __builtin_amdgcn_readlane(mine.rows, at), __builtin_amdgcn_readlane(mine.chunks, at)};
-            const int skip = (tile - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at))) * a.rows_per_tile;
-            o.row0 = o.first + skip;
-            o.rows = min(o.rows - skip, a.rows_per_tile);
-            return o;
-        }
-        before += __builtin_amdgcn_readlane(sum, kWave - 1);
+        if (base > 0) mine = group_at(a, base + (threadIdx.x & 63));
+        const unsigned long long its = __ballot(row >= mine.first && row < mine.first + mine.rows);
+        if (its != 0) return __builtin_amdgcn_readlane(mine.chunks, __builtin_ctzll(its));
     }
-    return kv8_group{0, 0, 0, 0};
+    return 0;
 }
 
-// The groups' shared chunks times the sets of four tiles that read them, in all (below 2^30), and the place of number `at` among them: chunk c of
-// rows row0 .. row0 + rows - 1 of a group.
-__device__ __forceinline__ int sets_of(const kv8_shared_args& a, const kv8_group& g) { return (g.rows + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile); }
-__device__ __forceinline__ int chunks_of_groups(const kv8_shared_args& a)
+// How much of something each group has, in all, and the group that number `at` of it falls into, with what lies in front of it there.
+template <class Count>
+__device__ __forceinline__ int count_groups(const kv8_shared_args& a, kv8_group mine, Count count)
 {
     int all = 0;
     for (int base = 0; base < a.n_groups; base += kWave) {
-        const kv8_group mine = group_at(a, base + (threadIdx.x & 63));
-        all += sets_of(a, mine) * mine.chunks;
+        if (base > 0) mine = group_at(a, base + (threadIdx.x & 63));
+        all += count(mine);
     }
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) all += __shfl_xor(all, off, kWave);
     return __builtin_amdgcn_readfirstlane(all);
 }
-__device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, int at, int& chunk)
+template <class Count>
+__device__ __forceinline__ kv8_group find_group(const kv8_shared_args& a, kv8_group mine, int at, int& within, Count count)
 {
     const int lane = threadIdx.x & 63;
     int before = 0;
     for (int base = 0; base < a.n_groups; base += kWave) {
-        const kv8_group mine = group_at(a, base + lane);
-        const int count = sets_of(a, mine) * mine.chunks;
-        int sum = count;
+        if (base > 0) mine = group_at(a, base + lane);
+        const int its = count(mine);
+        int sum = its;
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
             const int x = __shfl_up(sum, off, kWave);
@@ -113,17 +91,40 @@ __device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, i
         const unsigned long long past = __ballot(before + sum > at);
         if (past != 0) {
             const int g = __builtin_ctzll(past);
-            kv8_group o{__builtin_amdgcn_readlane(mine.first, g), 0, __builtin_amdgcn_readlane(mine.rows, g), __builtin_amdgcn_readlane(mine.chunks, g)};
-            const int in = at - before - (__builtin_amdgcn_readlane(sum, g) - __builtin_amdgcn_readlane(count, g)), set = in / o.chunks;
-            chunk = in - set * o.chunks;
-            o.row0 = o.first + 4 * a.rows_per_tile * set;
-            o.rows = min(o.rows - 4 * a.rows_per_tile * set, 4 * a.rows_per_tile);
-            return o;
+            within = at - before - (__builtin_amdgcn_readlane(sum, g) - __builtin_amdgcn_readlane(its, g));
+            return group_of_lane(mine, g);
         }
         before += __builtin_amdgcn_readlane(sum, kWave - 1);
     }
-    chunk = 0;
+    within = 0;
     return kv8_group{0, 0, 0, 0};
+}
+
+// Tile number `tile` of all groups' tiles of rows_per_tile rows: its rows; rows = 0 where there is none.
+__device__ __forceinline__ kv8_group tile_of_groups(const kv8_shared_args& a, const kv8_group& mine, int tile)
+{
+    int nth;
+    kv8_group o = find_group(a, mine, tile, nth, [&](const kv8_group& g) { return g.chunks > 0 ? (g.rows + a.rows_per_tile - 1) / a.rows_per_tile : 0; });
+    o.row0 = o.first + nth * a.rows_per_tile;
+    o.rows = min(o.rows - nth * a.rows_per_tile, a.rows_per_tile);
+    return o;
+}
+
+// The groups' shared chunks times the sets of four tiles that read them (below 2^30 in all); number `at` of them: the set's rows and its chunk.
+struct sets_of_groups {
+    int rows;  // of a set
+    __device__ __forceinline__ int operator()(const kv8_group& g) const { return g.chunks > 0 ? (g.rows + rows - 1) / rows * g.chunks : 0; }
+};
+__device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, const kv8_group& mine, int at, int& chunk)
+{
+    const sets_of_groups sets{4 * a.rows_per_tile};
+    int in;
+    kv8_group o = find_group(a, mine, at, in, sets);
+    const int set = o.chunks > 0 ? in / o.chunks : 0;
+    chunk = in - set * o.chunks;
+    o.row0 = o.first + sets.rows * set;
+    o.rows = min(o.rows - sets.rows * set, sets.rows);
+    return o;
 }
 
 // ---------------------------------------------------------------- chunks of a tile
@@ -658,29 +659,34 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     __shared__ __attribute__((aligned(1024))) uint8_t lds[FORM == kRuns && kRingLds > kTileLds ? kRingLds : kTileLds];
     const int kvh = blockIdx.x % a.c.Hkv;
     int nth = blockIdx.x / a.c.Hkv;
-    if (FORM != kNoGroups && nth < a.group_wgs) {
-        if constexpr (FORM == kRuns) {
-            const long long all = chunks_of_groups(a);
-            int at = (int)(all * nth / a.group_wgs);
-            const int to = (int)(all * (nth + 1) / a.group_wgs);
-            while (at < to) {
-                int c0;
-                const kv8_group tiles = place_in_groups(a, at, c0);
-                if (tiles.chunks == 0) return;
-                const int c1 = min(tiles.chunks, c0 + to - at);
-                chunks_of_tiles<WEIGHTS>(a, lds, kvh, tiles.row0, tiles.rows, a.slots ? a.slots[tiles.first] : tiles.first, c0, c1);
-                at += c1 - c0;
+    kv8_group mine{};
+    if constexpr (FORM != kNoGroups) {
+        mine = group_at(a, threadIdx.x & 63);
+        if (nth < a.group_wgs) {
+            if constexpr (FORM == kRuns) {
+                const long long all = count_groups(a, mine, sets_of_groups{4 * a.rows_per_tile});
+                int at = (int)(all * nth / a.group_wgs);
+                const int to = (int)(all * (nth + 1) / a.group_wgs);
+                while (at < to) {
+                    int c0;
+                    const kv8_group set = place_in_groups(a, mine, at, c0);
+                    if (set.chunks == 0) return;
+                    const int c1 = min(set.chunks, c0 + to - at);
+                    chunks_of_tiles<WEIGHTS>(a, lds, kvh, set.row0, set.rows, a.slots ? a.slots[set.first] : set.first, c0, c1);
+                    at += c1 - c0;
+                }
+            } else {
+                const kv8_group tile = tile_of_groups(a, mine, nth / a.group_steps);
+                const int first = nth % a.group_steps;
+                if (first >= tile.chunks) return;
+                // the pages are those of the group's first row
+                chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks,
+                                                     a.group_steps);
             }
-        } else {
-            const kv8_group tile = tile_of_groups(a, nth / a.group_steps);
-            const int first = nth % a.group_steps;
-            if (first >= tile.chunks) return;
-            // the pages are those of the group's first row
-            chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks, a.group_steps);
+            return;
         }
-        return;
+        nth -= a.group_wgs;
     }
-    if (FORM != kNoGroups) nth -= a.group_wgs;
     const int row = nth / a.row_steps, first = nth % a.row_steps;
     int slot;
     const int len = row_length(a, row, slot);
@@ -690,47 +696,58 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
                 reinterpret_cast<uint32_t*>(a.out + ((size_t)row * a.Hq + kvh * a.G) * kHeadDim)[i] = 0u;
         return;
     }
-    const int behind = FORM != kNoGroups && len > kChunk ? group_of_row(a, row).chunks : 0;
+    int behind = 0;
+    if constexpr (FORM != kNoGroups) behind = len > kChunk ? chunks_before(a, mine, row) : 0;
     chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, row, 1, slot, behind + first, a.chunks, a.row_steps);
 }
 
-// The chunks of one (row, head) of more than one chunk, folded in ascending order, one column a thread.  As kv8_attn_combine_kernel (attn_kv8.hip).
-__device__ __forceinline__ void combine_head(const kv8_shared_args& a, size_t at)
+// The chunks of a (row, head) of more than one chunk, folded in ascending order: the operations of kv8_attn_combine_kernel (attn_kv8.hip), down to the
+// empty chunks it ends with (a multiple of sixteen in all).  Four columns a lane, so that what every lane works out of a chunk's (m, l) serves four sums:
+// with one column a lane those instructions took the launch (32 us for 64 rows of 32 heads and 126 chunks; XX so).
+constexpr int kFoldChunks = 8, kCombineThreads = 128, kCombineHeads = kCombineThreads / 32;
+__device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t block)
 {
-    constexpr int kBlockChunks = 16;
-    int slot;
-    const int len = row_length(a, (int)(at / a.Hq), slot);
-    if (len <= kChunk) return;
-    const int chunks = (len + kChunk - 1) / kChunk;
+    const int lane = threadIdx.x & 31;
+    const size_t at = block * kCombineHeads + threadIdx.x / 32;
+    int slot, len = 0;
+    if (at < (size_t)a.R * a.Hq) len = row_length(a, (int)(at / a.Hq), slot);
+    const int chunks = len > kChunk ? (len + kChunk - 1) / kChunk : 0;
+    if (chunks == 0) return;
     const float4* ps = a.part + at * a.chunks;
-    const float* po = a.part_o + at * a.chunks * kHeadDim + threadIdx.x;
-    float x[2][kBlockChunks];
-    auto ask = [&](float (&to)[kBlockChunks], int c0) {
+    const float4* po = reinterpret_cast<const float4*>(a.part_o + at * a.chunks * kHeadDim) + lane;
+    float4 x[2][kFoldChunks];
+    auto ask = [&](float4 (&to)[kFoldChunks], int c0) {
 #pragma unroll
-        for (int k = 0; k < kBlockChunks; ++k) to[k] = po[(size_t)min(c0 + k, chunks - 1) * kHeadDim];
+        for (int k = 0; k < kFoldChunks; ++k) to[k] = po[(size_t)min(c0 + k, chunks - 1) * (kHeadDim / 4)];
     };
     ask(x[0], 0);
-    float m = -__builtin_inff(), l = 0.0f, o = 0.0f;
-    auto fold = [&](const float (&from)[kBlockChunks], int c0) {
-        float4 st[kBlockChunks];
+    float m = -__builtin_inff(), l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto fold = [&](const float4 (&from)[kFoldChunks], int c0) {
+        float4 st[kFoldChunks];
 #pragma unroll
-        for (int k = 0; k < kBlockChunks; ++k) st[k] = ps[min(c0 + k, chunks - 1)];
+        for (int k = 0; k < kFoldChunks; ++k) st[k] = ps[min(c0 + k, chunks - 1)];
 #pragma unroll
-        for (int k = 0; k < kBlockChunks; ++k) {  // past the last chunk: one without tokens, which changes nothing
+        for (int k = 0; k < kFoldChunks; ++k) {  // past the last chunk: one without tokens, which changes nothing
             const bool there = c0 + k < chunks;
             float fa, fb;
             fold_step(m, l, there ? st[k].x : -__builtin_inff(), there ? st[k].y : 0.0f, st[k].z, fa, fb);
-            o = fold_value(o, there ? from[k] : 0.0f, fa, fb);
+            o.x = fold_value(o.x, there ? from[k].x : 0.0f, fa, fb);
+            o.y = fold_value(o.y, there ? from[k].y : 0.0f, fa, fb);
+            o.z = fold_value(o.z, there ? from[k].z : 0.0f, fa, fb);
+            o.w = fold_value(o.w, there ? from[k].w : 0.0f, fa, fb);
         }
     };
-    for (int c0 = 0; c0 < chunks; c0 += 2 * kBlockChunks) {
-        if (c0 + kBlockChunks < chunks) ask(x[1], c0 + kBlockChunks);
+    const int all = (chunks + 15) & ~15;
+    for (int c0 = 0; c0 < all; c0 += 2 * kFoldChunks) {
+        ask(x[1], c0 + kFoldChunks);
         fold(x[0], c0);
-        if (c0 + kBlockChunks >= chunks) break;
-        if (c0 + 2 * kBlockChunks < chunks) ask(x[0], c0 + 2 * kBlockChunks);
-        fold(x[1], c0 + kBlockChunks);
+        if (c0 + 2 * kFoldChunks < all) ask(x[0], c0 + 2 * kFoldChunks);
+        fold(x[1], c0 + kFoldChunks);
     }
-    __builtin_nontemporal_store(to_bf16(o * row_factor(l)), &a.out[at * kHeadDim + threadIdx.x]);
+    const float by = row_factor(l);
+    stream_store(a.out + at * kHeadDim + 4 * lane, make_uint2((uint32_t)to_bf16(o.x * by) | (uint32_t)to_bf16(o.y * by) << 16,
+                                                              (uint32_t)to_bf16(o.z * by) | (uint32_t)to_bf16(o.w * by) << 16));
 }
 
 // ---------------------------------------------------------------- the pages' weights
@@ -738,7 +755,7 @@ __device__ __forceinline__ void combine_head(const kv8_shared_args& a, size_t at
 // weights_out[slot] = weights_in[slot] + what sixteen chunks' pages get from the rows that name the slot.  A thread has one chunk and every eighth
 // head; the rows' largest scores and sums are folded here again, beside the heads' own workgroups instead of behind them.  Sums in a fixed order:
 // of each eighth the rows ascending and in a row its heads, then the eighths.  A row whose softmax is not finite adds nothing.
-constexpr int kWeightChunks = 16, kWeightParts = 8, kCombineThreads = kWeightChunks * kWeightParts;
+constexpr int kWeightChunks = 16, kWeightParts = kCombineThreads / kWeightChunks;
 struct weights_lds {
     float2 stats[kCombineThreads];
     float4 parts[kWeightParts - 1][kWeightChunks];
@@ -809,20 +826,19 @@ __device__ __forceinline__ void page_weights(const kv8_shared_args& a, weights_l
     }
 }
 
-// Grid (R * Hq) of a column a thread; before them, if the pages are weighed, (blocks of chunks, slots).
+// Grid: blocks of kCombineHeads of the R * Hq; before them, if the pages are weighed, (blocks of chunks, slots).
 template <bool WEIGHTS>
 __global__ __launch_bounds__(kCombineThreads) void kv8_shared_combine_kernel(kv8_shared_args a, int weight_blocks)
 {
-    static_assert(kCombineThreads == kHeadDim);
     if constexpr (WEIGHTS) {
         __shared__ weights_lds lds;
         if ((int)blockIdx.x < weight_blocks * a.c.n_slots) {
             page_weights(a, lds, blockIdx.x / weight_blocks, blockIdx.x % weight_blocks);
             return;
         }
-        combine_head(a, blockIdx.x - (size_t)weight_blocks * a.c.n_slots);
+        combine_heads(a, blockIdx.x - (size_t)weight_blocks * a.c.n_slots);
     } else {
-        combine_head(a, blockIdx.x);
+        combine_heads(a, blockIdx.x);
     }
 }
 
@@ -898,7 +914,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         }
     }
     const long long grid = (a.group_wgs + (long long)R * a.row_steps) * cache.Hkv, blocks = weights ? (a.chunks + kWeightChunks - 1) / kWeightChunks : 0,
-                    second = blocks * cache.n_slots + (long long)R * Hq;
+                    second = blocks * cache.n_slots + ((long long)R * Hq + kCombineHeads - 1) / kCombineHeads;
     if (grid > 0x7FFFFFFFll / 256 || second > 0x7FFFFFFFll / kCombineThreads) return DET_ESHAPE;
     auto launch = [&](auto form) {
         if (a.G <= 4) launch_shared<decltype(form)::value, true>(a, weights, (unsigned)grid, s);
