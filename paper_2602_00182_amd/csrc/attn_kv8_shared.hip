@@ -129,7 +129,8 @@ __device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, c
 
 // ---------------------------------------------------------------- chunks of a tile
 
-// Every step-th chunk from first_chunk on, below end_chunk, for `rows` rows from row0 on, all of which read the pages of slot `now`.  As
+// Every step-th chunk from first_chunk on, below end_chunk, for `rows` rows from row0 on, all of which read the pages of slot `now`: of a group, or (rows =
+// 1) a row of length row_len.  As
 // kv8_attn_chunk_kernel takes one (attn_kv8.hip): a page a wave for the scores, 32 columns a wave for the weighted sums.
 template <bool PACK>
 struct tile_lds {
@@ -140,8 +141,8 @@ struct tile_lds {
 };
 
 template <bool PACK, bool WEIGHTS, bool GROUP>
-__device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int now, int first_chunk,
-                                               int end_chunk, int step)
+__device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int row_len, int now,
+                                               int first_chunk, int end_chunk, int step)
 {
     constexpr int NP = PACK ? 1 : 4;  // pairs of a lane
     constexpr int DIGITS = tile_lds<PACK>::DIGITS;
@@ -150,13 +151,18 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
     auto& top = shared.top;
     auto& lsum = shared.lsum;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane >> 4, col = lane & 15;
-    int slot, len = 0;
-    if (col < rows * a.G) len = row_length(a, row0 + pair_row(a, col), slot);
-    if (GROUP && len <= kChunk) len = 0;  // such a row is read for itself
-    int longest = len;
+    int len = 0, longest = row_len;
+    if constexpr (GROUP) {
+        int slot;
+        if (col < rows * a.G) len = row_length(a, row0 + pair_row(a, col), slot);
+        if (len <= kChunk) len = 0;  // such a row is read for itself
+        longest = len;
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
-    longest = __builtin_amdgcn_readfirstlane(longest);
+        for (int off = 1; off < 16; off <<= 1) longest = max(longest, __shfl_xor(longest, off, kWave));
+        longest = __builtin_amdgcn_readfirstlane(longest);
+    } else {
+        len = col < a.G ? row_len : 0;
+    }
     end_chunk = min(end_chunk, (longest + kChunk - 1) / kChunk);
     if (first_chunk >= end_chunk) return;
 
@@ -680,7 +686,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
                 const int first = nth % a.group_steps;
                 if (first >= tile.chunks) return;
                 // the pages are those of the group's first row
-                chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks,
+                chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, 0, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks,
                                                      a.group_steps);
             }
             return;
@@ -698,7 +704,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     }
     int behind = 0;
     if constexpr (FORM != kNoGroups) behind = len > kChunk ? chunks_before(a, mine, row) : 0;
-    chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, row, 1, slot, behind + first, a.chunks, a.row_steps);
+    chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, row, 1, len, slot, behind + first, a.chunks, a.row_steps);
 }
 
 // The chunks of a (row, head) of more than one chunk, folded in ascending order: the operations of kv8_attn_combine_kernel (attn_kv8.hip), down to the
@@ -715,23 +721,25 @@ __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t b
     if (chunks == 0) return;
     const float4* ps = a.part + at * a.chunks;
     const float4* po = reinterpret_cast<const float4*>(a.part_o + at * a.chunks * kHeadDim) + lane;
-    float4 x[2][kFoldChunks];
-    auto ask = [&](float4 (&to)[kFoldChunks], int c0) {
+    float4 x[2][kFoldChunks], st[2][kFoldChunks];
+    auto ask = [&](int to, int c0) {
 #pragma unroll
-        for (int k = 0; k < kFoldChunks; ++k) to[k] = po[(size_t)min(c0 + k, chunks - 1) * (kHeadDim / 4)];
+        for (int k = 0; k < kFoldChunks; ++k) {
+            const int c = min(c0 + k, chunks - 1);
+            st[to][k] = ps[c];
+            x[to][k] = po[(size_t)c * (kHeadDim / 4)];
+        }
     };
-    ask(x[0], 0);
+    ask(0, 0);
     float m = -__builtin_inff(), l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto fold = [&](const float4 (&from)[kFoldChunks], int c0) {
-        float4 st[kFoldChunks];
-#pragma unroll
-        for (int k = 0; k < kFoldChunks; ++k) st[k] = ps[min(c0 + k, chunks - 1)];
+    auto fold = [&](int of, int c0) {
+        const float4(&from)[kFoldChunks] = x[of];
 #pragma unroll
         for (int k = 0; k < kFoldChunks; ++k) {  // past the last chunk: one without tokens, which changes nothing
             const bool there = c0 + k < chunks;
             float fa, fb;
-            fold_step(m, l, there ? st[k].x : -__builtin_inff(), there ? st[k].y : 0.0f, st[k].z, fa, fb);
+            fold_step(m, l, there ? st[of][k].x : -__builtin_inff(), there ? st[of][k].y : 0.0f, st[of][k].z, fa, fb);
             o.x = fold_value(o.x, there ? from[k].x : 0.0f, fa, fb);
             o.y = fold_value(o.y, there ? from[k].y : 0.0f, fa, fb);
             o.z = fold_value(o.z, there ? from[k].z : 0.0f, fa, fb);
@@ -740,10 +748,10 @@ __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t b
     };
     const int all = (chunks + 15) & ~15;
     for (int c0 = 0; c0 < all; c0 += 2 * kFoldChunks) {
-        ask(x[1], c0 + kFoldChunks);
-        fold(x[0], c0);
-        if (c0 + 2 * kFoldChunks < all) ask(x[0], c0 + 2 * kFoldChunks);
-        fold(x[1], c0 + kFoldChunks);
+        ask(1, c0 + kFoldChunks);
+        fold(0, c0);
+        if (c0 + 2 * kFoldChunks < all) ask(0, c0 + 2 * kFoldChunks);
+        fold(1, c0 + kFoldChunks);
     }
     const float by = row_factor(l);
     stream_store(a.out + at * kHeadDim + 4 * lane, make_uint2((uint32_t)to_bf16(o.x * by) | (uint32_t)to_bf16(o.y * by) << 16,
@@ -899,12 +907,21 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         const long long room = wgs / (rows * cache.Hkv);
         return room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
     };
-    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_TAIL_WGS : DET_KV8_CHUNK_WGS);
+    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_RUN_WGS : DET_KV8_CHUNK_WGS);
     bool ring = false;
     if (step.n_groups > 0) {
-        ring = (long long)R * a.G > (long long)DET_KV8_RING_PAIRS * step.n_groups;
+        auto of_head = [&](long long most, long long wgs) {  // workgroups of a KV head
+            const long long n = wgs / cache.Hkv < 1 ? 1 : wgs / cache.Hkv;
+            return (int)(most < n ? most : n);
+        };
+        ring = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile * a.chunks * cache.Hkv >= DET_KV8_RING_CHUNKS;
         if (ring) {
-            a.group_wgs = DET_KV8_RING_WGS / cache.Hkv < 1 ? 1 : DET_KV8_RING_WGS / cache.Hkv;
+            // Two workgroups a compute unit: all of them for runs of several chunks, else some are left to what rows read for themselves, beside them.  60 rows
+            // of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7; 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
+            const long long sets = ((long long)R + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile), most = (sets > step.n_groups ? sets : step.n_groups) * a.chunks,
+                            rest = DET_KV8_RUN_WGS - (long long)R * cache.Hkv;
+            const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS;
+            a.group_wgs = of_head(most, several ? DET_KV8_RUN_WGS : rest > DET_KV8_RUN_WGS / 2 ? rest : DET_KV8_RUN_WGS / 2);
         } else {
             // a group of n rows has at most n / rows_per_tile + 1 tiles, and at most n
             const long long tiles = R / a.rows_per_tile + step.n_groups < R ? R / a.rows_per_tile + step.n_groups : R;
