@@ -605,6 +605,29 @@ int det_qdecoder_layer_kv8(const det_layer_weights *w, const det_layer_cfg *cfg,
                            const int32_t *slots, const float *rope_cos, const float *rope_sin, void *ws,
                            size_t ws_bytes, int R, void *stream);
 
+/* The same layers with det_attn_decode_kv8_shared or det_attn_decode_kv8_weights in the place of det_attn_decode_kv8: step (a host struct of device pointers)
+ * says which rows share what, and where the pages' weights are added up, over rows, heads, layers and steps (NULL: nowhere).  step NULL, or without groups
+ * and weights: the calls above.  A layer's bytes are the same whatever step says.  R <= 65535 with groups or weights.
+ * Workspace: *_kv8_step_workspace_bytes(cfg, R, max_pages, weights), weights != 0 where step has some; without groups and weights that of the calls above. */
+typedef struct det_kv8_step {
+    const int32_t *group_rows; /* [n_groups + 1] */
+    const int32_t *shared;     /* [n_groups] */
+    float *weights;            /* [n_slots, max_pages], added to, or NULL */
+    int32_t n_groups;
+} det_kv8_step;
+size_t det_decoder_layer_kv8_step_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages, int weights);
+int det_decoder_layer_kv8_step(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
+                               const int32_t *page_table, int n_pages, int n_slots, int max_pages,
+                               const int32_t *positions, const int32_t *slots, const float *rope_cos,
+                               const float *rope_sin, const det_kv8_step *step /* host */, void *ws, size_t ws_bytes,
+                               int R, void *stream);
+size_t det_qdecoder_layer_kv8_step_workspace_bytes(const det_layer_cfg *cfg /* host */, int R, int max_pages, int weights);
+int det_qdecoder_layer_kv8_step(const det_layer_weights *w, const det_layer_cfg *cfg, void *x_inout, void *pool,
+                                const int32_t *page_table, int n_pages, int n_slots, int max_pages,
+                                const int32_t *positions, const int32_t *slots, const float *rope_cos,
+                                const float *rope_sin, const det_kv8_step *step /* host */, void *ws, size_t ws_bytes,
+                                int R, void *stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Verification of drafted tokens against the target's probabilities, from given random numbers (section 6.6: the tokens are a function of
  * what is given; nothing is drawn here).  For sequence b with n = n_drafts[b] drafts (n_drafts NULL: N; clamped to 0..N):

@@ -20,6 +20,10 @@ class LayerWeights(C.Structure):
                 ("w_norm2", C.c_void_p), ("wgu", C.c_void_p), ("wdown", C.c_void_p)]
 
 
+class Kv8Step(C.Structure):
+    _fields_ = [("group_rows", C.c_void_p), ("shared", C.c_void_p), ("weights", C.c_void_p), ("n_groups", C.c_int32)]
+
+
 class LogitsRules(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("penalties", "history", "history_rows", "history_lens", "generated_from", "bias_begin", "bias_tokens",
                                           "bias_values", "masks", "mask_rows")]
@@ -111,6 +115,12 @@ SIGNATURES = {
     "det_qdecoder_layer_kv8_rows_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i]),
     "det_qdecoder_layer_kv8": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
                                     _vp, _sz, _i, _vp]),
+    "det_decoder_layer_kv8_step_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i, _i]),
+    "det_decoder_layer_kv8_step": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
+                                        C.POINTER(Kv8Step), _vp, _sz, _i, _vp]),
+    "det_qdecoder_layer_kv8_step_workspace_bytes": (_sz, [C.POINTER(LayerCfg), _i, _i, _i]),
+    "det_qdecoder_layer_kv8_step": (_i, [C.POINTER(LayerWeights), C.POINTER(LayerCfg), _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp,
+                                         C.POINTER(Kv8Step), _vp, _sz, _i, _vp]),
     "det_verify_drafts_workspace_bytes": (_sz, [_i, _i]),
     "det_verify_drafts": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _vp]),
     "det_sha256_init": (_i, [C.POINTER(Sha256Ctx)]),

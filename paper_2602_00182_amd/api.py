@@ -8,7 +8,7 @@ import ctypes as C
 
 import torch
 
-from ._lib import LayerCfg, LayerWeights, LogitsRules, Sha256Ctx, lib
+from ._lib import Kv8Step, LayerCfg, LayerWeights, LogitsRules, Sha256Ctx, lib
 
 __all__ = [
     "DetError", "det_gemm_bf16", "det_gemm_bf16_fixed_tile", "det_probe_lds_fill", "det_gemm_wide_rows", "det_gemm_tile", "det_qgemm_tile", "det_gemm_packed_b_bytes", "det_gemm_pack_b", "det_gemm_bf16_residual",
@@ -25,12 +25,13 @@ __all__ = [
     "det_qgemm_w4a8_swiglu", "det_quant_pack_w4_gate_up", "quant_pack_gate_up", "det_rmsnorm_quant_q8",
     "det_qdecoder_layer_workspace_bytes", "det_qdecoder_layer", "det_attn_decode_quant_q8",
     "det_qgemm_w4a8_swiglu_quant_supported", "det_qgemm_w4a8_swiglu_quant",
-    "KV8_PAGE", "KV8_RECORD", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
+    "KV8_PAGE", "KV8_RECORD", "KV8_SHARED_CHUNK", "det_kv8_pool_bytes", "kv8_pool", "det_kv8_rope_append", "det_kv8_read", "det_kv8_copy_pages",
     "det_attn_decode_kv8_workspace_bytes", "det_attn_decode_kv8_rows_workspace_bytes", "det_attn_decode_kv8",
     "det_decoder_layer_kv8_workspace_bytes", "det_decoder_layer_kv8_rows_workspace_bytes", "det_decoder_layer_kv8",
     "det_qdecoder_layer_kv8_workspace_bytes", "det_qdecoder_layer_kv8_rows_workspace_bytes", "det_qdecoder_layer_kv8", "det_verify_drafts_workspace_bytes", "det_verify_drafts",
     "det_attn_decode_kv8_shared_workspace_bytes", "det_attn_decode_kv8_shared", "det_attn_decode_kv8_weights_workspace_bytes",
-    "det_attn_decode_kv8_weights", "det_kv8_pick_pages", "logits_rules", "det_logits_process", "det_logits_advance",
+    "det_attn_decode_kv8_weights", "det_kv8_pick_pages", "kv8_step", "det_decoder_layer_kv8_step_workspace_bytes", "det_decoder_layer_kv8_step",
+    "det_qdecoder_layer_kv8_step_workspace_bytes", "det_qdecoder_layer_kv8_step", "logits_rules", "det_logits_process", "det_logits_advance",
 ]
 
 _CODES = {1: "DET_EINVAL", 2: "DET_ESHAPE", 3: "DET_EALIGN", 4: "DET_EWORKSPACE", 5: "DET_EHIP"}
@@ -716,6 +717,7 @@ def det_next_token(prompts, prompt_lens, last_sampled, tokens_out, positions_out
 
 
 KV8_PAGE, KV8_RECORD = 64, 16896  # tokens of a page of the 8-bit cache; bytes of a page and KV head
+KV8_SHARED_CHUNK = 256  # tokens that rows which share pages read together
 
 
 def det_kv8_pool_bytes(n_pages: int, Hkv: int, D: int = 128) -> int:
@@ -897,6 +899,46 @@ def det_decoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, p
 def det_qdecoder_layer_kv8(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream=None) -> None:
     """det_decoder_layer_kv8 on quantized weights; wqkv packed by quant_pack_weight."""
     det_decoder_layer_kv8(w, cfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, ws, stream, _entry="det_qdecoder_layer_kv8")
+
+
+def kv8_step(group_rows=None, shared=None, weights=None) -> Kv8Step:
+    """What det_decoder_layer_kv8_step is told of its rows, over device tensors, which it keeps: groups as det_attn_decode_kv8_shared takes them, and weights
+    [n_slots, max_pages] fp32, to which every layer adds what the pages get."""
+    s = Kv8Step()
+    s.group_rows, s.shared, s.n_groups = _groups(group_rows, shared)
+    s.weights = None if weights is None else _contig(weights, torch.float32)
+    s._tensors = (group_rows, shared, weights)
+    return s
+
+
+def det_decoder_layer_kv8_step_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int, weights: bool) -> int:
+    return lib().det_decoder_layer_kv8_step_workspace_bytes(C.byref(cfg), R, max_pages, int(weights))
+
+
+def det_qdecoder_layer_kv8_step_workspace_bytes(cfg: LayerCfg, R: int, max_pages: int, weights: bool) -> int:
+    return lib().det_qdecoder_layer_kv8_step_workspace_bytes(C.byref(cfg), R, max_pages, int(weights))
+
+
+def det_decoder_layer_kv8_step(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, step, ws, stream=None,
+                               _entry: str = "det_decoder_layer_kv8_step") -> None:
+    """det_decoder_layer_kv8 with what `step` (kv8_step, or None) says: shared chunks read once, the pages' weights added up."""
+    R = x.shape[0]
+    cache, Hkv = _kv8(pool, page_table)
+    if x.shape != (R, cfg.H) or Hkv != cfg.Hkv or positions.shape != (R,):
+        raise ValueError("bad layer shapes")
+    if rope_cos.shape != (cfg.Lmax, cfg.D // 2) or rope_sin.shape != rope_cos.shape:
+        raise ValueError("bad layer shapes")
+    if step is not None and step._tensors[2] is not None and step._tensors[2].shape != page_table.shape:
+        raise ValueError("a weight for each entry of the page table")
+    _check(_entry, getattr(lib(), _entry)(
+        C.byref(w), C.byref(cfg), _contig(x, torch.bfloat16), *cache, _contig(positions, torch.int32), _slots(slots, R, cache[3]),
+        _contig(rope_cos, torch.float32), _contig(rope_sin, torch.float32), None if step is None else C.byref(step), _contig(ws), ws.nbytes, R,
+        _stream(stream)))
+
+
+def det_qdecoder_layer_kv8_step(w: LayerWeights, cfg: LayerCfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, step, ws, stream=None) -> None:
+    """det_decoder_layer_kv8_step on quantized weights."""
+    det_decoder_layer_kv8_step(w, cfg, x, pool, page_table, positions, slots, rope_cos, rope_sin, step, ws, stream, _entry="det_qdecoder_layer_kv8_step")
 
 
 def det_verify_drafts_workspace_bytes(B: int, V: int) -> int:

@@ -15,7 +15,8 @@ void set_last_hip_error(int e) { g_last_hip_error = e; }
 extern "C" const char* det_fingerprint(void)
 {
     return "libdetinfer gfx950 hip-" DET_STR(HIP_VERSION_MAJOR) "." DET_STR(HIP_VERSION_MINOR) "." DET_STR(
-        HIP_VERSION_PATCH) " canon-2 kv8-3(pack@4heads,walk@" DET_STR(DET_KV8_WALK_TILES) "tiles,chunks@" DET_STR(DET_KV8_CHUNK_WGS) "wg,run@" DET_STR(DET_KV8_RUN_ROWS) "rows)"
+        HIP_VERSION_PATCH) " canon-2 kv8-3(pack@4heads,walk@" DET_STR(DET_KV8_WALK_TILES) "tiles,chunks@" DET_STR(DET_KV8_CHUNK_WGS) "wg,run@" DET_STR(DET_KV8_RUN_ROWS)
+        "rows,shared@" DET_STR(DET_KV8_RING_CHUNKS) "chunks|" DET_STR(DET_KV8_RUN_WGS) "wg)"
         " gemm-16x16x32-k64"
         // launch geometry revision: which tile shapes and kernel forms the row count (GEMM), the batch
         // (attention) select.  They move no output byte, but a receipt pins them all the same, so a change of

@@ -212,23 +212,43 @@ struct Kv8LayerWs {
     size_t qkv, attn, attn_bytes, total;
 };
 
-static Kv8LayerWs kv8_layer_ws(const det_layer_cfg& c, int R, int max_pages, bool named, size_t at)
+// Whose attention a layer's step takes: every row for itself (rows that name slots need less), groups, or groups and the pages' weights.
+enum Kv8Form { kKv8Plain, kKv8Named, kKv8Step, kKv8Weights };
+
+static Kv8Form kv8_form(const det_kv8_step* step, const int32_t* slots)
+{
+    if (step && step->weights) return kKv8Weights;
+    return step && step->n_groups > 0 ? kKv8Step : slots ? kKv8Named : kKv8Plain;
+}
+
+static Kv8LayerWs kv8_layer_ws(const det_layer_cfg& c, int R, int max_pages, Kv8Form form, size_t at)
 {
     Kv8LayerWs w{};
     w.qkv = at;
     w.attn = w.qkv + up256(2 * (size_t)R * (c.Hq + 2 * c.Hkv) * c.D);
-    w.attn_bytes = attn_decode_kv8_workspace(R, c.Hq, c.Hkv, max_pages, named);
+    w.attn_bytes = form >= kKv8Step ? attn_shared_kv8_workspace(R, c.Hq, max_pages, form == kKv8Weights)
+                                    : attn_decode_kv8_workspace(R, c.Hq, c.Hkv, max_pages, form == kKv8Named);
     w.total = w.attn + up256(w.attn_bytes);
     return w;
 }
 
+static int kv8_layer_attention(const det_layer_cfg& c, const kv8_cache& cache, const det_kv8_step* step, const int32_t* positions, const int32_t* slots,
+                               const void* q, void* out, void* ws, size_t ws_bytes, int R, hipStream_t s)
+{
+    if (kv8_form(step, slots) < kKv8Step) return attn_decode_kv8_impl(q, cache, positions, slots, 1, out, ws, ws_bytes, R, c.Hq, c.D, c.scale, s);
+    return attn_shared_kv8_impl(q, cache, positions, slots, 1, kv8_step{step->group_rows, step->shared, step->n_groups, step->weights, step->weights}, out, ws,
+                                ws_bytes, R, c.Hq, c.D, c.scale, s);
+}
+
 static int kv8_layer_check(const det_layer_weights* w, const det_layer_cfg* cfg, const void* x, const void* pool, const int32_t* table, int n_pages,
                            int n_slots, int max_pages, const int32_t* positions, const int32_t* slots, const float* rope_cos,
-                           const float* rope_sin, const void* ws, int R)
+                           const float* rope_sin, const det_kv8_step* step, const void* ws, int R)
 {
     if (!w || !cfg || !x || !positions || !rope_cos || !rope_sin || !ws || R < 1) return DET_EINVAL;
     if (!w->w_norm1 || !w->wqkv || !w->wo || !w->w_norm2 || !w->wgu || !w->wdown) return DET_EINVAL;
+    if (step && (step->n_groups < 0 || (step->n_groups > 0 && (!step->group_rows || !step->shared)))) return DET_EINVAL;
     if (!layer_cfg_ok(cfg)) return DET_ESHAPE;
+    if (kv8_form(step, slots) >= kKv8Step && (R > 65535 || step->n_groups > R || (step->weights && n_slots > 65535))) return DET_ESHAPE;
     const int rc = kv8_check(pool, table, n_pages, n_slots, max_pages, cfg->Hkv, cfg->D);
     if (rc != DET_OK) return rc;
     if (cfg->Hq / cfg->Hkv > 16 || (!slots && (n_slots < R || R > 65535))) return DET_ESHAPE;
@@ -244,24 +264,31 @@ static bool kv8_layer_sizes_ok(const det_layer_cfg* cfg, int R, int max_pages)
 
 extern "C" size_t det_decoder_layer_kv8_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
-    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_layer_ws(*cfg, R, max_pages, false, layer_ws(*cfg, R).attn).total : 0;
+    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_layer_ws(*cfg, R, max_pages, kKv8Plain, layer_ws(*cfg, R).attn).total : 0;
 }
 
 extern "C" size_t det_decoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
     if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
-    return kv8_layer_ws(*cfg, R, max_pages, true, layer_ws(*cfg, R).attn).total;
+    return kv8_layer_ws(*cfg, R, max_pages, kKv8Named, layer_ws(*cfg, R).attn).total;
 }
 
-extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
-                                     int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
-                                     const float* rope_cos, const float* rope_sin, void* ws, size_t ws_bytes, int R, void* stream)
+extern "C" size_t det_decoder_layer_kv8_step_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages, int weights)
 {
-    const int bad = kv8_layer_check(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, ws, R);
+    if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
+    return kv8_layer_ws(*cfg, R, max_pages, weights ? kKv8Weights : kKv8Step, layer_ws(*cfg, R).attn).total;
+}
+
+extern "C" int det_decoder_layer_kv8_step(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
+                                          int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
+                                          const float* rope_cos, const float* rope_sin, const det_kv8_step* step, void* ws, size_t ws_bytes, int R,
+                                          void* stream)
+{
+    const int bad = kv8_layer_check(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, step, ws, R);
     if (bad != DET_OK) return bad;
     const det_layer_cfg c = *cfg;
     const LayerWs l = layer_ws(c, R);
-    const Kv8LayerWs k = kv8_layer_ws(c, R, max_pages, slots != nullptr, l.attn);
+    const Kv8LayerWs k = kv8_layer_ws(c, R, max_pages, kv8_form(step, slots), l.attn);
     if (ws_bytes < k.total) return DET_EWORKSPACE;
     char* base = static_cast<char*>(ws);
     const int nq = c.Hq * c.D, n = (c.Hq + 2 * c.Hkv) * c.D;
@@ -269,44 +296,59 @@ extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer
     DET_TRY(det_rmsnorm_gemm_bf16(x_inout, c.H, w->w_norm1, c.eps, w->wqkv, base + l.h, base + k.qkv, n, R, n, c.H, DET_BF16, stream));
     DET_TRY(det_kv8_rope_append(base + k.qkv, n, base + l.qbuf, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin,
                                 R, c.Hq, c.Hkv, c.D, c.Lmax, stream));
-    DET_TRY(attn_decode_kv8_impl(base + l.qbuf, cache, positions, slots, 1, base + l.att, base + k.attn, k.attn_bytes, R, c.Hq, c.D, c.scale,
-                                 static_cast<hipStream_t>(stream)));
+    DET_TRY(kv8_layer_attention(c, cache, step, positions, slots, base + l.qbuf, base + l.att, base + k.attn, k.attn_bytes, R, static_cast<hipStream_t>(stream)));
     DET_TRY(det_gemm_bf16_residual(base + l.att, nq, w->wo, x_inout, c.H, x_inout, c.H, R, c.H, nq, stream));
     DET_TRY(det_rmsnorm_gemm_swiglu_bf16(x_inout, c.H, w->w_norm2, c.eps, w->wgu, base + l.h, base + l.mm, c.F, R, c.F, c.H, stream));
     DET_TRY(det_gemm_bf16_residual(base + l.mm, c.F, w->wdown, x_inout, c.H, x_inout, c.H, R, c.H, c.F, stream));
     return DET_OK;
 }
 
+extern "C" int det_decoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
+                                     int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
+                                     const float* rope_cos, const float* rope_sin, void* ws, size_t ws_bytes, int R, void* stream)
+{
+    return det_decoder_layer_kv8_step(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, nullptr, ws,
+                                      ws_bytes, R, stream);
+}
+
 // The quantized layer's attention output in bf16 (its rows are quantized for the output projection) lies where the plain layer has none.
-static Kv8LayerWs kv8_qlayer_ws(const det_layer_cfg& c, const QLayerWs& l, int R, int max_pages, bool named, size_t& att)
+static Kv8LayerWs kv8_qlayer_ws(const det_layer_cfg& c, const QLayerWs& l, int R, int max_pages, Kv8Form form, size_t& att)
 {
     att = l.attn;
-    return kv8_layer_ws(c, R, max_pages, named, l.attn + up256(2 * (size_t)R * c.Hq * c.D));
+    return kv8_layer_ws(c, R, max_pages, form, l.attn + up256(2 * (size_t)R * c.Hq * c.D));
 }
 
 extern "C" size_t det_qdecoder_layer_kv8_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
     size_t att;
-    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, false, att).total : 0;
+    return kv8_layer_sizes_ok(cfg, R, max_pages) ? kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, kKv8Plain, att).total : 0;
 }
 
 extern "C" size_t det_qdecoder_layer_kv8_rows_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages)
 {
     size_t att;
     if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
-    return kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, true, att).total;
+    return kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, kKv8Named, att).total;
 }
 
-extern "C" int det_qdecoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
-                                      int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
-                                      const float* rope_cos, const float* rope_sin, void* ws, size_t ws_bytes, int R, void* stream)
+extern "C" size_t det_qdecoder_layer_kv8_step_workspace_bytes(const det_layer_cfg* cfg, int R, int max_pages, int weights)
 {
-    const int bad = kv8_layer_check(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, ws, R);
+    size_t att;
+    if (!kv8_layer_sizes_ok(cfg, R, max_pages) || cfg->Hq / cfg->Hkv > 16) return 0;
+    return kv8_qlayer_ws(*cfg, qlayer_ws(*cfg, R), R, max_pages, weights ? kKv8Weights : kKv8Step, att).total;
+}
+
+extern "C" int det_qdecoder_layer_kv8_step(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
+                                           int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
+                                           const float* rope_cos, const float* rope_sin, const det_kv8_step* step, void* ws, size_t ws_bytes, int R,
+                                           void* stream)
+{
+    const int bad = kv8_layer_check(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, step, ws, R);
     if (bad != DET_OK) return bad;
     const det_layer_cfg c = *cfg;
     const QLayerWs l = qlayer_ws(c, R);
     size_t att;
-    const Kv8LayerWs k = kv8_qlayer_ws(c, l, R, max_pages, slots != nullptr, att);
+    const Kv8LayerWs k = kv8_qlayer_ws(c, l, R, max_pages, kv8_form(step, slots), att);
     if (ws_bytes < k.total) return DET_EWORKSPACE;
     char* base = static_cast<char*>(ws);
     const int nq = c.Hq * c.D, n = (c.Hq + 2 * c.Hkv) * c.D;
@@ -315,10 +357,17 @@ extern "C" int det_qdecoder_layer_kv8(const det_layer_weights* w, const det_laye
     DET_TRY(det_qgemm_w4a8(base + l.codes, base + l.scales, w->wqkv, base + k.qkv, n, R, n, c.H, DET_BF16, stream));
     DET_TRY(det_kv8_rope_append(base + k.qkv, n, base + l.qbuf, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin,
                                 R, c.Hq, c.Hkv, c.D, c.Lmax, stream));
-    DET_TRY(attn_decode_kv8_impl(base + l.qbuf, cache, positions, slots, 1, base + att, base + k.attn, k.attn_bytes, R, c.Hq, c.D, c.scale,
-                                 static_cast<hipStream_t>(stream)));
+    DET_TRY(kv8_layer_attention(c, cache, step, positions, slots, base + l.qbuf, base + att, base + k.attn, k.attn_bytes, R, static_cast<hipStream_t>(stream)));
     DET_TRY(det_quant_act_q8(base + att, nq, base + l.codes, base + l.scales, R, nq, stream));
     DET_TRY(det_qgemm_w4a8_residual(base + l.codes, base + l.scales, w->wo, x_inout, c.H, x_inout, c.H, R, c.H, nq, stream));
     DET_TRY(qlayer_mlp(w, c, l, x_inout, base, R, stream));
     return DET_OK;
+}
+
+extern "C" int det_qdecoder_layer_kv8(const det_layer_weights* w, const det_layer_cfg* cfg, void* x_inout, void* pool, const int32_t* page_table,
+                                      int n_pages, int n_slots, int max_pages, const int32_t* positions, const int32_t* slots,
+                                      const float* rope_cos, const float* rope_sin, void* ws, size_t ws_bytes, int R, void* stream)
+{
+    return det_qdecoder_layer_kv8_step(w, cfg, x_inout, pool, page_table, n_pages, n_slots, max_pages, positions, slots, rope_cos, rope_sin, nullptr, ws,
+                                       ws_bytes, R, stream);
 }

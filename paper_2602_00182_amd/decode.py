@@ -9,8 +9,9 @@ prompt tokens of all sequences through each layer in one call (rows that name th
 then decodes.  Either way a sequence's bytes are those of the single-sequence, token-by-token run,
 whatever batch it sits in.
 
-With an 8-bit paged cache (DecodeModel(..., cache8=True)) the prompts of several continuations are run once and their pages shared
-(`samples`), and speculative_decode lets a second model draft tokens that the first one verifies several at a time."""
+With an 8-bit paged cache (DecodeModel(..., cache8=True)) the prompts of several continuations are run once, their pages shared (`samples`) and read once
+a step, long sequences may give up the pages that get little weight (`evict`), and speculative_decode lets a second model draft tokens that the first one
+verifies several at a time.  `rules` come between the output head and the choice of a token: penalties, biases, a grammar's masks."""
 from __future__ import annotations
 
 import contextlib
@@ -66,20 +67,25 @@ class DecodeModel:
                                        packed["wgu"], packed["wdown"])
             self.layers.append((packed, struct))
 
-    def layer_workspace_bytes(self, lcfg, rows: int, named: bool = False) -> int:
-        """For steps of `rows` rows; named: rows that name their slots, which takes less of an 8-bit cache."""
+    def layer_workspace_bytes(self, lcfg, rows: int, named: bool = False, step=None) -> int:
+        """For steps of `rows` rows; named: rows that name their slots, which takes less of an 8-bit cache; step: as layer takes it."""
         if self.cache8:
             kind = "det_qdecoder_layer_kv8" if self.quantized else "det_decoder_layer_kv8"
+            if step is not None:
+                return getattr(api, kind + "_step_workspace_bytes")(lcfg, rows, -(-lcfg.Lmax // api.KV8_PAGE), bool(step.weights))
             size = getattr(api, kind + ("_rows_workspace_bytes" if named else "_workspace_bytes"))
             return size(lcfg, rows, -(-lcfg.Lmax // api.KV8_PAGE))
         if self.quantized:
             return api.det_qdecoder_layer_workspace_bytes(lcfg, rows)
         return api.det_decoder_layer_workspace_bytes(lcfg, rows)
 
-    def layer(self, struct, lcfg, x, kcache, vcache, positions, slots, rope_cos, rope_sin, ws, stream=None):
-        """One decoder layer on rows x; slots None: row r is the sequence in cache slot r.  With an 8-bit cache kcache is the layer's pool and
-        vcache the page table."""
-        if self.cache8:
+    def layer(self, struct, lcfg, x, kcache, vcache, positions, slots, rope_cos, rope_sin, ws, stream=None, step=None):
+        """One decoder layer on rows x; slots None: row r is the sequence in cache slot r.  With an 8-bit cache kcache is the layer's pool,
+        vcache the page table, and step (api.kv8_step) may say which rows share what and where the pages' weights go."""
+        if self.cache8 and step is not None:
+            run = api.det_qdecoder_layer_kv8_step if self.quantized else api.det_decoder_layer_kv8_step
+            run(struct, lcfg, x, kcache, vcache, positions, slots, rope_cos, rope_sin, step, ws, stream)
+        elif self.cache8:
             run = api.det_qdecoder_layer_kv8 if self.quantized else api.det_decoder_layer_kv8
             run(struct, lcfg, x, kcache, vcache, positions, slots, rope_cos, rope_sin, ws, stream)
         elif self.quantized:
@@ -96,7 +102,9 @@ class DecodeModel:
 
 class DecodeState:
     """KV caches, workspace and step buffers for B sequences of up to Lmax tokens.  With an 8-bit cache `pages` holds n_pages
-    pages (None: room for all of them), reserved at once unless reserve is False."""
+    pages (None: room for all of them), reserved at once unless reserve is False; `groups` (the first sequence of each group, and B; None) says which
+    sequences share pages that a step is to read once, and to `weights` ([B, pages of a sequence] fp32 or None) it adds what weight each page gets, over all
+    layers.  What a group shares is what the pages' tables say when the step is launched; a captured step keeps what they said then."""
 
     def __init__(self, model: DecodeModel, B: int, Lmax: int, rope_cos, rope_sin, reserve: bool = True, n_pages: int | None = None):
         c = model.cfg
@@ -117,6 +125,7 @@ class DecodeState:
                            for _ in range(c.n_layers)]
             self.vcache = [torch.zeros_like(k) for k in self.kcache]
         self.ws = torch.empty(model.layer_workspace_bytes(self.lcfg, B), dtype=torch.uint8, device=dev)
+        self.groups = self.weights = self._step = None
         self._buffers(B)
 
     def _buffers(self, rows: int):
@@ -131,9 +140,29 @@ class DecodeState:
         self.positions = torch.empty(rows, dtype=torch.int32, device=dev)
         self.slots = None
 
+    def _told(self):
+        """What the layers are told of groups and weights: as the pages lie now."""
+        if self.groups is None and self.weights is None:
+            return None
+        now = (tuple(self.groups or ()), self.weights, self.pages.version)
+        if self._step is None or self._step[0][0] != now[0] or self._step[0][1] is not now[1] or self._step[0][2] != now[2]:
+            rows = shared = None
+            if self.groups is not None:
+                g, dev = list(self.groups), self.tokens.device
+                if g[0] != 0 or g[-1] != self.B or any(a >= b for a, b in zip(g, g[1:])):
+                    raise ValueError("groups of sequences, one behind the other")
+                rows = torch.tensor(g, dtype=torch.int32).to(dev)
+                shared = torch.tensor([self.pages.shared_tokens(range(a, b)) for a, b in zip(g, g[1:])], dtype=torch.int32).to(dev)
+            self._step = (now, api.kv8_step(rows, shared, self.weights))
+            size = self.model.layer_workspace_bytes(self.lcfg, self.B, step=self._step[1])
+            if self.ws.nbytes < size:
+                self.ws = torch.empty(size, dtype=torch.uint8, device=self.tokens.device)
+        return self._step[1]
+
     def of_rows(self, slots: torch.Tensor) -> "DecodeState":
         """A state over the same caches whose steps take one row for each entry of slots (several rows may name one sequence)."""
         st = copy.copy(self)
+        st.groups = st.weights = st._step = None
         st.ws = torch.empty(self.model.layer_workspace_bytes(self.lcfg, slots.shape[0], named=True), dtype=torch.uint8, device=slots.device)
         st._buffers(slots.shape[0])
         st.slots = slots
@@ -142,10 +171,11 @@ class DecodeState:
     def forward(self, stream=None):
         """One decode step on self.tokens / self.positions; leaves fp32 logits in self.logits."""
         m, c = self.model, self.model.cfg
+        step = self._told()
         api.det_embed_gather(m.embed, self.tokens, self.x, stream)
         for i, (_, struct) in enumerate(m.layers):
             m.layer(struct, self.lcfg, self.x, self.kcache[i], self.vcache[i], self.positions, self.slots, self.rope_cos,
-                    self.rope_sin, self.ws, stream)
+                    self.rope_sin, self.ws, stream, step)
         self.head(stream)
 
     def head(self, stream=None):
@@ -168,6 +198,81 @@ class SamplingPolicy:
     top_p: float
     seed: int
     seq_ids: torch.Tensor
+
+
+@dataclass
+class Grammar:
+    """Which tokens may come where, as an automaton over classes of tokens: in state s the tokens whose bit in masks[s] ([n_states, ceil(V / 32)] int32) is
+    set; a token leads to transitions[s, class] ([n_states, n_classes] int32; -1: nothing is barred from there on).  token_class [V] int32 or None (every
+    token is its own class); start: the state in which every sequence begins.  Tensors on the device."""
+    masks: torch.Tensor
+    transitions: torch.Tensor
+    token_class: torch.Tensor | None = None
+    start: int = 0
+
+
+@dataclass
+class LogitsPolicy:
+    """Rules on the logits of every step (det_logits_process): tokens of the prompt or generated so far are made less likely by `repetition` (their
+    logits divided, where positive, or multiplied by it), generated ones also by `frequency` for each time and by `presence` once; `biases`
+    {token: added}; `grammar`.  The same for every sequence of a call."""
+    repetition: float = 1.0
+    frequency: float = 0.0
+    presence: float = 0.0
+    biases: dict | None = None
+    grammar: Grammar | None = None
+
+
+@dataclass
+class EvictPolicy:
+    """A sequence of an 8-bit cache comes back to `keep` pages every `every` steps: of those but its first and last ones it gives up the pages that its
+    generated tokens, over all layers and heads, have given the least weight (KVPages.evict)."""
+    keep: int
+    every: int = 64
+    first: int = 1
+    recent: int = 4
+
+
+class _Rules:
+    """A LogitsPolicy while B sequences are decoded: their history and grammar states, on the device."""
+
+    def __init__(self, policy: LogitsPolicy, prompts, lens_host, n_new: int, V: int, out):
+        B, dev = len(lens_host), prompts.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.out = out
+        self.history = self.lens = self.grammar = self.states = None
+        given = {}
+        if (policy.repetition, policy.frequency, policy.presence) != (1.0, 0.0, 0.0):
+            if not policy.repetition > 0:
+                raise ValueError("repetition is a factor above 0")
+            self.history = torch.zeros((B, int(lens_host.max()) + n_new), **i32)
+            self.history[:, :prompts.shape[1]] = prompts[:, :self.history.shape[1]]
+            begin = lens_host.to(torch.int32).to(dev)
+            self.lens = begin.clone()
+            values = torch.tensor([policy.repetition, policy.frequency, policy.presence], dtype=torch.float32)
+            given |= dict(penalties=values.repeat(B, 1).to(dev), history=self.history, history_lens=self.lens, generated_from=begin)
+        if policy.biases:
+            n = len(policy.biases)
+            given |= dict(bias_begin=(torch.arange(B + 1, dtype=torch.int32) * n).to(dev),
+                          bias_tokens=torch.tensor(list(policy.biases), dtype=torch.int32).repeat(B).to(dev),
+                          bias_values=torch.tensor(list(policy.biases.values()), dtype=torch.float32).repeat(B).to(dev))
+        if policy.grammar is not None:
+            self.grammar = policy.grammar
+            self.states = torch.full((B,), policy.grammar.start, **i32)
+            given |= dict(masks=policy.grammar.masks, mask_rows=self.states)
+        self.rules = api.logits_rules(**given)
+
+    def process(self, logits, stream):
+        """The logits with the rules applied, in `out` (None: in their own place)."""
+        out = logits if self.out is None else self.out
+        api.det_logits_process(logits, out, self.rules, stream)
+        return out
+
+    def advance(self, tokens, stream):
+        g = self.grammar
+        if self.history is not None or g is not None:
+            api.det_logits_advance(tokens, self.history, self.lens, self.lens, None if g is None else g.transitions,
+                                   None if g is None else g.token_class, self.states, self.states, stream)
 
 
 def greedy_decode(model: DecodeModel, prompts: torch.Tensor, prompt_lens: torch.Tensor, n_new: int,
@@ -212,8 +317,12 @@ def _greedy_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, keep_
     return gen, kept
 
 
-def _select(policy, logits, positions, out, stream):
-    if policy is None:
+def _select(policy, logits, positions, out, stream, rules=None):
+    if rules is not None:
+        logits = rules.process(logits, stream)
+        _select(policy, logits, positions, out, stream)
+        rules.advance(out, stream)
+    elif policy is None:
         api.det_argmax(logits, out, stream)
     else:
         api.det_sample(logits, policy.temperature, policy.top_k, policy.top_p, policy.seed, policy.seq_ids,
@@ -222,11 +331,15 @@ def _select(policy, logits, positions, out, stream):
 
 def prefill_decode(model: DecodeModel, prompts: torch.Tensor, prompt_lens: torch.Tensor, n_new: int,
                    rope_cos: torch.Tensor, rope_sin: torch.Tensor, stream=None,
-                   policy: SamplingPolicy | None = None, keep_logits: bool = False, samples: int = 1):
+                   policy: SamplingPolicy | None = None, keep_logits: bool = False, samples: int = 1, rules: LogitsPolicy | None = None,
+                   evict: EvictPolicy | None = None):
     """Same results as greedy_decode, with the prompts processed in one pass.
 
     samples > 1 (8-bit cache): that many continuations of each prompt, sequence b * samples + i the i-th of prompt b, as if every prompt
-    stood samples times in `prompts`; each prompt is run once and its pages are shared, but for the last one where it is not full.
+    stood samples times in `prompts`; each prompt is run once and its pages are shared, but for the last one where it is not full, and read once a step.
+
+    rules: what the logits go through before a token is chosen (kept logits are those of the head).  evict (8-bit cache): sequences give up pages as they
+    go on, which changes what they attend to, but not with the batch they are in.
 
     Prefill: row r is token prompts[b, p] with position p and cache slot b, for every b and p < len_b
     (R = sum of the lengths).  Each layer writes all keys and values first and then lets row r attend
@@ -237,16 +350,18 @@ def prefill_decode(model: DecodeModel, prompts: torch.Tensor, prompt_lens: torch
     Returns (generated [B, n_new] int32 on the device, list of n_new logits clones [B, V] if
     keep_logits else [])."""
     with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-        return _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stream, policy, keep_logits, samples)
+        return _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stream, policy, keep_logits, samples, rules, evict)
 
 
-def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stream, policy, keep_logits, samples):
+def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stream, policy, keep_logits, samples, rules, evict):
     c = model.cfg
     B, _ = prompts.shape
     dev = prompts.device
     lens_host = prompt_lens.cpu().to(torch.int64)
     if samples < 1 or (samples > 1 and not model.cache8):
         raise ValueError("several continuations of a prompt need the 8-bit paged cache")
+    if evict is not None and (not model.cache8 or evict.keep < 1 or evict.every < 1 or evict.first < 0 or evict.recent < 1):
+        raise ValueError("pages that are given up need the 8-bit paged cache, and a page that stays")
     T = int(lens_host.max()) + n_new - 1
     if rope_cos.shape[0] < T:
         raise ValueError("rope tables shorter than the run")
@@ -280,18 +395,28 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
         for b, n in enumerate(lens_host.tolist()):
             st.pages.fork(b * samples, range(b * samples + 1, (b + 1) * samples), n, stream)
         st.pages.reserve(range(B * samples), [T] * (B * samples), torch.repeat_interleave(lens_host, samples).tolist(), stream)
+    groups = list(range(0, B * samples + 1, samples)) if samples > 1 and int(lens_host.max()) >= api.KV8_SHARED_CHUNK else None
+    weights = torch.zeros(st.pages.table.shape, dtype=torch.float32, device=dev) if evict is not None else None
+    st.groups, st.weights = groups, weights
+    of_rules = None
+    if rules is not None:
+        out = torch.empty_like(st.logits) if keep_logits else None
+        of_rules = _Rules(rules, torch.repeat_interleave(prompts.to(torch.int32), samples, 0), torch.repeat_interleave(lens_host, samples), n_new, c.V, out)
+    kept_pages = torch.full((B * samples,), evict.keep, dtype=torch.int32, device=dev) if evict is not None else None
 
     gen = torch.zeros((n_new, B * samples), dtype=torch.int32, device=dev)
     kept = []
     base_pos = torch.repeat_interleave(lens_host - 1, samples).to(torch.int32).to(dev)   # position of each sequence's last prompt token
     st.positions.copy_(base_pos)
-    _select(policy, st.logits, st.positions, gen[0], stream)
+    _select(policy, st.logits, st.positions, gen[0], stream, of_rules)
     if keep_logits:
         kept.append(st.logits.clone())
     for j in range(1, n_new):
         api.det_decode_advance(gen[j - 1], base_pos, j, st.tokens, st.positions, stream)
+        if evict is not None and j % evict.every == 0:
+            st.pages.evict(weights, st.positions, kept_pages, evict.first, evict.recent, stream)
         st.forward(stream)
-        _select(policy, st.logits, st.positions, gen[j], stream)
+        _select(policy, st.logits, st.positions, gen[j], stream, of_rules)
         if keep_logits:
             kept.append(st.logits.clone())
     return gen.t().contiguous(), kept

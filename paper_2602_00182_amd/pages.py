@@ -1,7 +1,8 @@
 """Bookkeeping of an 8-bit paged KV cache (host integers; the bytes move in det_kv8_copy_pages).
 
 A pool of pages for all layers and a table [slots, max_pages] on the device that names the pages of each slot.  Slots may share pages (`fork`); a shared
-page is copied before a slot may write into it (`reserve`); a page that no slot names is free again.  The table tensor keeps its address, so a captured
+page is copied before a slot may write into it (`reserve`); a page that no slot names is free again.  A slot may give up pages that its attention gave
+little weight to (`evict`); they are holes in its table, and the tokens behind them keep their positions.  The table tensor keeps its address, so a captured
 graph sees what it holds at the replay."""
 from __future__ import annotations
 
@@ -28,6 +29,7 @@ class KVPages:
         self._forked = [0] * n_slots                # tokens of each slot up to which a fork shared its pages: it goes on behind them
         self._refs = [0] * n_pages
         self._free = list(range(n_pages))           # a heap: the lowest page first
+        self.version = 0                            # another one whenever the table has changed
 
     @property
     def free_pages(self) -> int:
@@ -40,7 +42,7 @@ class KVPages:
                 raise ValueError(f"slot {slot} of {len(self._pages)}")
 
     def pages(self, slot: int) -> list[int]:
-        """The pages of a slot, in order."""
+        """The pages of a slot, in order; -1 where one was given up."""
         self._slots(slot)
         return list(self._pages[slot])
 
@@ -53,9 +55,12 @@ class KVPages:
         for slot, pages in enumerate(self._pages):
             self._host[slot].fill_(-1)
             self._host[slot, :len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        self.version += 1
         self.table.copy_(self._host)
 
     def _drop(self, page: int) -> None:
+        if page < 0:
+            return
         self._refs[page] -= 1
         if self._refs[page] == 0:
             heapq.heappush(self._free, page)
@@ -83,7 +88,12 @@ class KVPages:
         # how many references to each page go before its last sharer may keep it
         refs = dict()
         for slot, begin, count in want:
-            for page in self._pages[slot][begin // api.KV8_PAGE:]:
+            for i, page in enumerate(self._pages[slot][begin // api.KV8_PAGE:], begin // api.KV8_PAGE):
+                if page < 0:
+                    if i * api.KV8_PAGE < begin:
+                        raise ValueError("tokens in front of write_from lie in a page that was given up")
+                    need += 1
+                    continue
                 r = refs.get(page, self._refs[page])
                 if r > 1:
                     refs[page] = r - 1
@@ -96,7 +106,10 @@ class KVPages:
             for slot, begin, count in want:
                 pages = self._pages[slot]
                 for i in range(begin // api.KV8_PAGE, len(pages)):
-                    if self._refs[pages[i]] > 1:
+                    if pages[i] < 0:
+                        pages[i] = heapq.heappop(self._free)
+                        self._refs[pages[i]] = 1
+                    elif self._refs[pages[i]] > 1:
                         page = heapq.heappop(self._free)
                         if i * api.KV8_PAGE < begin:
                             copies.append((pages[i], page))
@@ -123,7 +136,8 @@ class KVPages:
                 self._forked[s] = length
                 self._forked[src] = max(self._forked[src], length)
                 for page in self._pages[s]:
-                    self._refs[page] += 1
+                    if page >= 0:
+                        self._refs[page] += 1
             self._write_table()
 
     def truncate(self, slot: int, length: int, stream=None) -> None:
@@ -141,6 +155,37 @@ class KVPages:
 
     def release(self, slot: int, stream=None) -> None:
         self.truncate(slot, 0, stream)
+
+    def evict(self, weights, lengths, keep, first: int = 1, recent: int = 4, stream=None) -> list[list[int]]:
+        """Each slot of lengths[s] tokens comes back to keep[s] pages: of those but its first `first` and last `recent` ones, it gives up the pages of least
+        weight (det_kv8_pick_pages on weights [slots, max_pages], which attention with weights has added up; lengths and keep are int32 tensors on the
+        device).  A page that other slots name stays theirs.  Waits for the device.  Returns the places in each slot's table that are holes now."""
+        if recent < 1:
+            raise ValueError("the page that is written goes on being there")
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            dropped = torch.empty(self.table.shape, dtype=torch.uint8, device=self.table.device)
+            api.det_kv8_pick_pages(weights, self.table, self.pool.shape[1], lengths, keep, first, recent, dropped, stream)
+            return self._give_up(dropped.cpu())
+
+    def _give_up(self, dropped) -> list[list[int]]:
+        gone = [[i for i in range(len(pages)) if dropped[slot, i] and pages[i] >= 0] for slot, pages in enumerate(self._pages)]
+        for slot, places in enumerate(gone):
+            for i in places:
+                self._drop(self._pages[slot][i])
+                self._pages[slot][i] = -1
+        self._write_table()
+        return gone
+
+    def shared_tokens(self, slots) -> int:
+        """How many of their first tokens the slots hold in the same pages (whole pages; ones that all have given up among them): what groups of rows say."""
+        self._slots(*slots)
+        pages = [self._pages[s] for s in slots]
+        same = 0
+        for of in zip(*pages):
+            if any(p != of[0] for p in of):
+                break
+            same += 1
+        return same * api.KV8_PAGE
 
     def compact(self, stream=None) -> int:
         """Moves the pages in use to the front of the pool; returns how many there are."""
