@@ -708,54 +708,63 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
 }
 
 // The chunks of a (row, head) of more than one chunk, folded in ascending order: the operations of kv8_attn_combine_kernel (attn_kv8.hip), down to the
-// empty chunks it ends with (a multiple of sixteen in all).  Four columns a lane, so that what every lane works out of a chunk's (m, l) serves four sums:
-// with one column a lane those instructions took the launch (32 us for 64 rows of 32 heads and 126 chunks; XX so).
-constexpr int kFoldChunks = 8, kCombineThreads = 128, kCombineHeads = kCombineThreads / 32;
+// empty chunks it ends with (a multiple of sixteen in all).  A wave has a head, a lane two columns.  The factors of 64 chunks come from one load, a chunk a
+// lane: the largest score so far is a maximum over the lanes in front (exact in any order), the factors follow from it, and are read from their lane
+// while the sums are folded.  That leaves ten instructions a chunk and takes the statistics out of the way between two trips to memory: worked out by every
+// lane, a column each, they were the launch (64 rows of 32 heads and 126 chunks 33 us, now XX; 8 rows of 16 heads and up to 79 chunks 10.6, now XX).
+constexpr int kFoldChunks = 16, kCombineThreads = 128, kCombineHeads = kCombineThreads / kWave;
 __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t block)
 {
-    const int lane = threadIdx.x & 31;
-    const size_t at = block * kCombineHeads + threadIdx.x / 32;
-    int slot, len = 0;
-    if (at < (size_t)a.R * a.Hq) len = row_length(a, (int)(at / a.Hq), slot);
-    const int chunks = len > kChunk ? (len + kChunk - 1) / kChunk : 0;
-    if (chunks == 0) return;
+    const int lane = threadIdx.x & 63;
+    const size_t at = block * kCombineHeads + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (at >= (size_t)a.R * a.Hq) return;
+    int slot;
+    const int len = row_length(a, (int)(at / a.Hq), slot);
+    if (len <= kChunk) return;
+    const int chunks = (len + kChunk - 1) / kChunk, all = (chunks + 15) & ~15;
     const float4* ps = a.part + at * a.chunks;
-    const float4* po = reinterpret_cast<const float4*>(a.part_o + at * a.chunks * kHeadDim) + lane;
-    float4 x[2][kFoldChunks], st[2][kFoldChunks];
-    auto ask = [&](int to, int c0) {
+    const float2* po = reinterpret_cast<const float2*>(a.part_o + at * a.chunks * kHeadDim) + lane;
+    float2 x[2][kFoldChunks];
+    auto ask = [&](float2 (&to)[kFoldChunks], int c0) {
 #pragma unroll
-        for (int k = 0; k < kFoldChunks; ++k) {
-            const int c = min(c0 + k, chunks - 1);
-            st[to][k] = ps[c];
-            x[to][k] = po[(size_t)c * (kHeadDim / 4)];
-        }
+        for (int k = 0; k < kFoldChunks; ++k) to[k] = po[(size_t)min(c0 + k, chunks - 1) * (kHeadDim / 2)];
     };
-    ask(0, 0);
+    auto ask_part = [&](int c) { return c < chunks ? ps[c] : make_float4(-__builtin_inff(), 0.0f, 1.0f, 0.0f); };
+    auto lane_of = [](float v, int from) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), from)); };
+    float4 st = ask_part(lane);
+    ask(x[0], 0);
     float m = -__builtin_inff(), l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto fold = [&](int of, int c0) {
-        const float4(&from)[kFoldChunks] = x[of];
+    float2 o = make_float2(0.0f, 0.0f);
+    for (int c0 = 0; c0 < all; c0 += kWave) {
+        float top = st.x;
 #pragma unroll
-        for (int k = 0; k < kFoldChunks; ++k) {  // past the last chunk: one without tokens, which changes nothing
-            const bool there = c0 + k < chunks;
-            float fa, fb;
-            fold_step(m, l, there ? st[of][k].x : -__builtin_inff(), there ? st[of][k].y : 0.0f, st[of][k].z, fa, fb);
-            o.x = fold_value(o.x, there ? from[k].x : 0.0f, fa, fb);
-            o.y = fold_value(o.y, there ? from[k].y : 0.0f, fa, fb);
-            o.z = fold_value(o.z, there ? from[k].z : 0.0f, fa, fb);
-            o.w = fold_value(o.w, there ? from[k].w : 0.0f, fa, fb);
+        for (int off = 1; off < kWave; off <<= 1) {
+            const float y = __shfl_up(top, off, kWave);
+            top = lane >= off ? fmaxf(top, y) : top;
         }
-    };
-    const int all = (chunks + 15) & ~15;
-    for (int c0 = 0; c0 < all; c0 += 2 * kFoldChunks) {
-        ask(1, c0 + kFoldChunks);
-        fold(0, c0);
-        if (c0 + 2 * kFoldChunks < all) ask(0, c0 + 2 * kFoldChunks);
-        fold(1, c0 + kFoldChunks);
+        top = fmaxf(m, top);
+        const float up = __shfl_up(top, 1, kWave);
+        const float fa = pow2_step(lane == 0 ? m : up, top), fl = pow2_step(st.x, top), fb = fl * st.z, lc = st.y;
+        m = lane_of(top, kWave - 1);
+        st = ask_part(c0 + kWave + lane);
+#pragma unroll
+        for (int q = 0; q < kWave / kFoldChunks; ++q) {
+            const int c = c0 + q * kFoldChunks;
+            if (c >= all) break;
+            if (c + kFoldChunks < all) ask(x[(q + 1) & 1], c + kFoldChunks);
+#pragma unroll
+            for (int k = 0; k < kFoldChunks; ++k) {  // past the last chunk: one without tokens, which changes nothing
+                const int i = q * kFoldChunks + k;
+                const bool there = c + k < chunks;
+                const float by = lane_of(fa, i), in = lane_of(fb, i);
+                l = __builtin_fmaf(lane_of(lc, i), lane_of(fl, i), l * by);
+                o.x = fold_value(o.x, there ? x[q & 1][k].x : 0.0f, by, in);
+                o.y = fold_value(o.y, there ? x[q & 1][k].y : 0.0f, by, in);
+            }
+        }
     }
     const float by = row_factor(l);
-    stream_store(a.out + at * kHeadDim + 4 * lane, make_uint2((uint32_t)to_bf16(o.x * by) | (uint32_t)to_bf16(o.y * by) << 16,
-                                                              (uint32_t)to_bf16(o.z * by) | (uint32_t)to_bf16(o.w * by) << 16));
+    __builtin_nontemporal_store((uint32_t)to_bf16(o.x * by) | (uint32_t)to_bf16(o.y * by) << 16, reinterpret_cast<uint32_t*>(a.out + at * kHeadDim) + lane);
 }
 
 // ---------------------------------------------------------------- the pages' weights
@@ -764,6 +773,7 @@ __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t b
 // head; the rows' largest scores and sums are folded here again, beside the heads' own workgroups instead of behind them.  Sums in a fixed order:
 // of each eighth the rows ascending and in a row its heads, then the eighths.  A row whose softmax is not finite adds nothing.
 constexpr int kWeightChunks = 16, kWeightParts = kCombineThreads / kWeightChunks;
+constexpr int kWeightHeads = 4, kStatChunks = 32;  // heads of a thread, chunks of a head, that are asked for at once
 struct weights_lds {
     float2 stats[kCombineThreads];
     float4 parts[kWeightParts - 1][kWeightChunks];
@@ -777,34 +787,47 @@ __device__ __forceinline__ void page_weights(const kv8_shared_args& a, weights_l
         const int len = row_length(a, row, its), chunks = (len + kChunk - 1) / kChunk;
         if (its != slot || block * kWeightChunks >= chunks) return;
         for (int h0 = 0; h0 < a.Hq; h0 += kCombineThreads) {
+            const int count = min(a.Hq - h0, kCombineThreads);
+            // what this thread adds of its first heads is asked for before the statistics are worked out
+            float4 e[kWeightHeads];
+            float mc[kWeightHeads];
+            auto ask = [&](int h) {
+#pragma unroll
+                for (int k = 0; k < kWeightHeads; ++k) {
+                    const size_t at = ((size_t)row * a.Hq + h0 + min(h + k * kWeightParts, count - 1)) * a.chunks + min(chunk, chunks - 1);
+                    e[k] = a.page_sums[at];
+                    mc[k] = a.part[at].x;
+                }
+            };
+            ask(part);
             __syncthreads();
-            if (h0 + tid < a.Hq) {
+            if (tid < count) {
                 const float4* ps = a.part + ((size_t)row * a.Hq + h0 + tid) * a.chunks;
                 float m = -__builtin_inff(), l = 0.0f, fa, fb;
-                for (int c0 = 0; c0 < chunks; c0 += 8) {
-                    float4 st[8];
+                for (int c0 = 0; c0 < chunks; c0 += kStatChunks) {
+                    float2 st[kStatChunks];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) st[k] = ps[min(c0 + k, chunks - 1)];
+                    for (int k = 0; k < kStatChunks; ++k) st[k] = *reinterpret_cast<const float2*>(&ps[min(c0 + k, chunks - 1)]);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (c0 + k < chunks) fold_step(m, l, st[k].x, st[k].y, st[k].z, fa, fb);
+                    for (int k = 0; k < kStatChunks; ++k)
+                        if (c0 + k < chunks) fold_step(m, l, st[k].x, st[k].y, 1.0f, fa, fb);
                 }
                 lds.stats[tid] = make_float2(m, row_factor(l));
             }
             __syncthreads();
-            if (chunk >= chunks) continue;
-            const int count = min(a.Hq - h0, kCombineThreads);
-#pragma unroll 4
-            for (int h = part; h < count; h += kWeightParts) {
-                const size_t at = ((size_t)row * a.Hq + h0 + h) * a.chunks + chunk;
-                const float2 st = lds.stats[h];
-                const float4 e = a.page_sums[at];
-                float by = pow2_step(a.part[at].x, st.x) * st.y;
-                const bool fine = by < __builtin_inff();
-                sum.x = fine ? __builtin_fmaf(e.x, by, sum.x) : sum.x;
-                sum.y = fine ? __builtin_fmaf(e.y, by, sum.y) : sum.y;
-                sum.z = fine ? __builtin_fmaf(e.z, by, sum.z) : sum.z;
-                sum.w = fine ? __builtin_fmaf(e.w, by, sum.w) : sum.w;
+            for (int h = part; h < count; h += kWeightHeads * kWeightParts) {
+                if (h != part) ask(h);
+#pragma unroll
+                for (int k = 0; k < kWeightHeads; ++k) {
+                    if (h + k * kWeightParts >= count) break;
+                    const float2 st = lds.stats[h + k * kWeightParts];
+                    const float by = pow2_step(mc[k], st.x) * st.y;
+                    const bool fine = by < __builtin_inff() && chunk < chunks;
+                    sum.x = fine ? __builtin_fmaf(e[k].x, by, sum.x) : sum.x;
+                    sum.y = fine ? __builtin_fmaf(e[k].y, by, sum.y) : sum.y;
+                    sum.z = fine ? __builtin_fmaf(e[k].z, by, sum.z) : sum.z;
+                    sum.w = fine ? __builtin_fmaf(e[k].w, by, sum.w) : sum.w;
+                }
             }
         }
     };
