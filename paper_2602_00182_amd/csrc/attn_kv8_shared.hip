@@ -21,7 +21,9 @@ struct kv8_shared_args : kv8_attn_args {
     float4* page_sums;          // [R, Hq, chunks]: of each page of a chunk the sum of its e, or null
     const float* weights_in;    // [n_slots, max_pages] or null
     float* weights_out;
-    int group_wgs, group_steps; // workgroups of a KV head that take shared chunks; of them to a tile
+    int group_wgs, group_steps; // workgroups of a KV head that take shared chunks (at most 2^15 of runs); of them to a tile
+    int part_rows;              // rows of a tile, or of the four that go together
+    uint32_t part_inverse;
     int row_steps;              // workgroups of a KV head to a row
 };
 
@@ -61,37 +63,41 @@ __device__ __forceinline__ int chunks_before(const kv8_shared_args& a, kv8_group
     return 0;
 }
 
-// How much of something each group has, in all, and the group that number `at` of it falls into, with what lies in front of it there.
+// How much of something (a count of each group) lies in front of and in this lane's group.
 template <class Count>
-__device__ __forceinline__ int count_groups(const kv8_shared_args& a, kv8_group mine, Count count)
-{
-    int all = 0;
-    for (int base = 0; base < a.n_groups; base += kWave) {
-        if (base > 0) mine = group_at(a, base + (threadIdx.x & 63));
-        all += count(mine);
-    }
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) all += __shfl_xor(all, off, kWave);
-    return __builtin_amdgcn_readfirstlane(all);
-}
-template <class Count>
-__device__ __forceinline__ kv8_group find_group(const kv8_shared_args& a, kv8_group mine, int at, int& within, Count count)
+__device__ __forceinline__ int count_up(const kv8_group& mine, Count count)
 {
     const int lane = threadIdx.x & 63;
+    int sum = count(mine);
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int x = __shfl_up(sum, off, kWave);
+        sum += lane >= off ? x : 0;
+    }
+    return sum;
+}
+// How much of it there is in all; sum: count_up of the first 64 groups.
+template <class Count>
+__device__ __forceinline__ int count_groups(const kv8_shared_args& a, int sum, Count count)
+{
+    int all = __builtin_amdgcn_readlane(sum, kWave - 1);
+    for (int base = kWave; base < a.n_groups; base += kWave) all += __builtin_amdgcn_readlane(count_up(group_at(a, base + (threadIdx.x & 63)), count), kWave - 1);
+    return all;
+}
+// The group that number `at` of it falls into, and how much lies in front of it there.
+template <class Count>
+__device__ __forceinline__ kv8_group find_group(const kv8_shared_args& a, kv8_group mine, int sum, int at, int& within, Count count)
+{
     int before = 0;
     for (int base = 0; base < a.n_groups; base += kWave) {
-        if (base > 0) mine = group_at(a, base + lane);
-        const int its = count(mine);
-        int sum = its;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const int x = __shfl_up(sum, off, kWave);
-            sum += lane >= off ? x : 0;
+        if (base > 0) {
+            mine = group_at(a, base + (threadIdx.x & 63));
+            sum = count_up(mine, count);
         }
         const unsigned long long past = __ballot(before + sum > at);
         if (past != 0) {
             const int g = __builtin_ctzll(past);
-            within = at - before - (__builtin_amdgcn_readlane(sum, g) - __builtin_amdgcn_readlane(its, g));
+            within = at - before - (g > 0 ? __builtin_amdgcn_readlane(sum, g - 1) : 0);
             return group_of_lane(mine, g);
         }
         before += __builtin_amdgcn_readlane(sum, kWave - 1);
@@ -100,31 +106,23 @@ __device__ __forceinline__ kv8_group find_group(const kv8_shared_args& a, kv8_gr
     return kv8_group{0, 0, 0, 0};
 }
 
-// Tile number `tile` of all groups' tiles of rows_per_tile rows: its rows; rows = 0 where there is none.
-__device__ __forceinline__ kv8_group tile_of_groups(const kv8_shared_args& a, const kv8_group& mine, int tile)
-{
-    int nth;
-    kv8_group o = find_group(a, mine, tile, nth, [&](const kv8_group& g) { return g.chunks > 0 ? (g.rows + a.rows_per_tile - 1) / a.rows_per_tile : 0; });
-    o.row0 = o.first + nth * a.rows_per_tile;
-    o.rows = min(o.rows - nth * a.rows_per_tile, a.rows_per_tile);
-    return o;
-}
-
-// The groups' shared chunks times the sets of four tiles that read them (below 2^30 in all); number `at` of them: the set's rows and its chunk.
-struct sets_of_groups {
-    int rows;  // of a set
-    __device__ __forceinline__ int operator()(const kv8_group& g) const { return g.chunks > 0 ? (g.rows + rows - 1) / rows * g.chunks : 0; }
+// Rows by tiles, or by sets of four tiles, of a group; n / rows by one multiplication (rows <= 64, n below 2^17).
+struct parts_of_groups {
+    int rows;          // of a part
+    uint32_t inverse;  // 2^32 / rows, rounded up
+    bool chunks;       // a part counts once for each shared chunk
+    __device__ __forceinline__ int operator()(const kv8_group& g) const
+    {
+        const int parts = rows == 1 ? g.rows : (int)__umulhi((uint32_t)(g.rows + rows - 1), inverse);
+        return g.chunks > 0 ? (chunks ? parts * g.chunks : parts) : 0;
+    }
 };
-__device__ __forceinline__ kv8_group place_in_groups(const kv8_shared_args& a, const kv8_group& mine, int at, int& chunk)
+
+// Part number `nth` of a group: its rows.
+__device__ __forceinline__ void take_part(kv8_group& g, int nth, int rows)
 {
-    const sets_of_groups sets{4 * a.rows_per_tile};
-    int in;
-    kv8_group o = find_group(a, mine, at, in, sets);
-    const int set = o.chunks > 0 ? in / o.chunks : 0;
-    chunk = in - set * o.chunks;
-    o.row0 = o.first + sets.rows * set;
-    o.rows = min(o.rows - sets.rows * set, sets.rows);
-    return o;
+    g.row0 = g.first + nth * rows;
+    g.rows = min(g.rows - nth * rows, rows);
 }
 
 // ---------------------------------------------------------------- chunks of a tile
@@ -669,20 +667,26 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     if constexpr (FORM != kNoGroups) {
         mine = group_at(a, threadIdx.x & 63);
         if (nth < a.group_wgs) {
+            const parts_of_groups parts{a.part_rows, a.part_inverse, FORM == kRuns};
+            const int sum = count_up(mine, parts);
             if constexpr (FORM == kRuns) {
-                const long long all = count_groups(a, mine, sets_of_groups{4 * a.rows_per_tile});
-                int at = (int)(all * nth / a.group_wgs);
-                const int to = (int)(all * (nth + 1) / a.group_wgs);
+                // the shared chunks of all sets of tiles (below 2^30) in group_wgs runs
+                const int all = count_groups(a, sum, parts), each = all / a.group_wgs, rest = all - each * a.group_wgs;
+                int at = each * nth + rest * nth / a.group_wgs;
+                const int to = each * (nth + 1) + rest * (nth + 1) / a.group_wgs;
                 while (at < to) {
-                    int c0;
-                    const kv8_group set = place_in_groups(a, mine, at, c0);
+                    int in;
+                    kv8_group set = find_group(a, mine, sum, at, in, parts);
                     if (set.chunks == 0) return;
-                    const int c1 = min(set.chunks, c0 + to - at);
+                    const int nth_set = in / set.chunks, c0 = in - nth_set * set.chunks, c1 = min(set.chunks, c0 + to - at);
+                    take_part(set, nth_set, a.part_rows);
                     chunks_of_tiles<WEIGHTS>(a, lds, kvh, set.row0, set.rows, a.slots ? a.slots[set.first] : set.first, c0, c1);
                     at += c1 - c0;
                 }
             } else {
-                const kv8_group tile = tile_of_groups(a, mine, nth / a.group_steps);
+                int in;
+                kv8_group tile = find_group(a, mine, sum, nth / a.group_steps, in, parts);
+                take_part(tile, in, a.part_rows);
                 const int first = nth % a.group_steps;
                 if (first >= tile.chunks) return;
                 // the pages are those of the group's first row
@@ -953,6 +957,8 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
             a.group_wgs = (int)(tiles * a.group_steps);
         }
     }
+    a.part_rows = (ring ? 4 : 1) * a.rows_per_tile;
+    a.part_inverse = a.part_rows > 1 ? (uint32_t)((1ull << 32) / a.part_rows + ((1ull << 32) % a.part_rows != 0)) : 0u;
     const long long grid = (a.group_wgs + (long long)R * a.row_steps) * cache.Hkv, blocks = weights ? (a.chunks + kWeightChunks - 1) / kWeightChunks : 0,
                     second = blocks * cache.n_slots + ((long long)R * Hq + kCombineHeads - 1) / kCombineHeads;
     if (grid > 0x7FFFFFFFll / 256 || second > 0x7FFFFFFFll / kCombineThreads) return DET_ESHAPE;
