@@ -858,8 +858,9 @@ def det_attn_decode_kv8_weights(q, pool, page_table, seqlens, slots, group_rows,
 def det_kv8_pick_pages(weights, page_table, n_pages: int, lengths, keep, first: int, recent: int, dropped, stream=None) -> None:
     """dropped [n_slots, max_pages] (bytes): 1 for the pages of least weight that bring a slot of lengths[s] tokens back to keep[s] pages; the first
     `first` and the last `recent` pages stay."""
-    shape = n_slots, max_pages = page_table.shape
-    if weights.shape != shape or dropped.shape != shape or lengths.shape != (n_slots,) or keep.shape != (n_slots,):
+    shape, of_slots = page_table.shape, lengths.shape
+    n_slots, max_pages = shape
+    if weights.shape != shape or dropped.shape != shape or of_slots != (n_slots,) or keep.shape != of_slots:
         raise ValueError("bad page shapes")
     _check("det_kv8_pick_pages", lib().det_kv8_pick_pages(
         _contig(weights, torch.float32), _contig(page_table, torch.int32), n_pages, n_slots, max_pages, _contig(lengths, torch.int32),
@@ -1012,33 +1013,44 @@ def logits_rules(history=None, history_lens=None, history_rows=None, generated_f
     return r
 
 
+_LOGITS = {torch.float32: DET_F32, torch.bfloat16: DET_BF16}
+
+
 def det_logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
     """out [B, V] = logits with the rules (logits_rules) applied; fp32 or bf16, rows may have a stride; out may be logits."""
-    shape = B, V = logits.shape
+    shape = logits.shape
+    B, V = shape
     dtype = logits.dtype
-    if out.shape != shape or out.dtype != dtype or logits.stride(1) != 1 or out.stride(1) != 1 or rules._rows not in (None, B):
+    (ld_in, each), (ld_out, other) = logits.stride(), out.stride()
+    if out.shape != shape or out.dtype != dtype or each != 1 or other != 1 or rules._rows not in (None, B):
         raise ValueError("bad logits or rules of other rows")
+    if B == 1:  # the stride of a single row says nothing
+        ld_in, ld_out = max(ld_in, V), max(ld_out, V)
     _check("det_logits_process", lib().det_logits_process(
-        _ptr(logits), _ld(logits, V), _ptr(out), _ld(out, V), {torch.float32: DET_F32, torch.bfloat16: DET_BF16}[dtype], B, V, C.byref(rules),
-        _stream(stream)))
+        _ptr(logits), ld_in, _ptr(out), ld_out, _LOGITS[dtype], B, V, C.byref(rules), _stream(stream)))
 
 
 def det_logits_advance(tokens, history, lens_in, lens_out, transitions=None, token_class=None, states_in=None, states_out=None, stream=None) -> None:
     """tokens [B] go into history [B, most] at lens_in (lens_out: one more), and states_out = transitions[states_in, class of the token] ([n_states,
     n_classes]; token_class [V], None: a token is its class).  history None or transitions None leaves a part out."""
-    B, = tokens.shape
+    of_rows = tokens.shape
+    B, = of_rows
     i32 = torch.int32
     most = V = n_states = n_classes = 0
+    had = n_in = n_out = to = classes = s_in = s_out = None
     if history is not None:
         rows, most = history.shape
-        if rows != B or lens_in.shape != (B,) or lens_out.shape != (B,):
+        if rows != B or lens_in.shape != of_rows or lens_out.shape != of_rows:
             raise ValueError("bad history")
+        had, n_in, n_out = _contig(history, i32), _contig(lens_in, i32), _contig(lens_out, i32)
     if transitions is not None:
         n_states, n_classes = transitions.shape
-        V = n_classes if token_class is None else token_class.shape[0]
-        if states_in.shape != (B,) or states_out.shape != (B,) or (token_class is not None and token_class.dim() != 1):
+        V = n_classes
+        if token_class is not None:
+            V, = token_class.shape
+            classes = _contig(token_class, i32)
+        if states_in.shape != of_rows or states_out.shape != of_rows:
             raise ValueError("bad states")
-    opt = lambda t: None if t is None else _contig(t, i32)
+        to, s_in, s_out = _contig(transitions, i32), _contig(states_in, i32), _contig(states_out, i32)
     _check("det_logits_advance", lib().det_logits_advance(
-        _contig(tokens, i32), opt(history), most, opt(lens_in), opt(lens_out), opt(transitions), n_states, n_classes, opt(token_class), V,
-        opt(states_in), opt(states_out), B, _stream(stream)))
+        _contig(tokens, i32), had, most, n_in, n_out, to, n_states, n_classes, classes, V, s_in, s_out, B, _stream(stream)))
