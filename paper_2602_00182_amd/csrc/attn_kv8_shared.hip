@@ -934,7 +934,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         const long long room = wgs / (rows * cache.Hkv);
         return room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
     };
-    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_RUN_WGS : DET_KV8_CHUNK_WGS);
+    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_RUN_WGS / 2 : DET_KV8_CHUNK_WGS);
     bool ring = false;
     if (step.n_groups > 0) {
         auto of_head = [&](long long most, long long wgs) {  // workgroups of a KV head

@@ -85,7 +85,7 @@ def test_layer_steps_that_are_refused(d, models):  # noqa: F811
 
 
 @pytest.mark.parametrize("quantized", [False, True])
-def test_continuations_of_long_prompts(dec, models, quantized):  # noqa: F811
+def test_continuations_of_long_prompts(dec, models, quantized, monkeypatch):  # noqa: F811
     """What shares whole chunks goes through the shared kernels; tokens and logits as from prompts that stand there several times."""
     m = models(quantized)
     lens = np.array([530, 256, 700, 40], dtype=np.int32)
@@ -93,6 +93,7 @@ def test_continuations_of_long_prompts(dec, models, quantized):  # noqa: F811
     cos, sin = tables(760)
     policy = dec.SamplingPolicy(1.0, 50, 0.95, 77, torch.arange(20, dtype=torch.int32, device=DEV))
     step("five continuations of four prompts")
+    monkeypatch.setattr(dec, "GROUPS_FROM", 1)
     shared, logits = dec.prefill_decode(m, prompts, up(lens), 50, cos, sin, policy=policy, keep_logits=True, samples=5)
     apart, want = dec.prefill_decode(m, prompts.repeat_interleave(5, 0), up(np.repeat(lens, 5)), 50, cos, sin, policy=policy, keep_logits=True)
     assert torch.equal(shared, apart) and all(torch.equal(a, b) for a, b in zip(logits, want))
@@ -162,12 +163,13 @@ def test_rules_with_a_bf16_cache_and_sampling(dec, models):  # noqa: F811
 
 
 @pytest.mark.parametrize("samples", [1, 3])
-def test_sequences_that_give_up_pages(dec, models, samples):  # noqa: F811
+def test_sequences_that_give_up_pages(dec, models, samples, monkeypatch):  # noqa: F811
     """They come back to their budgets, alone as in a batch; with room for all pages nothing changes."""
     m = models()
     lens = np.array([600, 90, 330], dtype=np.int32)
     prompts, (cos, sin) = up(ds.uniform_int(9000, (3, 600), 0, CFG["V"] - 1)), tables(700)
     run = lambda p, n, s=samples, **more: dec.prefill_decode(m, p, up(n), 60, cos, sin, keep_logits=True, samples=s, **more)  # noqa: E731
+    monkeypatch.setattr(dec, "GROUPS_FROM", 1)
     step("evict nothing")
     want, logits = run(prompts, lens)
     got, same = run(prompts, lens, evict=dec.EvictPolicy(keep=11, every=8))
