@@ -4,8 +4,13 @@
 // what a row has behind them is read for itself.  A chunk's sums are the same numbers whoever computes them, and chunks are folded in ascending order in a
 // launch of their own, so the bytes are those of det_attn_decode_kv8.
 //
-// The weight of a page: what the chunk's softmax sums to over its 64 tokens is kept beside the chunk's sums, and a last launch adds it up over the heads
-// once the row's largest score and sum are known.
+// With s a token's score in powers of two, m_c = ceil of a chunk's largest and e = 2^(s - m_c), a chunk leaves m_c, l_c = sum e and o_c = sum e v.  The row's
+// output is sum 2^(m_c - m) o_c / l with m = max m_c and l = sum 2^(m_c - m) l_c.  The weight of a page is what e sums to over its 64 tokens, kept beside the
+// chunk's sums, times 2^(m_c - m) / l, added up over heads and rows in the second launch.
+//
+// What bounds it: the partial sums of every (row, head, chunk), which the order of folding asks for (528 bytes, written and read), and, from some rows a
+// group on, the digits' products: 96 multiplications of 16 x 16 x 64 codes and what prepares them a (tile, page).  64 rows of 32 heads that share 32000
+// tokens: 106 + 25 us, of which 186 MB of partial sums; each row for itself 1100 MB of cache.
 #include <type_traits>
 
 #include "attn_kv8.h"
@@ -24,7 +29,8 @@ struct kv8_shared_args : kv8_attn_args {
     int group_wgs, group_steps; // workgroups of a KV head that take shared chunks (at most 2^15 of runs); of them to a tile
     int part_rows;              // rows of a tile, or of the four that go together
     uint32_t part_inverse;
-    int row_steps;              // workgroups of a KV head to a row
+    int row_steps;              // workgroups of a KV head to a row; or 0: what all rows read for themselves is cut into equal runs,
+    int row_wgs;                // for so many; or 0: some of group_wgs take them
 };
 
 // ---------------------------------------------------------------- groups
@@ -39,7 +45,7 @@ __device__ __forceinline__ kv8_group group_at(const kv8_shared_args& a, int g)
     const bool is = g < a.n_groups;
     const int begin = a.group_rows[is ? g : 0], end = a.group_rows[is ? g + 1 : 0], shared = a.shared[is ? g : 0];
     kv8_group o;
-    o.first = o.row0 = min(max(begin, 0), a.R);
+    o.first = o.row0 = is ? min(max(begin, 0), a.R) : a.R;
     o.rows = is ? min(end, a.R) - o.row0 : 0;
     o.chunks = o.rows >= 2 ? min(max(shared, 0) / kChunk, a.chunks) : 0;
     return o;
@@ -63,18 +69,36 @@ __device__ __forceinline__ int chunks_before(const kv8_shared_args& a, kv8_group
     return 0;
 }
 
+// The same for this lane's row: the last group that begins at or in front of it, among 64 lanes in ascending order, by halves.
+__device__ __forceinline__ int chunks_before_lane(const kv8_shared_args& a, kv8_group mine, int row)
+{
+    int chunks = 0;
+    for (int base = 0; base < a.n_groups; base += kWave) {
+        if (base > 0) mine = group_at(a, base + (threadIdx.x & 63));
+        int g = 0;
+#pragma unroll
+        for (int step = kWave / 2; step > 0; step >>= 1) g += __shfl(mine.first, g + step, kWave) <= row ? step : 0;
+        const int first = __shfl(mine.first, g, kWave), rows = __shfl(mine.rows, g, kWave), its = __shfl(mine.chunks, g, kWave);
+        chunks = row >= first && row < first + rows ? its : chunks;
+    }
+    return chunks;
+}
+
 // How much of something (a count of each group) lies in front of and in this lane's group.
-template <class Count>
-__device__ __forceinline__ int count_up(const kv8_group& mine, Count count)
+__device__ __forceinline__ int sum_up(int sum)
 {
     const int lane = threadIdx.x & 63;
-    int sum = count(mine);
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
         const int x = __shfl_up(sum, off, kWave);
         sum += lane >= off ? x : 0;
     }
     return sum;
+}
+template <class Count>
+__device__ __forceinline__ int count_up(const kv8_group& mine, Count count)
+{
+    return sum_up(count(mine));
 }
 // How much of it there is in all; sum: count_up of the first 64 groups.
 template <class Count>
@@ -128,8 +152,8 @@ __device__ __forceinline__ void take_part(kv8_group& g, int nth, int rows)
 // ---------------------------------------------------------------- chunks of a tile
 
 // Every step-th chunk from first_chunk on, below end_chunk, for `rows` rows from row0 on, all of which read the pages of slot `now`: of a group, or (rows =
-// 1) a row of length row_len.  As
-// kv8_attn_chunk_kernel takes one (attn_kv8.hip): a page a wave for the scores, 32 columns a wave for the weighted sums.
+// 1) a row of length row_len.  As kv8_attn_chunk_kernel takes one (attn_kv8.hip): a page a wave for the scores, 32 columns a wave for the weighted sums.
+// Calls may follow one another: what the last one read behind its last barrier is not written in front of the first.
 template <bool PACK>
 struct tile_lds {
     static constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
@@ -348,17 +372,23 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
 
 // ---------------------------------------------------------------- chunks of four tiles
 
-// A wave has a tile, and the four go through a run of chunks together: a chunk's eight pages of codes, of K and then of V, 8 KB each, come by LDS-DMA
-// through a ring of six slots, five in flight, one barrier a page.  A chunk's sums go to memory, so nothing is kept from chunk to chunk and any run of
-// chunks can be a workgroup's.  All 128 columns are summed at once (96 sums a lane), page by page: a page's digits are cut while the page in front of it is
-// multiplied, and two pages' of them are all that LDS holds.
+// A wave has a tile, and the four go through a run of chunks together: the codes come by LDS-DMA, two pages of K or of V a step, 16 KB, through a ring of
+// three slots, two steps in flight, one barrier a step.  A chunk's sums go to memory, so nothing is kept from chunk to chunk and any run of chunks can be a
+// workgroup's.  All 128 columns are summed at once (96 sums a lane), page by page: a page's digits are cut while the page in front of it is multiplied, and
+// two pages' of them are all that LDS holds.
 //
 // K rows and their scales lie in LDS as in kv8_attn_walk_kernel (attn_kv8.hip).  V: column 64 h + 4 c + i of sixteen tokens at [h][i][c], so that a lane
 // ends with four neighbouring columns of a pair, twice.  Digits: the 64 bytes of pair p at row 4 (p % 4) + p / 4, their sixteen-byte pieces swizzled by
 // p % 4: neither writes nor reads meet in a bank.
 //
-// A chunk's results are stored during the next one's K pages, in front of a page's loads: a wait, which counts the loads behind the page it waits for, then
+// A chunk's results are stored in the next one's first step, in front of that step's loads: a wait, which counts the loads behind the step it waits for, then
 // waits for no load that was asked for later.
+//
+// A chunk of four tiles takes a workgroup 10 us, two of them on a unit: 1274 vector instructions and 192 products a wave, which hardly run beside each other
+// (a product of 16 cycles holds its SIMD's issue for about ten), 8 us without loads and stores.  Registers: 252, and a spill would wait for every load in
+// flight; the pairs' factors, lengths and places lie in LDS therefore, and heads of 8 and more a KV head, whose rows read chunks of their own with 16 pairs,
+// spill a few only outside the loop.
+// Against kTiles: 64 rows that share 32000 tokens 123 us against 245, 16 that share 2900 15.8 against 20, but 4 that share 1000, 4 KV heads, 14.2 against 12.0.
 constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = 2 * kRecordV;  // slots, steps in flight, bytes of a slot
 constexpr int kSteps = kChunkPages;                                          // of a chunk: two pages each, K codes and then V codes
 constexpr int kPageDigits = 3 * kPairs * kPage;                          // bytes
@@ -652,9 +682,54 @@ __device__ __forceinline__ void chunks_of_tiles(const kv8_shared_args& a, uint8_
 
 // ---------------------------------------------------------------- the launches
 
-// Grid: workgroups of shared chunks, then row_steps of every row; neighbours take the KV heads of one page, whose records lie side by side.
-// kRuns: four tiles go through a run of chunks together.  All chunks of all groups, one behind the other, are cut into group_wgs equal runs.
+__device__ __forceinline__ void no_tokens(const kv8_shared_args& a, int kvh, int row)
+{
+    for (int i = threadIdx.x; i < a.G * kHeadDim / 2; i += kBlock) reinterpret_cast<uint32_t*>(a.out + ((size_t)row * a.Hq + kvh * a.G) * kHeadDim)[i] = 0u;
+}
+
+// What this lane's row reads for itself: `count` chunks from `first` on (of a row without tokens one, in which its zeros are written).
+struct kv8_own {
+    int len, slot, first, count;
+};
+__device__ __forceinline__ kv8_own own_chunks(const kv8_shared_args& a, const kv8_group& mine, int row)
+{
+    kv8_own o{0, -1, 0, 0};
+    if (row < a.R) o.len = row_length(a, row, o.slot);  // asked for in front of the search
+    o.first = chunks_before_lane(a, mine, row);
+    o.first = o.len > kChunk ? o.first : 0;
+    o.count = row < a.R ? max((max(o.len, 1) + kChunk - 1) / kChunk - o.first, 0) : 0;
+    return o;
+}
+
+// The nth of `parts` runs, equal but for one, of `all`.
+__device__ __forceinline__ void run_of(int all, int nth, int parts, int& at, int& to)
+{
+    const int each = all / parts, rest = all - each * parts;
+    at = each * nth + rest * nth / parts;
+    to = each * (nth + 1) + rest * (nth + 1) / parts;
+}
+
+// Of all rows.
+__device__ __forceinline__ int count_own(const kv8_shared_args& a, const kv8_group& mine)
+{
+    int all = 0;
+    for (int base = 0; base < a.R; base += kWave) all += __builtin_amdgcn_readlane(sum_up(own_chunks(a, mine, base + (threadIdx.x & 63)).count), kWave - 1);
+    return all;
+}
+
+// How many of `wgs` workgroups take the shared chunks, which count twice, if `own` others are left to the rest (one of them at least): as many as their
+// share, or fewer if the longest run stays as long.
+__device__ __forceinline__ int wgs_of_groups(int shared, int own, int wgs)
+{
+    const long long twice = 2ll * shared;
+    const int share = min(max((int)(twice * wgs / max(twice + own, 1ll)), 1), wgs - 1), longest = (shared + share - 1) / share;
+    return longest > 0 ? (shared + longest - 1) / longest : 0;
+}
+
+// Grid: workgroups of shared chunks, then those of what rows read for themselves; neighbours take the KV heads of one page, whose records lie side by side.
+// kRuns: four tiles go through a run of chunks together.  All chunks of all groups, one behind the other, are cut into equal runs.
 // kTiles: a workgroup takes every group_steps-th chunk of a tile.  PACK: a row's up to four heads a KV head.
+// A unit holds two workgroups of kRuns at a time (LDS, registers), empty ones among them: their number is kept near 512.
 enum { kNoGroups, kTiles, kRuns };
 template <int FORM, bool PACK, bool WEIGHTS>
 __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_shared_kernel(kv8_shared_args a)
@@ -664,35 +739,62 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     const int kvh = blockIdx.x % a.c.Hkv;
     int nth = blockIdx.x / a.c.Hkv;
     kv8_group mine{};
-    if constexpr (FORM != kNoGroups) {
-        mine = group_at(a, threadIdx.x & 63);
-        if (nth < a.group_wgs) {
-            const parts_of_groups parts{a.part_rows, a.part_inverse, FORM == kRuns};
-            const int sum = count_up(mine, parts);
-            if constexpr (FORM == kRuns) {
-                // the shared chunks of all sets of tiles (below 2^30) in group_wgs runs
-                const int all = count_groups(a, sum, parts), each = all / a.group_wgs, rest = all - each * a.group_wgs;
-                int at = each * nth + rest * nth / a.group_wgs;
-                const int to = each * (nth + 1) + rest * (nth + 1) / a.group_wgs;
+    if constexpr (FORM != kNoGroups) mine = group_at(a, threadIdx.x & 63);
+    if constexpr (FORM == kRuns) {
+        const parts_of_groups parts{a.part_rows, a.part_inverse, true};
+        int group_wgs = a.group_wgs, row_wgs = a.row_wgs, at, to;
+        if (nth < group_wgs) {
+            // the shared chunks of all sets of tiles (below 2^30) in group_wgs runs
+            const int sum = count_up(mine, parts), shared = count_groups(a, sum, parts);
+            if (a.row_steps == 0 && row_wgs == 0) {
+                group_wgs = wgs_of_groups(shared, count_own(a, mine), a.group_wgs);
+                row_wgs = a.group_wgs - group_wgs;
+            }
+            if (nth < group_wgs) {
+                run_of(shared, nth, group_wgs, at, to);
                 while (at < to) {
                     int in;
                     kv8_group set = find_group(a, mine, sum, at, in, parts);
-                    if (set.chunks == 0) return;
+                    if (set.chunks == 0 || in < 0) return;
                     const int nth_set = in / set.chunks, c0 = in - nth_set * set.chunks, c1 = min(set.chunks, c0 + to - at);
                     take_part(set, nth_set, a.part_rows);
                     chunks_of_tiles<WEIGHTS>(a, lds, kvh, set.row0, set.rows, a.slots ? a.slots[set.first] : set.first, c0, c1);
                     at += c1 - c0;
                 }
-            } else {
-                int in;
-                kv8_group tile = find_group(a, mine, sum, nth / a.group_steps, in, parts);
-                take_part(tile, in, a.part_rows);
-                const int first = nth % a.group_steps;
-                if (first >= tile.chunks) return;
-                // the pages are those of the group's first row
-                chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, 0, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks,
-                                                     a.group_steps);
+                return;
             }
+        }
+        nth -= group_wgs;
+        if (a.row_steps == 0) {
+            // what all rows read for themselves in row_wgs runs
+            run_of(count_own(a, mine), nth, row_wgs, at, to);
+            int before = 0;
+            for (int base = 0; base < a.R && at < to; base += kWave) {
+                const kv8_own own = own_chunks(a, mine, base + (threadIdx.x & 63));
+                const int sum = before + sum_up(own.count);
+                before = __builtin_amdgcn_readlane(sum, kWave - 1);
+                while (at < min(to, before)) {
+                    const int r = __builtin_ctzll(__ballot(sum > at)), len = __builtin_amdgcn_readlane(own.len, r), last = __builtin_amdgcn_readlane(sum, r);
+                    const int end = __builtin_amdgcn_readlane(own.first, r) + __builtin_amdgcn_readlane(own.count, r);
+                    if (len == 0) no_tokens(a, kvh, base + r);
+                    else chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, base + r, 1, len, __builtin_amdgcn_readlane(own.slot, r), end - (last - at), end - max(last - to, 0), 1);
+                    at = min(to, last);
+                }
+            }
+            return;
+        }
+    }
+    if constexpr (FORM == kTiles) {
+        if (nth < a.group_wgs) {
+            const parts_of_groups parts{a.part_rows, a.part_inverse, false};
+            int in;
+            kv8_group tile = find_group(a, mine, count_up(mine, parts), nth / a.group_steps, in, parts);
+            take_part(tile, in, a.part_rows);
+            const int first = nth % a.group_steps;
+            if (first >= tile.chunks) return;
+            // the pages are those of the group's first row
+            chunks_of_tile<false, WEIGHTS, true>(a, lds, kvh, tile.row0, tile.rows, 0, a.slots ? a.slots[tile.first] : tile.first, first, tile.chunks,
+                                                 a.group_steps);
             return;
         }
         nth -= a.group_wgs;
@@ -701,9 +803,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     int slot;
     const int len = row_length(a, row, slot);
     if (len == 0) {
-        if (first == 0)
-            for (int i = threadIdx.x; i < a.G * kHeadDim / 2; i += kBlock)
-                reinterpret_cast<uint32_t*>(a.out + ((size_t)row * a.Hq + kvh * a.G) * kHeadDim)[i] = 0u;
+        if (first == 0) no_tokens(a, kvh, row);
         return;
     }
     int behind = 0;
@@ -715,7 +815,8 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
 // empty chunks it ends with (a multiple of sixteen in all).  A wave has a head, a lane two columns.  The factors of 64 chunks come from one load, a chunk a
 // lane: the largest score so far is a maximum over the lanes in front (exact in any order), the factors follow from it, and are read from their lane
 // while the sums are folded.  That leaves ten instructions a chunk and takes the statistics out of the way between two trips to memory: worked out by every
-// lane, a column each, they were the launch (64 rows of 32 heads and 126 chunks 33 us, now XX; 8 rows of 16 heads and up to 79 chunks 10.6, now XX).
+// lane, a column each, they were the launch.  64 rows of 32 heads and 129 chunks 33 -> 25 us, 133 MB at 5.3 TB/s, which bounds it; 8 rows of 16 heads and up to
+// 79 chunks with the pages' weights beside them 10.6 -> 7.2.
 constexpr int kFoldChunks = 16, kCombineThreads = 128, kCombineHeads = kCombineThreads / kWave;
 __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t block)
 {
@@ -934,7 +1035,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         const long long room = wgs / (rows * cache.Hkv);
         return room < 1 ? 1 : (room < a.chunks ? (int)room : a.chunks);
     };
-    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_RUN_WGS / 2 : DET_KV8_CHUNK_WGS);
+    a.row_steps = steps(R, step.n_groups > 0 ? DET_KV8_OWN_WGS : DET_KV8_CHUNK_WGS);
     bool ring = false;
     if (step.n_groups > 0) {
         auto of_head = [&](long long most, long long wgs) {  // workgroups of a KV head
@@ -943,12 +1044,20 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         };
         ring = ((long long)R + a.rows_per_tile - 1) / a.rows_per_tile * a.chunks * cache.Hkv >= DET_KV8_RING_CHUNKS;
         if (ring) {
-            // Two workgroups a compute unit: all of them for runs of several chunks, else some are left to what rows read for themselves, beside them.  60 rows
-            // of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7; 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
-            const long long sets = ((long long)R + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile), most = (sets > step.n_groups ? sets : step.n_groups) * a.chunks,
-                            rest = DET_KV8_RUN_WGS - (long long)R * cache.Hkv;
-            const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS;
-            a.group_wgs = of_head(most, several ? DET_KV8_RUN_WGS : rest > DET_KV8_RUN_WGS / 2 ? rest : DET_KV8_RUN_WGS / 2);
+            const long long sets = ((long long)R + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile), most = (sets > step.n_groups ? sets : step.n_groups) * a.chunks;
+            // Two workgroups a compute unit.  All of them for runs of several chunks, with those of the rows' own chunks behind them; where the shared chunks
+            // need not fill them, they are split between both.  60 rows of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7;
+            // 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
+            // What rows read for themselves: where (row, KV head) alone would leave units idle, in equal runs; else a workgroup each, which the dispatcher
+            // levels.  Against two to eight workgroups a row: 16 rows of up to 16000 tokens behind 512 shared ones 120 -> 72 us, 4 of up to 30000 60 -> 43, 16 of 4
+            // prompts of 1000 with up to 8000 77 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.3, 8 of 20000 with up to 100 21.9 -> 23.1: the counting.  Equal runs
+            // for more rows lose: 64 of 4 prompts of 2000, 4 KV heads, 17.6 -> 20.2, 32 of 8 prompts of 4000 28.6 -> 31.5.
+            const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS, few = (long long)R * cache.Hkv < DET_KV8_RUN_WGS / 2;
+            if (few) {
+                a.row_steps = 0;
+                a.row_wgs = several ? of_head((long long)R * a.chunks, DET_KV8_OWN_WGS) : 0;
+            }
+            a.group_wgs = several ? of_head(most, DET_KV8_RUN_WGS) : few ? of_head(most + (long long)R * a.chunks, DET_KV8_RUN_WGS) : of_head(most, DET_KV8_RUN_WGS / 2);
         } else {
             // a group of n rows has at most n / rows_per_tile + 1 tiles, and at most n
             const long long tiles = R / a.rows_per_tile + step.n_groups < R ? R / a.rows_per_tile + step.n_groups : R;
@@ -959,7 +1068,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
     }
     a.part_rows = (ring ? 4 : 1) * a.rows_per_tile;
     a.part_inverse = a.part_rows > 1 ? (uint32_t)((1ull << 32) / a.part_rows + ((1ull << 32) % a.part_rows != 0)) : 0u;
-    const long long grid = (a.group_wgs + (long long)R * a.row_steps) * cache.Hkv, blocks = weights ? (a.chunks + kWeightChunks - 1) / kWeightChunks : 0,
+    const long long grid = (a.group_wgs + (a.row_steps > 0 ? (long long)R * a.row_steps : a.row_wgs)) * cache.Hkv, blocks = weights ? (a.chunks + kWeightChunks - 1) / kWeightChunks : 0,
                     second = blocks * cache.n_slots + ((long long)R * Hq + kCombineHeads - 1) / kCombineHeads;
     if (grid > 0x7FFFFFFFll / 256 || second > 0x7FFFFFFFll / kCombineThreads) return DET_ESHAPE;
     auto launch = [&](auto form) {
