@@ -202,6 +202,28 @@ def test_groups_of_many_rows(d, what, common, lengths, Hq, Hkv):
     assert same_bytes(out, want) and torch.equal(weights, others[perm])
 
 
+# rows' own chunks, cut into runs: of one group, of more rows and groups than a wave has lanes, rows without tokens, and groups that fill the chip
+BEHIND = [
+    ("one group", [512], [[600 + 397 * i for i in range(15)] + [0, 512]]),
+    ("no group shares anything", [0, 192], [[900 + 90 * i for i in range(12)], [200, 2000, 192, 3000]]),
+    ("many groups", [256 * (g % 4) for g in range(100)], [[256 * (g % 4) + 1 + 31 * g % 1500, 256 * (g % 4) + 2 * g] for g in range(100)]),
+    ("long and short behind groups of every size", [256 * (g % 3) for g in range(70)], [[1000 + 40 * g, 530 + g, 777][:1 + g % 3] for g in range(70)]),
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (8, 1), (6, 2)])
+@pytest.mark.parametrize("what,common,lengths", BEHIND, ids=[s[0] for s in BEHIND])
+def test_rows_with_much_behind_what_they_share(d, what, common, lengths, Hq, Hkv):
+    c = SharedCache(800 + Hq, Hkv, common, lengths)
+    _, q, pool, table, lens = fill(c, 801 + Hq, Hq)
+    step(f"{what}, {Hq}/{Hkv} heads")
+    want = plain(d, q, pool, table, lens)
+    assert same_bytes(grouped(d, q, pool, table, lens, up(c.group_rows), up(c.shared)), want)
+    out, weights = weighed(d, q, pool, table, lens, None, up(c.group_rows), up(c.shared))
+    _, others = weighed(d, q, pool, table, lens, None)
+    assert same_bytes(out, want) and torch.equal(weights, others)
+
+
 def test_missing_pages_and_slots_that_are_none(d):
     """Pages given up weigh nothing, whole chunks of them too; rows without any page, slot or token give zeros and add nothing."""
     c = SharedCache(800, 2, [1024], [[1100, 1200, 1300, 1024]])
