@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2602_00182_amd as d
-from paper_2602_00182_amd._lib import LogitsRules
+from paper_2602_00182_amd._lib import Kv8Step, LayerWeights, LogitsRules
 
 EINVAL, ESHAPE, EALIGN, EWORKSPACE = 1, 2, 3, 4
 P = 4096  # a 16-byte aligned address that is never read: every call below ends before a launch
@@ -47,6 +47,32 @@ CASES += [("det_logits_advance", ADVANCE, change, code) for change, code in [
 def test_a_call_that_is_refused_says_why(name, args, change, code):
     call = {**args, **change}
     assert getattr(lib(), name)(*[None if isinstance(v, int) and v == 0 and k in POINTERS else v for k, v in call.items()]) == code
+
+
+LAYER = dict(x=P, pool=P, table=P, n_pages=4, n_slots=4, max_pages=2, positions=P, slots=None, cos=P, sin=P, step={}, ws=P, ws_bytes=1 << 40, R=2)
+
+
+@pytest.mark.parametrize("name", ["det_decoder_layer_kv8_step", "det_qdecoder_layer_kv8_step"])
+@pytest.mark.parametrize("change,code", [
+    (dict(step=dict(group_rows=0)), EINVAL), (dict(step=dict(shared=0)), EINVAL), (dict(step=dict(n_groups=-1)), EINVAL), (dict(step=dict(n_groups=3)), ESHAPE),
+    (dict(R=65536, slots=P), ESHAPE), (dict(step=dict(weights=P), n_slots=65536), ESHAPE), (dict(step=dict(n_groups=0, weights=P), R=65536, slots=P), ESHAPE),
+    (dict(ws_bytes="size - 1"), EWORKSPACE), (dict(step=dict(weights=P), max_pages=200, ws_bytes="size"), EWORKSPACE), (dict(R=5), ESHAPE), (dict(x=None), EINVAL),
+    (dict(pool=P + 8), EALIGN), (dict(ws=P + 8), EALIGN)])
+def test_a_layers_step_that_is_refused_says_why(name, change, code):
+    a = {**LAYER, **change}
+    cfg, w = d.layer_cfg(512, 4, 2, 128, 1024, 256, 1e-5, 0.1), LayerWeights(*[P] * 6)
+    step = Kv8Step(**{**dict(group_rows=P, shared=P, n_groups=1), **a["step"]})
+    size = getattr(d, name + "_workspace_bytes")(cfg, a["R"], a["max_pages"], False)
+    n_bytes = {"size - 1": size - 1, "size": size}.get(a["ws_bytes"], a["ws_bytes"])
+    call = [a[k] for k in ("x", "pool", "table", "n_pages", "n_slots", "max_pages", "positions", "slots", "cos", "sin")]
+    assert getattr(lib(), name)(ctypes.byref(w), ctypes.byref(cfg), *call, ctypes.byref(step), a["ws"], n_bytes, a["R"], None) == code
+
+
+def test_a_layers_workspace():
+    cfg = d.layer_cfg(512, 4, 2, 128, 1024, 256, 1e-5, 0.1)
+    for name in ("det_decoder_layer_kv8", "det_qdecoder_layer_kv8"):
+        size = lambda weights, R=3, pages=9: getattr(d, name + "_step_workspace_bytes")(cfg, R, pages, weights)  # noqa: E731, B023
+        assert getattr(d, name + "_workspace_bytes")(cfg, 3, 9) == size(False) < size(True) and size(False, 0) == size(True, 3, 0) == size(True, 3, 131073) == 0
 
 
 FULL = dict(penalties=P, history=P, history_lens=P, bias_begin=P, bias_tokens=P, bias_values=P, masks=P, mask_rows=P, ld_history=10, n_history=2, n_biases=3,
