@@ -275,7 +275,8 @@ int det_sample(const float *logits, int B, int V, float temperature, int top_k, 
  *   bias_begin [B + 1]: row b's entries are bias_begin[b] .. bias_begin[b+1]-1 of bias_tokens, bias_values [n_biases].
  *   masks [n_masks, mask_words]: bit t % 32 of word t / 32; mask_rows [B]: the row's mask (NULL: b; outside 0..n_masks-1: none).
  * logits, out [B, V] fp32 (DET_F32) or bf16 (DET_BF16: computed in fp32, rounded once) with row strides ld >= V in elements; out may be logits (with
- * its stride), else the two may not overlap.  16-byte aligned (rows need not be).  B <= 65535, V <= 2^30, 32 mask_words >= V. */
+ * its stride), else the two may not overlap.  16-byte aligned (rows need not be).  B <= 65535, V <= 2^30, 32 mask_words >= V;  ld_history and n_biases
+ * at most 2^30. */
 typedef struct det_logits_rules {
     const float *penalties;
     const int32_t *history;
@@ -566,7 +567,8 @@ int det_attn_decode_kv8_shared(const void *q, const void *pool, const int32_t *p
 
 /* The same, and what weight each page of each slot got:
  *   weights_out[s][i] = weights_in[s][i] + sum over the rows r that name slot s, the heads h and the tokens j of page i (64 i .. 64 i + 63) of p[r][h][j],
- * p the softmax of row r and head h.  fp32, in a fixed order: of each row (ascending) the heads (ascending) into the sum h mod 8, these eight in order, then onto weights_in.  A row whose softmax is not finite adds nothing.  Output bytes as above.
+ * p the softmax of row r and head h.  fp32, in a fixed order: of each row (ascending) the heads (ascending) into the sum h mod 8, these eight in order, then
+ * onto weights_in.  A (row, head) whose softmax is not finite adds nothing.  Output bytes as above.
  *   weights_in, weights_out [n_slots, max_pages] fp32, every entry written; weights_in NULL: zeros; the two may be the same array.  n_slots <= 65535.
  *   ws: det_attn_decode_kv8_weights_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_weights_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);

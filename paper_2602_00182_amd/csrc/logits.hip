@@ -229,7 +229,7 @@ extern "C" int det_logits_process(const void* logits, int64_t ld_logits, void* o
     if (r.penalties && (!r.history || !r.history_lens || r.ld_history < 1 || r.n_history < 1 || (!r.history_rows && r.n_history < B))) return DET_EINVAL;
     if (r.bias_begin && (r.n_biases < 0 || (r.n_biases > 0 && (!r.bias_tokens || !r.bias_values)))) return DET_EINVAL;
     if (r.masks && (r.n_masks < 1 || r.mask_words < 1)) return DET_EINVAL;
-    if (B > 65535 || V > (1 << 30) || (r.masks && (long long)r.mask_words * 32 < V)) return DET_ESHAPE;
+    if (B > 65535 || V > (1 << 30) || (r.penalties && r.ld_history > (1 << 30)) || (r.bias_begin && r.n_biases > (1 << 30)) || (r.masks && (long long)r.mask_words * 32 < V)) return DET_ESHAPE;
     const int size = dtype == DET_F32 ? 4 : 2;
     if (!aligned16(logits) || !aligned16(out)) return DET_EALIGN;
     // the same rows in place, or rows apart

@@ -104,7 +104,7 @@ class DecodeState:
     """KV caches, workspace and step buffers for B sequences of up to Lmax tokens.  With an 8-bit cache `pages` holds n_pages
     pages (None: room for all of them), reserved at once unless reserve is False; `groups` (the first sequence of each group, and B; None) says which
     sequences share pages that a step is to read once, and to `weights` ([B, pages of a sequence] fp32 or None) it adds what weight each page gets, over all
-    layers.  What a group shares is what the pages' tables say when the step is launched; a captured step keeps what they said then."""
+    layers.  What a group shares is what the pages' tables say when the step is launched, or, of a captured step, when `tell` is called."""
 
     def __init__(self, model: DecodeModel, B: int, Lmax: int, rope_cos, rope_sin, reserve: bool = True, n_pages: int | None = None):
         c = model.cfg
@@ -125,7 +125,8 @@ class DecodeState:
                            for _ in range(c.n_layers)]
             self.vcache = [torch.zeros_like(k) for k in self.kcache]
         self.ws = torch.empty(model.layer_workspace_bytes(self.lcfg, B), dtype=torch.uint8, device=dev)
-        self.groups = self.weights = self._step = None
+        self.groups = self.weights = None
+        self._told, self._spaces = {}, {}  # group_rows, shared and the table's version of groups; workspaces without and with weights
         self._buffers(B)
 
     def _buffers(self, rows: int):
@@ -140,29 +141,39 @@ class DecodeState:
         self.positions = torch.empty(rows, dtype=torch.int32, device=dev)
         self.slots = None
 
-    def _told(self):
-        """What the layers are told of groups and weights: as the pages lie now."""
+    def tell(self, stream=None):
+        """What the layers are told of groups and weights, and their workspace: brought in line with the pages' tables.  A step does so by itself; a captured one
+        keeps the groups and the weights of its capture, needs a step or a call of this with them in front of it, and another call, outside the graph, when
+        the tables have changed."""
         if self.groups is None and self.weights is None:
-            return None
-        now = (tuple(self.groups or ()), self.weights, self.pages.version)
-        if self._step is None or self._step[0][0] != now[0] or self._step[0][1] is not now[1] or self._step[0][2] != now[2]:
-            rows = shared = None
-            if self.groups is not None:
-                g, dev = list(self.groups), self.tokens.device
-                if g[0] != 0 or g[-1] != self.B or any(a >= b for a, b in zip(g, g[1:])):
-                    raise ValueError("groups of sequences, one behind the other")
-                rows = torch.tensor(g, dtype=torch.int32).to(dev)
-                shared = torch.tensor([self.pages.shared_tokens(range(a, b)) for a, b in zip(g, g[1:])], dtype=torch.int32).to(dev)
-            self._step = (now, api.kv8_step(rows, shared, self.weights))
-            size = self.model.layer_workspace_bytes(self.lcfg, self.B, step=self._step[1])
-            if self.ws.nbytes < size:
-                self.ws = torch.empty(size, dtype=torch.uint8, device=self.tokens.device)
-        return self._step[1]
+            return None, self.ws
+        if not self.model.cache8 or (self.groups is not None and self.slots is not None):
+            raise ValueError("groups and weights are those of an 8-bit cache's sequences, a row each")
+        rows, dev, g = self.tokens.shape[0], self.tokens.device, tuple(self.groups or ())
+        if self.groups is not None and (len(g) < 2 or g[0] != 0 or g[-1] != rows or any(a >= b for a, b in zip(g, g[1:]))):
+            raise ValueError("groups of sequences, one behind the other")
+        weighs, told = self.weights is not None, self._told.get(g)
+        if weighs not in self._spaces or (g and (told is None or told[2] != self.pages.version)):
+            if dev.type == "cuda" and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("groups, weights and tables of a captured step are those of one before it")
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                if g:  # their addresses stay, for graphs
+                    shared = torch.tensor([self.pages.shared_tokens(range(a, b)) for a, b in zip(g, g[1:])], dtype=torch.int32)
+                    told = told or [torch.tensor(g, dtype=torch.int32).to(dev), torch.empty(len(g) - 1, dtype=torch.int32, device=dev), None]
+                    told[1].copy_(shared)
+                    told[2] = self.pages.version
+                    self._told[g] = told
+                if weighs not in self._spaces:
+                    size = self.model.layer_workspace_bytes(self.lcfg, rows, step=api.kv8_step(weights=self.weights))
+                    self._spaces[weighs] = torch.empty(size, dtype=torch.uint8, device=dev)
+        step = api.kv8_step(*(told[:2] if g else (None, None)), self.weights)
+        return step, self._spaces[weighs]
 
     def of_rows(self, slots: torch.Tensor) -> "DecodeState":
         """A state over the same caches whose steps take one row for each entry of slots (several rows may name one sequence)."""
         st = copy.copy(self)
-        st.groups = st.weights = st._step = None
+        st.groups = st.weights = None
+        st._told, st._spaces = {}, {}
         st.ws = torch.empty(self.model.layer_workspace_bytes(self.lcfg, slots.shape[0], named=True), dtype=torch.uint8, device=slots.device)
         st._buffers(slots.shape[0])
         st.slots = slots
@@ -171,11 +182,11 @@ class DecodeState:
     def forward(self, stream=None):
         """One decode step on self.tokens / self.positions; leaves fp32 logits in self.logits."""
         m, c = self.model, self.model.cfg
-        step = self._told()
+        step, ws = self.tell(stream)
         api.det_embed_gather(m.embed, self.tokens, self.x, stream)
         for i, (_, struct) in enumerate(m.layers):
             m.layer(struct, self.lcfg, self.x, self.kcache[i], self.vcache[i], self.positions, self.slots, self.rope_cos,
-                    self.rope_sin, self.ws, stream, step)
+                    self.rope_sin, ws, stream, step)
         self.head(stream)
 
     def head(self, stream=None):

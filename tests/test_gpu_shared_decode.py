@@ -199,3 +199,76 @@ def test_sequences_that_give_up_pages(dec, models, samples, monkeypatch):  # noq
         run(prompts, lens, evict=dec.EvictPolicy(keep=0))
     with pytest.raises(ValueError):
         dec.prefill_decode(dec.DecodeModel(dec.ModelCfg(**CFG), weights(8000, n_layers=2, **SIZES)), prompts, up(lens), 2, cos, sin, evict=policy)
+
+
+def test_a_captured_step_follows_the_tables(dec, models, monkeypatch):  # noqa: F811
+    """Groups, weights and workspace of a captured step stay where they are; after the tables have changed `tell` is enough."""
+    m = models()
+    B, T = 5, 700
+    cos, sin = tables(T)
+    st = m.new_state(B, T, cos, sin, reserve=False, n_pages=B * 11)
+    st.pages.reserve([0], [400], [0])
+    fill = ds.uniform_int(9300, (B, 399), 0, CFG["V"] - 1)
+    rows = st.of_rows(torch.zeros(399, dtype=torch.int32, device=DEV))
+    rows.tokens.copy_(up(fill[0]))
+    rows.positions.copy_(torch.arange(399, dtype=torch.int32, device=DEV))
+    step("a prompt")
+    rows.forward()
+    st.pages.fork(0, range(1, B), 399)
+    tokens, positions = torch.arange(B, dtype=torch.int32, device=DEV), torch.full((B,), 399, dtype=torch.int32, device=DEV)
+    st.pages.reserve(range(B), [T] * B, [399] * B)
+
+    def forward(groups, weights):
+        st.groups, st.weights = groups, weights
+        st.tokens.copy_(tokens)
+        st.positions.copy_(positions)
+        st.forward()
+        return st.logits.clone()
+
+    with pytest.raises(ValueError):
+        forward([0, 3], None)
+    with pytest.raises(ValueError):
+        forward([], None)
+    with monkeypatch.context() as to, pytest.raises(RuntimeError):
+        to.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+        st.groups = [0, B]
+        st.tell()
+    few = st.of_rows(torch.zeros(2, dtype=torch.int32, device=DEV))
+    few.groups = [0, 2]
+    with pytest.raises(ValueError):
+        few.tell()
+    step("eager")
+    want = forward(None, None)
+    weights = torch.zeros(st.pages.table.shape, device=DEV)
+    assert torch.equal(forward([0, B], weights), want)
+    once = weights.clone()
+    assert once.sum() > 0
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        st.forward()
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        st.forward()
+    for _ in range(3):
+        step("replay")
+        weights.zero_()
+        st.logits.zero_()
+        graph.replay()
+        assert torch.equal(st.logits, want) and torch.equal(weights, once)
+        assert torch.equal(forward(None, None), want)     # another workspace
+        st.groups, st.weights = [0, B], weights
+    # two sequences go on in pages of their own: what all share ends at the first page
+    old = st.pages.table.clone()
+    for s in (1, 3):
+        st.pages.release(s)
+    st.pages.reserve([1, 3], [T] * 2, [0] * 2)
+    for pool in st.kcache:
+        pool[st.pages.table[[1, 3], :7].flatten().long()] = pool[old[[1, 3], :7].flatten().long()]
+    st.tell()
+    step("replay with other tables")
+    weights.zero_()
+    graph.replay()
+    assert torch.equal(st.logits, want) and torch.equal(weights, once)
+    assert int(st._told[0, B][1][0]) == 0 and torch.equal(forward([0, B], weights), want)

@@ -83,7 +83,7 @@ FULL = dict(penalties=P, history=P, history_lens=P, bias_begin=P, bias_tokens=P,
     (dict(logits=0), {}, EINVAL), (dict(out=0), {}, EINVAL), (dict(rules=None), {}, EINVAL), (dict(B=0), {}, EINVAL), (dict(V=0), {}, EINVAL),
     (dict(ld_in=99), {}, EINVAL), (dict(ld_out=99), {}, EINVAL), (dict(dtype=2), {}, EINVAL), ({}, dict(history=0), EINVAL),
     ({}, dict(history_lens=0), EINVAL), ({}, dict(ld_history=0), EINVAL), ({}, dict(n_history=0), EINVAL), ({}, dict(n_history=1), EINVAL),
-    ({}, dict(bias_tokens=0), EINVAL), ({}, dict(bias_values=0), EINVAL), ({}, dict(n_biases=-1), EINVAL), ({}, dict(n_masks=0), EINVAL),
+    ({}, dict(ld_history=(1 << 30) + 1), ESHAPE), ({}, dict(n_biases=(1 << 30) + 1), ESHAPE), ({}, dict(bias_tokens=0), EINVAL), ({}, dict(bias_values=0), EINVAL), ({}, dict(n_biases=-1), EINVAL), ({}, dict(n_masks=0), EINVAL),
     ({}, dict(mask_words=0), EINVAL), ({}, dict(mask_words=3), ESHAPE), (dict(B=65536), dict(n_history=70000), ESHAPE),
     (dict(V=(1 << 30) + 1, ld_in=1 << 31, ld_out=1 << 31), dict(masks=0), ESHAPE), (dict(logits=P + 4), {}, EALIGN), (dict(out=P + 8), {}, EALIGN),
     (dict(out=P, ld_out=101), {}, EINVAL),      # in place with another stride
