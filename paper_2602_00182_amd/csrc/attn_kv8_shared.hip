@@ -76,8 +76,8 @@ __device__ __forceinline__ int chunks_before_lane(const kv8_shared_args& a, kv8_
     for (int base = 0; base < a.n_groups; base += kWave) {
         if (base > 0) mine = group_at(a, base + (threadIdx.x & 63));
         int g = 0;
-#pragma unroll
-        for (int step = kWave / 2; step > 0; step >>= 1) g += __shfl(mine.first, g + step, kWave) <= row ? step : 0;
+        const int last = min(a.n_groups - base, kWave) - 1;
+        for (int step = last > 0 ? 1 << (31 - __builtin_clz(last)) : 0; step > 0; step >>= 1) g += __shfl(mine.first, g + step, kWave) <= row ? step : 0;
         const int first = __shfl(mine.first, g, kWave), rows = __shfl(mine.rows, g, kWave), its = __shfl(mine.chunks, g, kWave);
         chunks = row >= first && row < first + rows ? its : chunks;
     }
@@ -87,12 +87,13 @@ __device__ __forceinline__ int chunks_before_lane(const kv8_shared_args& a, kv8_
 // How much of something (a count of each group) lies in front of and in this lane's group.
 __device__ __forceinline__ int sum_up(int sum)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int x = __shfl_up(sum, off, kWave);
-        sum += lane >= off ? x : 0;
-    }
+    // within rows of sixteen lanes, then the row in front's total, then that of the half
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x142, 0xA, 0xF, false);
+    sum += __builtin_amdgcn_update_dpp(0, sum, 0x143, 0xC, 0xF, false);
     return sum;
 }
 template <class Count>
@@ -386,8 +387,8 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
 //
 // A chunk of four tiles takes a workgroup 10 us, two of them on a unit: 1274 vector instructions and 192 products a wave, which hardly run beside each other
 // (a product of 16 cycles holds its SIMD's issue for about ten), 8 us without loads and stores.  Registers: 252, and a spill would wait for every load in
-// flight; the pairs' factors, lengths and places lie in LDS therefore, and heads of 8 and more a KV head, whose rows read chunks of their own with 16 pairs,
-// spill a few only outside the loop.
+// flight; the pairs' factors, lengths and places lie in LDS therefore, and what the pages' weights cost more with 5 and more heads a KV head is spilled outside
+// the loop only.
 // Against kTiles: 64 rows that share 32000 tokens 123 us against 245, 16 that share 2900 15.8 against 20, but 4 that share 1000, 4 KV heads, 14.2 against 12.0.
 constexpr int kRing = 3, kRingAhead = kRing - 1, kStepBytes = 2 * kRecordV;  // slots, steps in flight, bytes of a slot
 constexpr int kSteps = kChunkPages;                                          // of a chunk: two pages each, K codes and then V codes
@@ -1049,8 +1050,8 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
             // need not fill them, they are split between both.  60 rows of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7;
             // 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
             // What rows read for themselves: where (row, KV head) alone would leave units idle, in equal runs; else a workgroup each, which the dispatcher
-            // levels.  Against two to eight workgroups a row: 16 rows of up to 16000 tokens behind 512 shared ones 120 -> 72 us, 4 of up to 30000 60 -> 43, 16 of 4
-            // prompts of 1000 with up to 8000 77 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.3, 8 of 20000 with up to 100 21.9 -> 23.1: the counting.  Equal runs
+            // levels.  Against two to eight workgroups a row: 16 rows of up to 16000 tokens behind 512 shared ones 120 -> 70 us, 4 of up to 30000 60 -> 41, 16 of 4
+            // prompts of 1000 with up to 8000 78 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.3, 8 of 20000 with up to 100 21.9 -> 22.8: the counting.  Equal runs
             // for more rows lose: 64 of 4 prompts of 2000, 4 KV heads, 17.6 -> 20.2, 32 of 8 prompts of 4000 28.6 -> 31.5.
             const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS, few = (long long)R * cache.Hkv < DET_KV8_RUN_WGS / 2;
             if (few) {
