@@ -10,7 +10,7 @@
 //
 // What bounds it: the partial sums of every (row, head, chunk), which the order of folding asks for (528 bytes, written and read), and, from some rows a
 // group on, the digits' products: 96 multiplications of 16 x 16 x 64 codes and what prepares them a (tile, page).  64 rows of 32 heads that share 32000
-// tokens: 106 + 25 us, of which 186 MB of partial sums; each row for itself 1100 MB of cache.
+// tokens: 105 + 25 us; the partial sums are 138 MB each way, the cache 135 MB, and 4400 MB if each row were read for itself.
 #include <type_traits>
 
 #include "attn_kv8.h"
