@@ -155,6 +155,9 @@ __device__ __forceinline__ void take_part(kv8_group& g, int nth, int rows)
 // Every step-th chunk from first_chunk on, below end_chunk, for `rows` rows from row0 on, all of which read the pages of slot `now`: of a group, or (rows =
 // 1) a row of length row_len.  As kv8_attn_chunk_kernel takes one (attn_kv8.hip): a page a wave for the scores, 32 columns a wave for the weighted sums.
 // Calls may follow one another: what the last one read behind its last barrier is not written in front of the first.
+// AHEAD: the next chunk's K codes are asked for once the scores are there, its V codes behind the products.  What rows read for themselves beside kRuns, whose
+// registers have room: 64 rows of up to 8000 tokens of their own 176 -> 171 us, 16 prompts of 4 rows with up to 4000 103 -> 98; elsewhere a third workgroup a
+// unit gives as much.
 template <bool PACK>
 struct tile_lds {
     static constexpr int PAIRS = PACK ? 4 : kPairs, DIGITS = PACK ? 1 : 3;
@@ -163,7 +166,7 @@ struct tile_lds {
     float lsum[4][PAIRS][16];
 };
 
-template <bool PACK, bool WEIGHTS, bool GROUP>
+template <bool PACK, bool WEIGHTS, bool GROUP, bool AHEAD = false>
 __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t* lds, int kvh, int row0, int rows, int row_len, int now,
                                                int first_chunk, int end_chunk, int step)
 {
@@ -215,37 +218,50 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
     int lens[NP];
 #pragma unroll
     for (int r = 0; r < NP; ++r) lens[r] = __shfl(len, PACK ? group : 4 * group + r, kWave);
-    bool first = true;
-    for (int chunk = first_chunk; chunk < end_chunk; chunk += step) {
-        // the chunk's pages; where one is missing, any record (its tokens weigh nothing)
-        const uint8_t *rec[kChunkPages], *keys = nullptr;
+    const uint8_t *rec[kChunkPages], *keys = nullptr;
+    v4i kc[4][2], vc[kChunkPages][2];
+    float dk[4], dv_asked[4] = {};
+    // the chunk's pages; where one is missing, any record (its tokens weigh nothing)
+    auto look_up = [&](int chunk) {
+        keys = nullptr;
 #pragma unroll
         for (int p = 0; p < kChunkPages; ++p) {
             const int page = chunk * kChunkPages + p;
-            const uint8_t* at = page * kPage < longest ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
+            const uint8_t* at = page * kPage < longest && (!AHEAD || chunk < end_chunk) ? kv8_record_uniform(a.c, now, page, kvh) : nullptr;
             keys = p == wave ? at : keys;
             rec[p] = at ? at : a.c.pool;
         }
-        if (!first) __syncthreads();  // the last chunk's digits have been read
-
-        v4i kc[4][2], vc[kChunkPages][2];
-        float dk[4], dv[4] = {};
-        if (keys) {
-            ask_scales(keys + kRecordKs, col, dk, dv);
+    };
+    auto ask_keys = [&] {
+        if (!keys) return;
+        ask_scales(keys + kRecordKs, col, dk, dv_asked);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) kc[t][h] = load16(keys, key_at, t * kHeadDim + 64 * h);
-        }
+            for (int h = 0; h < 2; ++h) kc[t][h] = load16(keys, key_at, t * kHeadDim + 64 * h);
+    };
+    auto ask_values = [&] {
 #pragma unroll
         for (int p = 0; p < kChunkPages; ++p)
 #pragma unroll
             for (int n = 0; n < 2; ++n) vc[p][n] = load16(rec[p], value_at, 256 * n);
+    };
+    bool first = true;
+    for (int chunk = first_chunk; chunk < end_chunk; chunk += step) {
+        if (!AHEAD || first) look_up(chunk);
+        if (!first) __syncthreads();  // the last chunk's digits have been read
+        if (!AHEAD || first) {
+            ask_keys();
+            ask_values();
+        }
         __builtin_amdgcn_sched_barrier(0);
         if (PACK && first) cut();  // while they are on their way
         first = false;
+        float dv[4];
         float s[4][NP];
         if (keys) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) dv[t] = dv_asked[t];
             clean_scales(dk, dv);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -269,6 +285,14 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < NP; ++r) s[t][r] = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) dv[t] = 0.0f;
+        }
+        if constexpr (AHEAD) {
+            __builtin_amdgcn_sched_barrier(0);
+            look_up(chunk + step);
+            ask_keys();
+            __builtin_amdgcn_sched_barrier(0);
         }
         // the chunk's largest score, then its largest weight, over the waves
         float mc[NP], unit[NP], up[NP], f[NP], own[NP];
@@ -341,6 +365,11 @@ __device__ __forceinline__ void chunks_of_tile(const kv8_shared_args& a, uint8_t
 #pragma unroll
                 for (int n = 0; n < 2; ++n) acc[g][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, vc[p][n], p == 0 ? zero : acc[g][n], 0, 0, 0);
             }
+        if constexpr (AHEAD) {
+            __builtin_amdgcn_sched_barrier(0);
+            ask_values();
+            __builtin_amdgcn_sched_barrier(0);
+        }
 
         // of each pair two columns a lane
 #pragma unroll
@@ -778,7 +807,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
                     const int r = __builtin_ctzll(__ballot(sum > at)), len = __builtin_amdgcn_readlane(own.len, r), last = __builtin_amdgcn_readlane(sum, r);
                     const int end = __builtin_amdgcn_readlane(own.first, r) + __builtin_amdgcn_readlane(own.count, r);
                     if (len == 0) no_tokens(a, kvh, base + r);
-                    else chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, base + r, 1, len, __builtin_amdgcn_readlane(own.slot, r), end - (last - at), end - max(last - to, 0), 1);
+                    else chunks_of_tile<PACK, WEIGHTS, false, PACK>(a, lds, kvh, base + r, 1, len, __builtin_amdgcn_readlane(own.slot, r), end - (last - at), end - max(last - to, 0), 1);
                     at = min(to, last);
                 }
             }
@@ -809,7 +838,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     }
     int behind = 0;
     if constexpr (FORM != kNoGroups) behind = len > kChunk ? chunks_before(a, mine, row) : 0;
-    chunks_of_tile<PACK, WEIGHTS, false>(a, lds, kvh, row, 1, len, slot, behind + first, a.chunks, a.row_steps);
+    chunks_of_tile<PACK, WEIGHTS, false, FORM == kRuns && PACK>(a, lds, kvh, row, 1, len, slot, behind + first, a.chunks, a.row_steps);
 }
 
 // The chunks of a (row, head) of more than one chunk, folded in ascending order: the operations of kv8_attn_combine_kernel (attn_kv8.hip), down to the

@@ -341,7 +341,8 @@ def _select(policy, logits, positions, out, stream, rules=None):
 
 
 # Tokens, times KV heads, that a step has to read less for groups to pay: with 4 KV heads 4 continuations of 1000 tokens (10 thousand) take 11.7 us a layer in
-# groups and 9.3 each for itself, 16 of 2900 (170 thousand) 13.5 and 15.3, 64 of 4 prompts of 4000 (900 thousand) 21 and 43.
+# groups and 9.3 each for itself, 16 of 2900 (170 thousand) 13.5 and 15.3, 64 of 4 prompts of 4000 (900 thousand) 21 and 43.  And they have to save as much as they leave: 64 of 2000 with up to
+# 2000 tokens of their own 31.8 and 38.7, with up to 4000 56.2 and 52.9; 8 KV heads, 64 of 4000 with up to 4000 98 and 112, with up to 8000 171 and 158.
 GROUPS_FROM = 80_000
 
 
@@ -411,8 +412,9 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
         for b, n in enumerate(lens_host.tolist()):
             st.pages.fork(b * samples, range(b * samples + 1, (b + 1) * samples), n, stream)
         st.pages.reserve(range(B * samples), [T] * (B * samples), torch.repeat_interleave(lens_host, samples).tolist(), stream)
-    saved = (samples - 1) * int((lens_host // api.KV8_SHARED_CHUNK).sum()) * api.KV8_SHARED_CHUNK * c.Hkv
-    groups = list(range(0, B * samples + 1, samples)) if saved >= GROUPS_FROM else None
+    shared = int((lens_host // api.KV8_SHARED_CHUNK).sum()) * api.KV8_SHARED_CHUNK
+    saved, behind = (samples - 1) * shared, samples * (int(lens_host.sum()) - shared)  # tokens that groups need not read, and that rows read for themselves
+    groups = list(range(0, B * samples + 1, samples)) if saved * c.Hkv >= GROUPS_FROM else None
     weights = torch.zeros(st.pages.table.shape, dtype=torch.float32, device=dev) if evict is not None else None
     st.groups, st.weights = groups, weights
     of_rules = None
@@ -432,6 +434,8 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
         api.det_decode_advance(gen[j - 1], base_pos, j, st.tokens, st.positions, stream)
         if evict is not None and j % evict.every == 0:
             st.pages.evict(weights, st.positions, kept_pages, evict.first, evict.recent, stream)
+        if saved < behind + j * B * samples:
+            st.groups = None
         st.forward(stream)
         _select(policy, st.logits, st.positions, gen[j], stream, of_rules)
         if keep_logits:
