@@ -795,9 +795,10 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
             }
         }
         nth -= group_wgs;
-        if (a.row_steps == 0) {
-            // what all rows read for themselves in row_wgs runs
-            run_of(count_own(a, mine), nth, row_wgs, at, to);
+        // what all rows read for themselves in row_wgs runs; of a chunk or two each, a row is a run
+        const int all = a.row_steps == 0 ? count_own(a, mine) : 0;
+        if (a.row_steps == 0 && (row_wgs != a.R || all > 2 * a.R)) {
+            run_of(all, nth, row_wgs, at, to);
             int before = 0;
             for (int base = 0; base < a.R && at < to; base += kWave) {
                 const kv8_own own = own_chunks(a, mine, base + (threadIdx.x & 63));
@@ -807,7 +808,8 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
                     const int r = __builtin_ctzll(__ballot(sum > at)), len = __builtin_amdgcn_readlane(own.len, r), last = __builtin_amdgcn_readlane(sum, r);
                     const int end = __builtin_amdgcn_readlane(own.first, r) + __builtin_amdgcn_readlane(own.count, r);
                     if (len == 0) no_tokens(a, kvh, base + r);
-                    else chunks_of_tile<PACK, WEIGHTS, false, PACK>(a, lds, kvh, base + r, 1, len, __builtin_amdgcn_readlane(own.slot, r), end - (last - at), end - max(last - to, 0), 1);
+                    else chunks_of_tile<PACK, WEIGHTS, false, PACK>(a, lds, kvh, base + r, 1, len, __builtin_amdgcn_readlane(own.slot, r), end - (last - at),
+                                                                    end - max(last - to, 0), 1);
                     at = min(to, last);
                 }
             }
@@ -829,7 +831,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
         }
         nth -= a.group_wgs;
     }
-    const int row = nth / a.row_steps, first = nth % a.row_steps;
+    const int row_steps = FORM == kRuns ? max(a.row_steps, 1) : a.row_steps, row = nth / row_steps, first = nth % row_steps;
     int slot;
     const int len = row_length(a, row, slot);
     if (len == 0) {
@@ -838,7 +840,7 @@ __global__ __launch_bounds__(256, FORM == kNoGroups && PACK ? 3 : 2) void kv8_sh
     }
     int behind = 0;
     if constexpr (FORM != kNoGroups) behind = len > kChunk ? chunks_before(a, mine, row) : 0;
-    chunks_of_tile<PACK, WEIGHTS, false, FORM == kRuns && PACK>(a, lds, kvh, row, 1, len, slot, behind + first, a.chunks, a.row_steps);
+    chunks_of_tile<PACK, WEIGHTS, false, FORM == kRuns && PACK>(a, lds, kvh, row, 1, len, slot, behind + first, a.chunks, row_steps);
 }
 
 // The chunks of a (row, head) of more than one chunk, folded in ascending order: the operations of kv8_attn_combine_kernel (attn_kv8.hip), down to the
@@ -1078,15 +1080,14 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
             // Two workgroups a compute unit.  All of them for runs of several chunks, with those of the rows' own chunks behind them; where the shared chunks
             // need not fill them, they are split between both.  60 rows of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7;
             // 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
-            // What rows read for themselves: where (row, KV head) alone would leave units idle, in equal runs; else a workgroup each, which the dispatcher
-            // levels.  Against two to eight workgroups a row: 16 rows of up to 16000 tokens behind 512 shared ones 120 -> 70 us, 4 of up to 30000 60 -> 41, 16 of 4
-            // prompts of 1000 with up to 8000 78 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.3, 8 of 20000 with up to 100 21.9 -> 22.8: the counting.  Equal runs
-            // for more rows lose: 64 of 4 prompts of 2000, 4 KV heads, 17.6 -> 20.2, 32 of 8 prompts of 4000 28.6 -> 31.5.
+            // What rows read for themselves, in equal runs.  Few rows: against two to eight workgroups a row 16 rows of up to 16000 tokens behind 512 shared ones
+            // 120 -> 70 us, 4 of up to 30000 60 -> 41, 16 of 4 prompts of 1000 with up to 8000 78 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.2, 8 of 20000
+            // with up to 100 21.9 -> 22.8: the counting.  Up to 64 rows: as many runs as rows; against a workgroup a row 64 rows of 4000 with up to 8000 171 -> 150,
+            // of 2000 with up to 4000 94 -> 76, 32 of 4 prompts of 2000 with up to 2000 32.6 -> 29.1, but of 8000 with a chunk 43.3 -> 44.3 and, if rows of a chunk
+            // or two were cut too, 60 of 6 prompts 28.4 -> 32.2.  More rows: a workgroup each; counting 256 costs more than it levels (90 -> 110).
             const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS, few = (long long)R * cache.Hkv < DET_KV8_RUN_WGS / 2;
-            if (few) {
-                a.row_steps = 0;
-                a.row_wgs = several ? of_head((long long)R * a.chunks, DET_KV8_OWN_WGS) : 0;
-            }
+            if (few || R <= kWave) a.row_steps = 0;
+            a.row_wgs = !few ? R : several ? of_head((long long)R * a.chunks, DET_KV8_OWN_WGS) : 0;
             a.group_wgs = several ? of_head(most, DET_KV8_RUN_WGS) : few ? of_head(most + (long long)R * a.chunks, DET_KV8_RUN_WGS) : of_head(most, DET_KV8_RUN_WGS / 2);
         } else {
             // a group of n rows has at most n / rows_per_tile + 1 tiles, and at most n

@@ -341,8 +341,8 @@ def _select(policy, logits, positions, out, stream, rules=None):
 
 
 # Tokens, times KV heads, that a step has to read less for groups to pay: with 4 KV heads 4 continuations of 1000 tokens (10 thousand) take 11.7 us a layer in
-# groups and 9.3 each for itself, 16 of 2900 (170 thousand) 13.5 and 15.3, 64 of 4 prompts of 4000 (900 thousand) 21 and 43.  And they have to save as much as they leave: 64 of 2000 with up to
-# 2000 tokens of their own 31.8 and 38.7, with up to 4000 56.2 and 52.9; 8 KV heads, 64 of 4000 with up to 4000 98 and 112, with up to 8000 171 and 158.
+# groups and 9.3 each for itself, 16 of 2900 (170 thousand) 13.5 and 15.3, 64 of 4 prompts of 4000 (900 thousand) 21 and 43.  And they have to save half of what they leave: 64 of 4000 with up to
+# 8000 tokens of their own 76 and 90 us; with 8 KV heads 64 of 1000 with up to 4000 77.6 and 78.3, of 16 prompts of 1000 86 and 82, 16 of 512 with up to 16000 71 and 68.
 GROUPS_FROM = 80_000
 
 
@@ -434,7 +434,7 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
         api.det_decode_advance(gen[j - 1], base_pos, j, st.tokens, st.positions, stream)
         if evict is not None and j % evict.every == 0:
             st.pages.evict(weights, st.positions, kept_pages, evict.first, evict.recent, stream)
-        if saved < behind + j * B * samples:
+        if 2 * saved < behind + j * B * samples:
             st.groups = None
         st.forward(stream)
         _select(policy, st.logits, st.positions, gen[j], stream, of_rules)

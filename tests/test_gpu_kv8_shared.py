@@ -206,12 +206,14 @@ def test_groups_of_many_rows(d, what, common, lengths, Hq, Hkv):
 BEHIND = [
     ("one group", [512], [[600 + 397 * i for i in range(15)] + [0, 512]]),
     ("no group shares anything", [0, 192], [[900 + 90 * i for i in range(12)], [200, 2000, 192, 3000]]),
+    ("forty rows", [512, 1024], [[513 + 97 * i for i in range(25)] + [0, 511, 3], [1025 + 61 * i for i in range(12)]]),
+    ("forty rows of a chunk or two", [512], [[513 + 7 * i for i in range(36)] + [0, 511, 3, 900]]),
     ("many groups", [256 * (g % 4) for g in range(100)], [[256 * (g % 4) + 1 + 31 * g % 1500, 256 * (g % 4) + 2 * g] for g in range(100)]),
     ("long and short behind groups of every size", [256 * (g % 3) for g in range(70)], [[1000 + 40 * g, 530 + g, 777][:1 + g % 3] for g in range(70)]),
 ]
 
 
-@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (8, 1), (6, 2)])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (8, 1), (6, 2), (16, 8)])
 @pytest.mark.parametrize("what,common,lengths", BEHIND, ids=[s[0] for s in BEHIND])
 def test_rows_with_much_behind_what_they_share(d, what, common, lengths, Hq, Hkv):
     c = SharedCache(800 + Hq, Hkv, common, lengths)
