@@ -909,6 +909,8 @@ __device__ __forceinline__ void combine_heads(const kv8_shared_args& a, size_t b
 // weights_out[slot] = weights_in[slot] + what sixteen chunks' pages get from the rows that name the slot.  A thread has one chunk and every eighth
 // head; the rows' largest scores and sums are folded here again, beside the heads' own workgroups instead of behind them.  Sums in a fixed order:
 // of each eighth the rows ascending and in a row its heads, then the eighths.  A row whose softmax is not finite adds nothing.
+// Bound by trips to memory: row, statistics, what is added.  Beside the folding 24 rows of 32 heads and up to 24 chunks 5.9 us, 8 of 16 heads and up to 79 chunks 7.2, with
+// the statistics asked for behind one another 7.1 and 9.8.
 constexpr int kWeightChunks = 16, kWeightParts = kCombineThreads / kWeightChunks;
 constexpr int kWeightHeads = 4, kStatChunks = 32;  // heads of a thread, chunks of a head, that are asked for at once
 struct weights_lds {
