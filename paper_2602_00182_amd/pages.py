@@ -2,8 +2,8 @@
 
 A pool of pages for all layers and a table [slots, max_pages] on the device that names the pages of each slot.  Slots may share pages (`fork`); a shared
 page is copied before a slot may write into it (`reserve`); a page that no slot names is free again.  A slot may give up pages that its attention gave
-little weight to (`evict`); they are holes in its table, and the tokens behind them keep their positions.  The table tensor keeps its address, so a captured
-graph sees what it holds at the replay."""
+little weight to (`evict`); they are holes in its table, the tokens behind them keep their positions, and they stay holes while the slot goes on.  The table
+tensor keeps its address, so a captured graph sees what it holds at the replay."""
 from __future__ import annotations
 
 import contextlib
@@ -27,6 +27,7 @@ class KVPages:
         self._host = torch.full((n_slots, max_pages), -1, dtype=torch.int32)
         self._pages = [[] for _ in range(n_slots)]  # of each slot, in order
         self._forked = [0] * n_slots                # tokens of each slot up to which a fork shared its pages: it goes on behind them
+        self._left = [None] * n_slots               # tokens at which a fork or a truncation left a slot that has not grown since
         self._refs = [0] * n_pages
         self._free = list(range(n_pages))           # a heap: the lowest page first
         self.version = 0                            # another one whenever the table has changed
@@ -68,7 +69,8 @@ class KVPages:
     def reserve(self, slots, lengths, write_from=None, stream=None) -> None:
         """Makes room for the first lengths[i] tokens of slots[i], and the pages from token write_from[i] on the slot's own: a shared page among
         them is copied where tokens in front of write_from[i] lie in it, else replaced.  Default: the slot is written behind the tokens that the longest of
-        its forks shared (or that a truncation left of them), if lengths[i] reaches beyond them; a slot that writes further in front says so."""
+        its forks shared (or that a truncation left of them), if lengths[i] reaches beyond them; a slot that writes further in front says so.
+        Pages that a slot gave up get a page again where they begin at write_from[i] or behind, and none by default."""
         slots, lengths = list(slots), list(lengths)
         self._slots(*slots)
         if len(set(slots)) != len(slots) or len(lengths) != len(slots) or (write_from is not None and len(write_from) != len(slots)):
@@ -82,14 +84,19 @@ class KVPages:
                 begin = int(write_from[i])
             else:
                 begin = self._forked[slot] if length > self._forked[slot] else len(have) * api.KV8_PAGE
+                left = self._left[slot]
+                if left is not None and left < length and left % api.KV8_PAGE and have[left // api.KV8_PAGE] < 0:
+                    raise ValueError("what is written next lies in a page that was given up")
             if begin < 0:
                 raise ValueError("bad write_from")
-            want.append((slot, begin, count))
+            want.append((slot, begin, count, length))
         # how many references to each page go before its last sharer may keep it
         refs = dict()
-        for slot, begin, count in want:
+        for slot, begin, count, _ in want:
             for i, page in enumerate(self._pages[slot][begin // api.KV8_PAGE:], begin // api.KV8_PAGE):
                 if page < 0:
+                    if write_from is None:
+                        continue
                     if i * api.KV8_PAGE < begin:
                         raise ValueError("tokens in front of write_from lie in a page that was given up")
                     need += 1
@@ -103,9 +110,13 @@ class KVPages:
             raise OutOfPages(f"{need} pages wanted, {len(self._free)} free")
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             copies = []
-            for slot, begin, count in want:
+            for slot, begin, count, length in want:
                 pages = self._pages[slot]
+                if self._left[slot] is not None and length > self._left[slot]:
+                    self._left[slot] = None
                 for i in range(begin // api.KV8_PAGE, len(pages)):
+                    if pages[i] < 0 and write_from is None:
+                        continue
                     if pages[i] < 0:
                         pages[i] = heapq.heappop(self._free)
                         self._refs[pages[i]] = 1
@@ -133,7 +144,7 @@ class KVPages:
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             for s in dsts:
                 self._pages[s] = self._pages[src][:count]
-                self._forked[s] = length
+                self._forked[s] = self._left[s] = length
                 self._forked[src] = max(self._forked[src], length)
                 for page in self._pages[s]:
                     if page >= 0:
@@ -149,6 +160,8 @@ class KVPages:
             keep = -(-length // api.KV8_PAGE)
             for page in self._pages[slot][keep:]:
                 self._drop(page)
+            if length < len(self._pages[slot]) * api.KV8_PAGE:
+                self._left[slot] = length
             del self._pages[slot][keep:]
             self._forked[slot] = min(self._forked[slot], length)
             self._write_table()
