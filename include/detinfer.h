@@ -268,7 +268,9 @@ int det_sample(const float *logits, int B, int V, float temperature, int top_k, 
  *   c > 0 of its occurrences are generated ones (index generated_from[b] or behind):  z = (z - frequency * c) - presence;
  *   t has an entry in the row's biases:  z = z + its value (several entries: the last one);
  *   the bit of t in the row's mask is 0:  z = -inf.
- * A token that no rule reaches keeps its bits.  A row whose mask allows nothing is -inf throughout: det_argmax gives 0 there.
+ * A token that no rule reaches keeps its bits.  A row whose mask allows nothing is -inf throughout.  Of such a row det_argmax gives token 0 and det_sample, for
+ * every seed, the last of its candidates, token min(top_k, V) - 1: both barred, and det_logits_advance takes the transition of whatever token it is given.  A
+ * caller who cannot rule such a row out looks at the chosen token's mask.
  * det_logits_rules: device pointers; the part whose first pointer is NULL is left out.
  *   penalties [B, 3] fp32: repetition (> 0), frequency, presence.  history [n_history, ld_history] int32, of which row b has the first history_lens[b] ids
  *   (0..ld_history) of row history_rows[b] (NULL: b; outside 0..n_history-1: none); ids outside 0..V-1 are ignored; generated_from [B] or NULL (0).

@@ -215,18 +215,50 @@ class SamplingPolicy:
 class Grammar:
     """Which tokens may come where, as an automaton over classes of tokens: in state s the tokens whose bit in masks[s] ([n_states, ceil(V / 32)] int32) is
     set; a token leads to transitions[s, class] ([n_states, n_classes] int32; -1: nothing is barred from there on).  token_class [V] int32 or None (every
-    token is its own class); start: the state in which every sequence begins.  Tensors on the device."""
+    token is its own class); start: the state in which every sequence begins.  Tensors on the device.  A state that start leads to has to allow a token:
+    in one without, every logit would be -inf, the choice a barred token all the same, and nothing barred behind it.  That is looked at once, here, on the host."""
     masks: torch.Tensor
     transitions: torch.Tensor
     token_class: torch.Tensor | None = None
     start: int = 0
+
+    def __post_init__(self):
+        if self.masks.dim() != 2 or self.transitions.dim() != 2 or (self.token_class is not None and self.token_class.dim() != 1):
+            raise ValueError("masks [n_states, words], transitions [n_states, n_classes] and the class of each token")
+        if self.masks.shape[0] != self.transitions.shape[0] or 32 * self.masks.shape[1] < self.tokens or not 0 <= self.start < self.masks.shape[0]:
+            raise ValueError("a mask over all tokens for each state, and one of them to begin in")
+        self.check(self.tokens)
+
+    @property
+    def tokens(self) -> int:
+        return self.transitions.shape[1] if self.token_class is None else self.token_class.shape[0]
+
+    def check(self, V: int, barred=()) -> None:
+        """Refuses states that start leads to without a token below V beside the barred ones."""
+        n, n_classes = self.transitions.shape
+        V = min(V, self.tokens)
+        masks, transitions = self.masks.cpu(), self.transitions.cpu()
+        of = torch.arange(V) if self.token_class is None else self.token_class[:V].cpu().long()
+        there = torch.ones(V, dtype=torch.bool)
+        there[[t for t in barred if 0 <= t < V]] = False
+        seen, todo = {self.start}, [self.start]
+        while todo:
+            state = todo.pop()
+            allowed = ((masks[state][:, None] >> torch.arange(32, dtype=torch.int32)) & 1).flatten()[:V].bool() & there
+            if not allowed.any():
+                raise ValueError(f"state {state} of the grammar allows no token")
+            classes = of[allowed].unique()
+            to = transitions[state][classes[(classes >= 0) & (classes < n_classes)]].unique().tolist()
+            new = [s for s in to if 0 <= s < n and s not in seen]
+            seen.update(new)
+            todo += new
 
 
 @dataclass
 class LogitsPolicy:
     """Rules on the logits of every step (det_logits_process): tokens of the prompt or generated so far are made less likely by `repetition` (their
     logits divided, where positive, or multiplied by it), generated ones also by `frequency` for each time and by `presence` once; `biases`
-    {token: added}; `grammar`.  The same for every sequence of a call."""
+    {token: added}; `grammar`, of which the biases may not bar (-inf) all that a state allows.  The same for every sequence of a call."""
     repetition: float = 1.0
     frequency: float = 0.0
     presence: float = 0.0
@@ -262,13 +294,17 @@ class _Rules:
             self.lens = begin.clone()
             values = torch.tensor([policy.repetition, policy.frequency, policy.presence], dtype=torch.float32)
             given |= dict(penalties=values.repeat(B, 1).to(dev), history=self.history, history_lens=self.lens, generated_from=begin)
+        barred = []
         if policy.biases:
             n = len(policy.biases)
-            given |= dict(bias_begin=(torch.arange(B + 1, dtype=torch.int32) * n).to(dev),
-                          bias_tokens=torch.tensor(list(policy.biases), dtype=torch.int32).repeat(B).to(dev),
-                          bias_values=torch.tensor(list(policy.biases.values()), dtype=torch.float32).repeat(B).to(dev))
+            tokens, added = torch.tensor(list(policy.biases), dtype=torch.int32), torch.tensor(list(policy.biases.values()), dtype=torch.float32)
+            barred = tokens[torch.isneginf(added)].tolist()
+            given |= dict(bias_begin=(torch.arange(B + 1, dtype=torch.int32) * n).to(dev), bias_tokens=tokens.repeat(B).to(dev),
+                          bias_values=added.repeat(B).to(dev))
         if policy.grammar is not None:
             self.grammar = policy.grammar
+            if barred or V < self.grammar.tokens:
+                self.grammar.check(V, barred)
             self.states = torch.full((B,), policy.grammar.start, **i32)
             given |= dict(masks=policy.grammar.masks, mask_rows=self.states)
         self.rules = api.logits_rules(**given)
