@@ -557,7 +557,8 @@ int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_tab
 /* det_attn_decode_kv8 for rows whose first tokens lie in the same pages (continuations of a prompt, a document that all requests begin with): the
  * shared chunks are read once for a group of rows.  Group g: rows group_rows[g] .. group_rows[g+1]-1 (group_rows ascending; rows in no group are read for
  * themselves), which hold their first shared[g] tokens in the same pages; of these the whole chunks of 256 tokens are read through the table of the
- * group's first row, whatever the tables of its other rows of more than 256 tokens name there.  A row may be shorter than what its group shares.
+ * group's first row, or, where that row has no slot or ends in front of their end, of the first that reaches it (of none: of the longest), whatever
+ * the tables of its other rows of more than 256 tokens name there.  A row may be shorter than what its group shares.
  * Output bytes are those of det_attn_decode_kv8 (whose arguments, rules and errors hold; slots NULL or not), whatever the groups.
  *   group_rows [n_groups + 1], shared [n_groups] int32;  0 <= n_groups <= R (n_groups = 0: both may be NULL);  R <= 65535;
  *   ws: det_attn_decode_kv8_shared_workspace_bytes bytes. */
