@@ -1109,7 +1109,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
             // of 2000 with up to 4000 94 -> 76, 32 of 4 prompts of 2000 with up to 2000 32.6 -> 29.1, but of 8000 with a chunk 43.3 -> 44.3 and, if rows of a chunk
             // or two were cut too, 60 of 6 prompts 28.4 -> 32.2.  More rows: a workgroup each; counting 256 costs more than it levels (90 -> 110).
             const bool several = most * cache.Hkv >= 2 * DET_KV8_RUN_WGS, few = (long long)R * cache.Hkv < DET_KV8_RUN_WGS / 2;
-            if (few || R <= kWave) a.row_steps = 0;
+            if (few || R <= DET_KV8_EVEN_ROWS) a.row_steps = 0;
             a.row_wgs = !few ? R : several ? of_head((long long)R * a.chunks, DET_KV8_OWN_WGS) : 0;
             a.group_wgs = several ? of_head(most, DET_KV8_RUN_WGS) : few ? of_head(most + (long long)R * a.chunks, DET_KV8_RUN_WGS) : of_head(most, DET_KV8_RUN_WGS / 2);
         } else {

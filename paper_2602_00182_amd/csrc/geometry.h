@@ -15,5 +15,6 @@
 #define DET_KV8_RING_CHUNKS 256    // (tile, chunk, KV head) of a call with groups from which shared chunks go to four tiles together
 #define DET_KV8_RUN_WGS 512        // workgroups that take runs of shared chunks
 #define DET_KV8_OWN_WGS 384        // and that take what few rows have behind them
+#define DET_KV8_EVEN_ROWS 64       // rows up to which that is cut into equal runs
 #define DET_KV8_RUN_ROWS 128       // rows of a call from which the 8-bit cache's value heads are stored in runs
 #define DET_ATTN_TURN_CHUNKS 32    // chunks of a cache up to which they change places from stream to stream
