@@ -165,7 +165,7 @@ class DecodeState:
                     self._told[g] = told
                 if weighs not in self._spaces:
                     size = self.model.layer_workspace_bytes(self.lcfg, rows, step=api.kv8_step(weights=self.weights))
-                    self._spaces[weighs] = torch.empty(size, dtype=torch.uint8, device=dev)
+                    self._spaces[weighs] = self.ws if size <= self.ws.nbytes else torch.empty(size, dtype=torch.uint8, device=dev)
         step = api.kv8_step(*(told[:2] if g else (None, None)), self.weights)
         return step, self._spaces[weighs]
 
