@@ -449,10 +449,8 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
             st.pages.fork(b * samples, range(b * samples + 1, (b + 1) * samples), n, stream)
         st.pages.reserve(range(B * samples), [T] * (B * samples), torch.repeat_interleave(lens_host, samples).tolist(), stream)
     shared = int((lens_host // api.KV8_SHARED_CHUNK).sum()) * api.KV8_SHARED_CHUNK
-    saved, behind = (samples - 1) * shared, samples * (int(lens_host.sum()) - shared)  # tokens that groups need not read, and that rows read for themselves
-    groups = list(range(0, B * samples + 1, samples)) if saved * c.Hkv >= GROUPS_FROM else None
     weights = torch.zeros(st.pages.table.shape, dtype=torch.float32, device=dev) if evict is not None else None
-    st.groups, st.weights = groups, weights
+    st.groups, st.weights = list(range(0, B * samples + 1, samples)) if samples > 1 else None, weights
     of_rules = None
     if rules is not None:
         out = torch.empty_like(st.logits) if keep_logits else None
@@ -469,9 +467,13 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
     for j in range(1, n_new):
         api.det_decode_advance(gen[j - 1], base_pos, j, st.tokens, st.positions, stream)
         if evict is not None and j % evict.every == 0:
-            st.pages.evict(weights, st.positions, kept_pages, evict.first, evict.recent, stream)
-        if 2 * saved < behind + j * B * samples:
-            st.groups = None
+            gone = st.pages.evict(weights, st.positions, kept_pages, evict.first, evict.recent, stream)
+            if st.groups is not None and any(gone):  # continuations give up pages of their own choice, and share those in front of the first that differs
+                shared = sum(st.pages.shared_tokens(range(a, b)) // api.KV8_SHARED_CHUNK for a, b in zip(st.groups, st.groups[1:])) * api.KV8_SHARED_CHUNK
+        if st.groups is not None:
+            saved, behind = (samples - 1) * shared, samples * (R - shared + j * B)  # tokens that groups need not read, and that rows read for themselves
+            if saved * c.Hkv < GROUPS_FROM or 2 * saved < behind:
+                st.groups = None
         st.forward(stream)
         _select(policy, st.logits, st.positions, gen[j], stream, of_rules)
         if keep_logits:
