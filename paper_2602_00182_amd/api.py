@@ -820,9 +820,9 @@ def _groups(group_rows, shared):
     """(group_rows, shared, n_groups) of a call; None and None: no groups."""
     if group_rows is None and shared is None:
         return None, None, 0
-    n, = shared.shape
-    if group_rows.shape != (n + 1,):
+    if group_rows is None or shared is None or shared.dim() != 1 or group_rows.shape != (shared.shape[0] + 1,):
         raise ValueError("n_groups + 1 first rows for the shared tokens of n_groups groups")
+    n, = shared.shape
     return _contig(group_rows, torch.int32), _contig(shared, torch.int32), n
 
 
@@ -981,8 +981,10 @@ def logits_rules(history=None, history_lens=None, history_rows=None, generated_f
         nonlocal B
         if t is None:
             return None
+        if t.dim() != 1:
+            raise ValueError(f"{what}: one value for each row of logits")
         n = t.shape[0] - (what == "bias_begin")
-        if t.dim() != 1 or (B is not None and n != B):
+        if B is not None and n != B:
             raise ValueError(f"{what}: one value for each row of logits")
         B = n
         return _contig(t, torch.int32)
@@ -1022,6 +1024,8 @@ def det_logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
     B, V = shape
     dtype = logits.dtype
     (ld_in, each), (ld_out, other) = logits.stride(), out.stride()
+    if dtype not in _LOGITS:
+        raise TypeError("logits must be fp32 or bf16")
     if out.shape != shape or out.dtype != dtype or each != 1 or other != 1 or rules._rows not in (None, B):
         raise ValueError("bad logits or rules of other rows")
     if B == 1:  # the stride of a single row says nothing
@@ -1039,11 +1043,15 @@ def det_logits_advance(tokens, history, lens_in, lens_out, transitions=None, tok
     most = V = n_states = n_classes = 0
     had = n_in = n_out = to = classes = s_in = s_out = None
     if history is not None:
+        if lens_in is None or lens_out is None:
+            raise ValueError("a history goes with its lengths")
         rows, most = history.shape
         if rows != B or lens_in.shape != of_rows or lens_out.shape != of_rows:
             raise ValueError("bad history")
         had, n_in, n_out = _contig(history, i32), _contig(lens_in, i32), _contig(lens_out, i32)
     if transitions is not None:
+        if states_in is None or states_out is None:
+            raise ValueError("transitions go with states")
         n_states, n_classes = transitions.shape
         V = n_classes
         if token_class is not None:
