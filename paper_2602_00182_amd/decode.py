@@ -376,10 +376,18 @@ def _select(policy, logits, positions, out, stream, rules=None):
                        positions, out, stream)
 
 
-# Tokens, times KV heads, that a step has to read less for groups to pay: with 4 KV heads 4 continuations of 1000 tokens (10 thousand) take 11.7 us a layer in
-# groups and 9.3 each for itself, 16 of 2900 (170 thousand) 13.5 and 15.3, 64 of 4 prompts of 4000 (900 thousand) 21 and 43.  And they have to save half of what they leave: 64 of 4000 with up to
-# 8000 tokens of their own 76 and 90 us; with 8 KV heads 64 of 1000 with up to 4000 77.6 and 78.3, of 16 prompts of 1000 86 and 82, 16 of 512 with up to 16000 71 and 68.
+# Where groups pay: `saved` tokens that a step need not read, `behind` tokens that its rows read for themselves, of n_groups of `samples` rows.  Beside the
+# fixed cost of groups each of them costs some, what rows read behind them is read slower, and two rows a group hardly gain: plain calls find in cache what
+# another row has read.  Over 5468 calls of 1 to 32 KV heads, 1 to 16 heads each, 1 to 48 prompts of 260 to 16400 tokens, 2 to 64 rows each and up to
+# 4000 tokens of their own the rule takes groups for 2283: together 90 ms without and 62 with them, 8 lose more than 3 % (7 % at most).  Of 700 others, drawn, it
+# took 423, of which 2 lost more than 3 % (10 %).  (saved * Hkv >= 80000 and 2 * saved >= behind alone let 317 of 3459 lose that much: 48 prompts of 300 tokens with 3
+# rows each, 32/32 heads 59 -> 79 us, 16 of 4100 with 2 rows and 4000 tokens of their own, 32/8 heads 95 -> 120.)  Groups gain most with many rows: 64
+# of 4 prompts of 4000 tokens, 16/4 heads, 43 -> 21 us.
 GROUPS_FROM = 80_000
+
+
+def _groups_pay(n_groups: int, samples: int, Hkv: int, saved: int, behind: int) -> bool:
+    return (saved - 0.8 * behind) * Hkv >= GROUPS_FROM * ((3 if samples == 2 else 1) + n_groups * Hkv / 80)
 
 
 def prefill_decode(model: DecodeModel, prompts: torch.Tensor, prompt_lens: torch.Tensor, n_new: int,
@@ -472,7 +480,7 @@ def _prefill_decode(model, prompts, prompt_lens, n_new, rope_cos, rope_sin, stre
                 shared = sum(st.pages.shared_tokens(range(a, b)) // api.KV8_SHARED_CHUNK for a, b in zip(st.groups, st.groups[1:])) * api.KV8_SHARED_CHUNK
         if st.groups is not None:
             saved, behind = (samples - 1) * shared, samples * (R - shared + j * B)  # tokens that groups need not read, and that rows read for themselves
-            if saved * c.Hkv < GROUPS_FROM or 2 * saved < behind:
+            if not _groups_pay(B, samples, c.Hkv, saved, behind):
                 st.groups = None
         st.forward(stream)
         _select(policy, st.logits, st.positions, gen[j], stream, of_rules)
