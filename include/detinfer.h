@@ -277,7 +277,7 @@ int det_sample(const float *logits, int B, int V, float temperature, int top_k, 
  *   bias_begin [B + 1]: row b's entries are bias_begin[b] .. bias_begin[b+1]-1 of bias_tokens, bias_values [n_biases].
  *   masks [n_masks, mask_words]: bit t % 32 of word t / 32; mask_rows [B]: the row's mask (NULL: b; outside 0..n_masks-1: none).
  * logits, out [B, V] fp32 (DET_F32) or bf16 (DET_BF16: computed in fp32, rounded once) with row strides ld >= V in elements; out may be logits (with
- * its stride), else the two may not overlap.  16-byte aligned (rows need not be).  B <= 65535, V <= 2^30, 32 mask_words >= V;  ld_history and n_biases
+ * its stride), else the two may not overlap, nor rows of the one lie between rows of the other.  16-byte aligned (rows need not be).  B <= 65535, V <= 2^30, 32 mask_words >= V;  ld_history and n_biases
  * at most 2^30. */
 typedef struct det_logits_rules {
     const float *penalties;
@@ -561,6 +561,7 @@ int det_attn_decode_kv8(const void *q, const void *pool, const int32_t *page_tab
  * the tables of its other rows of more than 256 tokens name there.  A row may be shorter than what its group shares.
  * Output bytes are those of det_attn_decode_kv8 (whose arguments, rules and errors hold; slots NULL or not), whatever the groups.
  *   group_rows [n_groups + 1], shared [n_groups] int32;  0 <= n_groups <= R (n_groups = 0: both may be NULL);  R <= 65535;
+ *   DET_ESHAPE also for calls of 2^23 workgroups and more (from R Hkv = 2^22 on);
  *   ws: det_attn_decode_kv8_shared_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_shared_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
 int det_attn_decode_kv8_shared(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,
@@ -572,7 +573,8 @@ int det_attn_decode_kv8_shared(const void *q, const void *pool, const int32_t *p
  *   weights_out[s][i] = weights_in[s][i] + sum over the rows r that name slot s, the heads h and the tokens j of page i (64 i .. 64 i + 63) of p[r][h][j],
  * p the softmax of row r and head h.  fp32, in a fixed order: of each row (ascending) the heads (ascending) into the sum h mod 8, these eight in order, then
  * onto weights_in.  A (row, head) whose softmax is not finite adds nothing.  Output bytes as above.
- *   weights_in, weights_out [n_slots, max_pages] fp32, every entry written; weights_in NULL: zeros; the two may be the same array.  n_slots <= 65535.
+ *   weights_in, weights_out [n_slots, max_pages] fp32, every entry written; weights_in NULL: zeros; the two may be the same array.  n_slots <= 65535,
+ *   and n_slots * ceil(max_pages / 64) + R Hq / 2 below 2^24 (DET_ESHAPE).
  *   ws: det_attn_decode_kv8_weights_workspace_bytes bytes. */
 size_t det_attn_decode_kv8_weights_workspace_bytes(int R, int Hq, int Hkv, int D, int max_pages);
 int det_attn_decode_kv8_weights(const void *q, const void *pool, const int32_t *page_table, int n_pages, int n_slots,

@@ -1024,14 +1024,15 @@ def det_logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
     B, V = shape
     dtype = logits.dtype
     (ld_in, each), (ld_out, other) = logits.stride(), out.stride()
-    if dtype not in _LOGITS:
+    kind = _LOGITS.get(dtype)
+    if kind is None:
         raise TypeError("logits must be fp32 or bf16")
     if out.shape != shape or out.dtype != dtype or each != 1 or other != 1 or rules._rows not in (None, B):
         raise ValueError("bad logits or rules of other rows")
     if B == 1:  # the stride of a single row says nothing
         ld_in, ld_out = max(ld_in, V), max(ld_out, V)
     _check("det_logits_process", lib().det_logits_process(
-        _ptr(logits), ld_in, _ptr(out), ld_out, _LOGITS[dtype], B, V, C.byref(rules), _stream(stream)))
+        _ptr(logits), ld_in, _ptr(out), ld_out, kind, B, V, C.byref(rules), _stream(stream)))
 
 
 def det_logits_advance(tokens, history, lens_in, lens_out, transitions=None, token_class=None, states_in=None, states_out=None, stream=None) -> None:

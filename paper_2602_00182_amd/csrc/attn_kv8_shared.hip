@@ -1101,7 +1101,7 @@ int attn_shared_kv8_impl(const void* q, const kv8_cache& cache, const int32_t* s
         if (ring) {
             const long long sets = ((long long)R + 4 * a.rows_per_tile - 1) / (4 * a.rows_per_tile), most = (sets > step.n_groups ? sets : step.n_groups) * a.chunks;
             // Two workgroups a compute unit.  All of them for runs of several chunks, with those of the rows' own chunks behind them; where the shared chunks
-            // need not fill them, they are split between both.  60 rows of 6 prompts of 300 to 4000 tokens 35 -> 32 us, 32 of 4 prompts of 4000 27.4 -> 23.7;
+            // need not fill them, they are split between both.  60 rows of 6 prompts of 300 to 4000 tokens 35 -> 32 us (28.5 with the steps since), 32 of 4 prompts of 4000 27.4 -> 23.7;
             // 32 of 8 prompts of 4000 would lose (31.9 -> 34.4).
             // What rows read for themselves, in equal runs.  Few rows: against two to eight workgroups a row 16 rows of up to 16000 tokens behind 512 shared ones
             // 120 -> 70 us, 4 of up to 30000 60 -> 41, 16 of 4 prompts of 1000 with up to 8000 78 -> 44; but 16 of 2900 with up to 500 16.0 -> 16.2, 8 of 20000

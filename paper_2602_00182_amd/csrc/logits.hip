@@ -4,7 +4,7 @@
 // A workgroup takes a stretch of 4096 of one row's tokens.  It counts the history's tokens that lie in the stretch in LDS (integers: their order is free)
 // while the logits are on their way, so a history of any length costs no table in memory and nothing is kept from step to step; every stretch of a row
 // reads the whole history, which comes from L2.  Bound by memory: 64 rows of 128000 fp32 logits without rules 11.8 us (65 MB: 5.5 TB/s), with histories of
-// 100 to 4000 tokens 15.6, with biases and masks too 16.5.  Smaller stretches read the history more often (2048 tokens 17.8), larger ones leave too few
+// 100 to 4000 tokens 15.6, with biases and masks too 16.5 (the median of a profiled run, whose inputs change, 17.0).  Smaller stretches read the history more often (2048 tokens 17.8), larger ones leave too few
 // waves a compute unit (8192 tokens 19 to 28), and ids asked for one after the other, not eight a lane, took 25.
 //
 // A vector of logits that the mask takes whole is not read.  In place, nothing that no rule reaches is read or written.

@@ -269,7 +269,8 @@ class LogitsPolicy:
 @dataclass
 class EvictPolicy:
     """A sequence of an 8-bit cache comes back to `keep` pages every `every` steps: of those but its first and last ones it gives up the pages that its
-    generated tokens, over all layers and heads, have given the least weight (KVPages.evict)."""
+    generated tokens, over all layers and heads, have given the least weight (KVPages.evict).  A step then reads less; the call's pool has room for all tokens
+    all the same, and what is given up serves no other sequence of it."""
     keep: int
     every: int = 64
     first: int = 1
