@@ -216,7 +216,7 @@ class Grammar:
     """Which tokens may come where, as an automaton over classes of tokens: in state s the tokens whose bit in masks[s] ([n_states, ceil(V / 32)] int32) is
     set; a token leads to transitions[s, class] ([n_states, n_classes] int32; -1: nothing is barred from there on).  token_class [V] int32 or None (every
     token is its own class); start: the state in which every sequence begins.  Tensors on the device.  A state that start leads to has to allow a token:
-    in one without, every logit would be -inf, the choice a barred token all the same, and nothing barred behind it.  That is looked at once, here, on the host."""
+    in one without, every logit would be -inf, the choice a barred token all the same, and nothing barred behind it.  That is looked at once, when it is made."""
     masks: torch.Tensor
     transitions: torch.Tensor
     token_class: torch.Tensor | None = None
@@ -236,19 +236,28 @@ class Grammar:
     def check(self, V: int, barred=()) -> None:
         """Refuses states that start leads to without a token below V beside the barred ones."""
         n, n_classes = self.transitions.shape
-        V = min(V, self.tokens)
-        masks, transitions = self.masks.cpu(), self.transitions.cpu()
-        of = torch.arange(V) if self.token_class is None else self.token_class[:V].cpu().long()
-        there = torch.ones(V, dtype=torch.bool)
+        V, dev = min(V, self.tokens), self.masks.device
+        bit = torch.arange(32, dtype=torch.int32, device=dev)
+        there = torch.ones(V, dtype=torch.bool, device=dev)
         there[[t for t in barred if 0 <= t < V]] = False
+        of = None
+        if self.token_class is not None:  # tokens without a class, in a column behind the others
+            of = self.token_class[:V].long()
+            of = torch.where((of >= 0) & (of < n_classes), of, n_classes)
         seen, todo = {self.start}, [self.start]
         while todo:
-            state = todo.pop()
-            allowed = ((masks[state][:, None] >> torch.arange(32, dtype=torch.int32)) & 1).flatten()[:V].bool() & there
-            if not allowed.any():
-                raise ValueError(f"state {state} of the grammar allows no token")
-            classes = of[allowed].unique()
-            to = transitions[state][classes[(classes >= 0) & (classes < n_classes)]].unique().tolist()
+            states, todo = todo[:64], todo[64:]  # some at a time: a state's tokens take 128 bytes a word of its mask
+            at = torch.tensor(states, device=dev)
+            allowed = ((self.masks[at][..., None] >> bit) & 1).flatten(1)[:, :V].bool() & there
+            some = allowed.any(1).tolist()
+            if not all(some):
+                raise ValueError(f"state {states[some.index(False)]} of the grammar allows no token")
+            classes = allowed
+            if of is not None:
+                row, token = allowed.nonzero(as_tuple=True)
+                classes = torch.zeros((len(states), n_classes + 1), dtype=torch.bool, device=dev)
+                classes[row, of[token]] = True
+            to = self.transitions[at][:, :classes.shape[1]][classes[:, :n_classes]].unique().tolist()
             new = [s for s in to if 0 <= s < n and s not in seen]
             seen.update(new)
             todo += new
